@@ -385,6 +385,86 @@ kvd_status kvd_block_forward(const kvd_attn_shape* shape, const kvd_block_weight
 /* Workspace bytes of kvd_block_forward (0 on invalid arguments).              */
 size_t kvd_block_workspace_bytes(const kvd_attn_shape* shape, int32_t d_ff, int32_t B, int32_t T);
 
+/* Attention of N >= 1 new tokens per sequence over a prefix that the whole batch
+ * shares, then over each sequence's own rows (Eqs. attn_weights, head_output over
+ * CONCAT(prefix, own)).  The prefix's keys and values are read once for all
+ * sequences.  For sequence b, len = own_len[b], n = n_new[b] and token i < n,
+ *   out[b][i][h] = softmax(q . K / sqrt(head_dim)) V
+ * over prefix rows 0 .. T_prefix-1 and own rows t <= len - n + i: the new tokens
+ * are the last n of the sequence's own rows, and each sees the rows up to itself.
+ * A token that sees no row gives out = 0.  Tokens i >= n[b] are not computed and
+ * their out rows are left as they were.  Own rows from len on are never read, and
+ * what a token does not see has no part in its result, whatever it holds.
+ *   q, out   [B][N][n_q_heads][head_dim].
+ *   prefix   K/V [n_kv_heads][t_cap][head_dim], rows t_off .. t_off+T_prefix-1;
+ *            may be NULL iff T_prefix == 0.
+ *   own      K/V [B][n_kv_heads][t_cap][head_dim], rows t_off .. t_off+T_own-1;
+ *            may be NULL iff T_own == 0.   T_prefix + T_own >= 1.
+ *   own_len, n_new   [B] int32 or NULL (T_own and N for every sequence); values are
+ *            taken as clamped to 0 .. T_own and 0 .. N.
+ *   weight   NULL, or [B][n_kv_heads][own->t_cap] fp32: what each own row t < len got,
+ *              weight[b][j][t_off+t] = decay * weight[b][j][t_off+t]
+ *                                      + sum over tokens i < n, heads h of group j
+ *                                        of the softmax weight of row t,
+ *            the softmax taken over the prefix too.  decay == 0: the earlier values
+ *            are not read (they may be NaN).  Rows from len on are left as they were.
+ *            Needs T_own >= 1.
+ *   ws       kvd_prefix_workspace_bytes(shape, B, N, T_prefix, T_own, weight != NULL)
+ *            bytes, 256-byte aligned, overwritten; it need not be cleared, and calls
+ *            ordered on one stream may share it.
+ * Results repeat bit for bit (no atomics).  The shape's d_model, rms_eps, rope_theta
+ * and w_layout are not used.  Any N; bf16 calls with N * n_q_heads / n_kv_heads <= 16
+ * rows per key keep the softmax weights in fp32, larger ones round each to bf16 before
+ * the value product.  B == 0 or N == 0 is a no-op.                              */
+kvd_status kvd_prefix_attn(const kvd_attn_shape* shape, const void* q, int32_t N,
+                           const kvd_kv_view* prefix, int32_t T_prefix, const kvd_kv_view* own,
+                           const int32_t* own_len, const int32_t* n_new, int32_t B, int32_t T_own,
+                           void* out, float* weight, float decay, void* ws, size_t ws_bytes,
+                           void* stream);
+
+/* Attention of N >= 1 new tokens per sequence over its cache that also adds up the
+ * weight every cached row receives: kvd_prefix_attn without a prefix and with
+ * weight (decay 1: summed over the decode, 0: this call's tokens alone).  T >= 1.
+ * ws: kvd_prefix_workspace_bytes(shape, B, N, 0, T, 1) bytes.                   */
+kvd_status kvd_weighted_attn(const kvd_attn_shape* shape, const void* q, int32_t N,
+                             const kvd_kv_view* kv, const int32_t* kv_len, const int32_t* n_new,
+                             int32_t B, int32_t T, void* out, float* weight, float decay, void* ws,
+                             size_t ws_bytes, void* stream);
+
+/* Workspace bytes of kvd_prefix_attn and kvd_weighted_attn (0 on invalid arguments).
+ * They do not fall as T_prefix or T_own grow from 1 on, so that a decode loop can size
+ * one workspace for its longest call.                                            */
+size_t kvd_prefix_workspace_bytes(const kvd_attn_shape* shape, int32_t B, int32_t N, int32_t T_prefix,
+                                  int32_t T_own, int32_t weights);
+
+/* Eviction by accumulated weight: every (sequence, KV head) of the cache keeps its
+ * n' = min(len, keep) foremost rows of len, in place.  Foremost are
+ *   protected rows: pos < sink, or pos > last_pos[b] - recent (the first positions and
+ *   the newest ones), then
+ *   larger weights (NaN below every number, -0 equal to +0);
+ * equal ones lowest slot first (so of more than n' protected rows the lowest slots
+ * stay).  Kept rows in slots below n' stay where they are; kept rows in slots from n'
+ * on move, in slot order, into the freed slots below n', in slot order, with their
+ * weights and positions: no fewer rows could move.  Afterwards rows 0 .. n'-1 are the
+ * cache (attention does not depend on their order), weight is 0 in slots n' .. len-1,
+ * where new rows will start from, and K, V and pos there are left as they were.
+ *   kv       K/V [B][n_kv_heads][t_cap][head_dim], rows t_off .. t_off+T-1.
+ *   kv_len   [B] int32, read (clamped to 0 .. T) and set to n'; or NULL: T rows in
+ *            every sequence.   T >= 1, keep >= 1.
+ *   weight   [B][n_kv_heads][t_cap] fp32.   pos  [B][n_kv_heads][t_cap] int32, required
+ *            when sink or recent is positive, else NULL or moved along.
+ *   last_pos [B] int32, required when recent is positive.
+ *   sink, recent >= 0.
+ *   ws       kvd_evict_workspace_bytes(shape, B, T) bytes, 256-byte aligned,
+ *            overwritten; it need not be cleared.
+ * Both dtypes.  With keep >= T no row leaves.  B == 0 is a no-op.                 */
+kvd_status kvd_evict(const kvd_attn_shape* shape, const kvd_kv_view* kv, int32_t* kv_len, int32_t B,
+                     int32_t T, int32_t keep, float* weight, int32_t* pos, const int32_t* last_pos,
+                     int32_t sink, int32_t recent, void* ws, size_t ws_bytes, void* stream);
+
+/* Workspace bytes of kvd_evict (0 on invalid arguments).                         */
+size_t kvd_evict_workspace_bytes(const kvd_attn_shape* shape, int32_t B, int32_t T);
+
 /* Merge step of split-K attention: out[b][h] = sum_s w_s acc_s / sum_s w_s l_s
  * with w_s = 2^(m_s - max_s m_s), over the S partial softmax states that a
  * preceding kvd_decode_attn / kvd_cached_attn / kvd_fused_recompute_attn call

@@ -52,6 +52,7 @@ __all__ = [
     "causal_attention",
     "block_forward",
     "recompute_residual",
+    "rows_attention", "evict",
 ]
 
 
@@ -286,3 +287,70 @@ def recompute_residual(h0, pos, layers, n_layers, n_q, n_kv, head_dim, eps, thet
     for i in range(n_layers):
         h = block_forward(h, pos, *layers[i], n_q, n_kv, head_dim, eps, theta)
     return h
+
+
+# ------------------------------------------------------------------ shared prefixes, weights, eviction
+
+def rows_attention(q, pk, pv, k, v, lens, n_new):
+    """Attention of new tokens over a prefix shared by the batch, then over their sequence's own rows.
+
+    q [B, N, n_q, hd]; pk, pv [n_kv, T_prefix, hd] or None; k, v [B, n_kv, T, hd] or None; lens, n_new [B].  Token i
+    < n_new[b] sees the prefix and own rows t <= lens[b] - n_new[b] + i.  Returns (out [B, N, n_q, hd], size [B, N,
+    n_q, hd], weight [B, n_kv, T]): out is 0 where nothing is seen or the token is not new; size is the
+    attention-weighted sum of |V|; weight the sum of the softmax weights each own row received.
+    """
+    q = np.asarray(q, dtype=np.float64)
+    B, N, n_q, hd = q.shape
+    n_kv = (pk if pk is not None else k[0]).shape[0]
+    T = 0 if k is None else k.shape[2]
+    g = n_q // n_kv
+    out, size, weight = np.zeros_like(q), np.zeros_like(q), np.zeros((B, n_kv, T))
+    for b in range(B):
+        for i in range(int(n_new[b])):
+            seen = max(0, int(lens[b]) - int(n_new[b]) + i + 1)
+            for j in range(n_kv):
+                ks = [] if pk is None else [pk[j]]
+                vs = [] if pv is None else [pv[j]]
+                if seen > 0:
+                    ks.append(k[b, j, :seen])
+                    vs.append(v[b, j, :seen])
+                if not ks:
+                    continue
+                kk, vv = np.concatenate(ks).astype(np.float64), np.concatenate(vs).astype(np.float64)
+                for h in range(j * g, j * g + g):
+                    s = kk @ q[b, i, h] / np.sqrt(hd)
+                    p = np.exp(s - s.max())
+                    p /= p.sum()
+                    out[b, i, h] = p @ vv
+                    size[b, i, h] = p @ np.abs(vv)
+                    if seen > 0:
+                        weight[b, j, :seen] += p[p.shape[0] - seen:]
+    return out, size, weight
+
+
+def evict(k, v, weight, pos, lens, last_pos, keep, sink, recent):
+    """Every (b, j) keeps its min(len, keep) foremost rows (protected, then heavier, then lower slot); kept rows behind
+    that many slots move into the freed ones, both in slot order.  pos and last_pos may be None.  Returns new
+    (k, v, weight, pos, lens); rows that nothing moves into stay as they were, weights of freed slots become 0."""
+    k, v, weight = k.copy(), v.copy(), weight.copy()
+    pos = None if pos is None else pos.copy()
+    lens = np.asarray(lens).copy()
+    for b in range(k.shape[0]):
+        n = int(lens[b])
+        left = min(n, keep)
+        for j in range(k.shape[1]):
+            def place(t):
+                w = weight[b, j, t]
+                if pos is not None and (pos[b, j, t] < sink or (recent > 0 and pos[b, j, t] > last_pos[b] - recent)):
+                    return (0, 0.0, t)
+                return (2, 0.0, t) if np.isnan(w) else (1, -float(w), t)
+            kept = set(sorted(range(n), key=place)[:left])
+            holes = [t for t in range(left) if t not in kept]
+            movers = [t for t in range(left, n) if t in kept]
+            for d, s in zip(holes, movers):
+                k[b, j, d], v[b, j, d], weight[b, j, d] = k[b, j, s], v[b, j, s], weight[b, j, s]
+                if pos is not None:
+                    pos[b, j, d] = pos[b, j, s]
+            weight[b, j, left:n] = 0.0
+        lens[b] = left
+    return k, v, weight, pos, lens

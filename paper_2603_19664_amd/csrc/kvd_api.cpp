@@ -864,6 +864,265 @@ kvd_status kvd_pack_matrix(const void* w, int32_t rows, int32_t cols, void* pack
   return device_status(kvd::launch_pack(w, nullptr, packed, rows, cols, (hipStream_t)stream), "kvd_pack_matrix launch");
 }
 
+// ------------------------------------------------------------------ shared prefixes, weights, eviction
+
+namespace {
+
+// Launch geometry and workspace of a kvd_prefix_attn / kvd_weighted_attn call.
+//
+// bf16 rows go to the streaming kernel while one MFMA column block (16) holds them,
+// else to 128-row tiles; fp32 to waves of 16 rows.  A sequence whose own rows fill half
+// a block takes prefix and own keys in one pass (joint): the prefix is then shared by
+// its own rows, and neither half leaves a partial state.
+struct RowsPlan {
+  int32_t R, joint, prefix_stream, own_stream, S_prefix, C_prefix, S_own, C_own, S_w, sc_ld;
+  size_t ml, acc, lse, sc, wpart, end;  // byte offsets in the workspace
+  long long items;                      // workgroups of the largest launch
+};
+
+// Slots of a key range that `units` workgroups share: about kRowsTargetWgs workgroups, each
+// of at least `least` keys, at most `most` slots.  Grows with keys only.
+int32_t row_slots(long long units, long long keys, int32_t least, int32_t most) {
+  const long long want = std::max(1ll, (kvd::kRowsTargetWgs + units - 1) / units);
+  return (int32_t)std::max(1ll, std::min({want, (keys + least - 1) / least, (long long)most}));
+}
+int32_t slot_keys(long long keys, int32_t slots) {
+  return (int32_t)((((keys + slots - 1) / slots) + 63) / 64 * 64);
+}
+
+// False when a size passes the kernels' 32-bit indexes.
+bool rows_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T_prefix, int32_t T_own, bool weights,
+               RowsPlan* p) {
+  const bool bf = s->dtype == KVD_BF16;
+  const int32_t g = s->n_q_heads / s->n_kv_heads, RB = bf ? kvd::kRowsTile : kvd::kRowsWave;
+  *p = RowsPlan{};
+  const long long R = (long long)N * g, Rt = R * B, units = (long long)B * s->n_kv_heads;
+  const long long keys = (long long)T_prefix + T_own;
+  if (Rt * s->n_kv_heads > INT32_MAX || keys > INT32_MAX - 1024 || units > INT32_MAX) return false;
+  p->R = (int32_t)R;
+  p->joint = T_prefix > 0 && T_own > 0 && R >= RB / 2;
+  const long long nbo = (R + RB - 1) / RB, nbp = (Rt + RB - 1) / RB;
+  if (p->joint) {
+    p->S_own = row_slots(units * nbo, keys, kvd::kRowsLeastKeys, kvd::kRowsMostSlots);
+    p->C_own = slot_keys(keys, p->S_own);
+    p->items = units * nbo * p->S_own;
+  } else {
+    if (T_prefix > 0) {
+      p->prefix_stream = bf && Rt <= kvd::kRowsStream;
+      const long long u = p->prefix_stream ? s->n_kv_heads : s->n_kv_heads * nbp;
+      p->S_prefix = row_slots(u, T_prefix, p->prefix_stream ? kvd::kSaBlock : kvd::kRowsLeastKeys,
+                              p->prefix_stream ? kvd::kSaMaxSplits : kvd::kRowsMostSlots);
+      p->C_prefix = slot_keys(T_prefix, p->S_prefix);
+      p->items += u * p->S_prefix;
+    }
+    if (T_own > 0) {
+      p->own_stream = bf && R <= kvd::kRowsStream;
+      const long long u = p->own_stream ? units : units * nbo;
+      p->S_own = row_slots(u, T_own, p->own_stream ? kvd::kSaBlock : kvd::kRowsLeastKeys,
+                           p->own_stream ? kvd::kSaMaxSplits : kvd::kRowsMostSlots);
+      p->C_own = slot_keys(T_own, p->S_own);
+      p->items += u * p->S_own;
+    }
+  }
+  const size_t rows = (size_t)Rt * s->n_kv_heads, S = (size_t)p->S_prefix + p->S_own;
+  size_t at = 0;
+  const auto take = [&at](size_t bytes) {
+    const size_t o = at;
+    at += kvd::align_up(bytes, 256);
+    return o;
+  };
+  p->ml = take(8 * S * rows);
+  p->acc = take(S > 1 ? 4 * S * rows * s->head_dim : 0);
+  if (weights && T_own > 0) {
+    if (p->own_stream) {
+      p->sc_ld = (T_own + 15) / 16 * 16;
+      p->sc = take(4 * (size_t)units * R * p->sc_ld);
+      p->items = std::max(p->items, (long long)rows + units * ((T_own + 255) / 256));
+    } else {
+      // tiles of keys, their rows in S_w parts of at least 256 until the chip is full
+      const long long tiles = units * ((T_own + (bf ? 127 : 15)) / (bf ? 128 : 16));
+      p->S_w = row_slots(tiles, R, 256, 64);
+      p->lse = take(4 * rows);
+      // S_w T_own grows with T_own up to a rounding: room for the largest of either
+      p->wpart = take(4 * (size_t)units * std::max((long long)p->S_w * T_own,
+                                                   p->S_w > 1 || R > 256 ? kvd::kRowsTargetWgs * 128ll / units + T_own : 0));
+      p->items = std::max(p->items, tiles * p->S_w);
+    }
+  }
+  p->items = std::max(p->items, (long long)rows);
+  p->end = std::max<size_t>(at, 256);
+  return p->items <= INT32_MAX / 2;
+}
+
+kvd_status rows_call(const kvd_attn_shape* shape, const void* q, int32_t N, const kvd_kv_view* prefix,
+                     int32_t T_prefix, const kvd_kv_view* own, const char* own_name, const int32_t* own_len,
+                     const int32_t* n_new, int32_t B, int32_t T_own, void* out, float* weight, float decay, void* ws,
+                     size_t ws_bytes, void* stream, const char* name) {
+  KVD_TRY(check_shape(shape));
+  KVD_TRY(check_batch(B));
+  if (N < 0) return fail(KVD_ERR_SHAPE, "N=%d must be >= 0", N);
+  if (T_prefix < 0 || T_own < 0 || (int64_t)T_prefix + T_own < 1)
+    return fail(KVD_ERR_SHAPE, "T_prefix=%d T_own=%d: need both >= 0 and at least one key", T_prefix, T_own);
+  if (weight != nullptr && T_own < 1) return fail(KVD_ERR_SHAPE, "weights need own rows (T_own=%d)", T_own);
+  if (!std::isfinite(decay)) return fail(KVD_ERR_SHAPE, "decay must be finite");
+  if (B == 0 || N == 0) return KVD_OK;
+  KVD_TRY(check_ptr(q, "q"));
+  KVD_TRY(check_ptr(out, "out"));
+  if (T_prefix > 0) KVD_TRY(check_view(prefix, T_prefix, "prefix"));
+  if (T_own > 0) KVD_TRY(check_view(own, T_own, own_name));
+  if (weight != nullptr) KVD_TRY(check_ptr(weight, "weight"));
+  RowsPlan p;
+  if (!rows_plan(shape, B, N, T_prefix, T_own, weight != nullptr, &p))
+    return fail(KVD_ERR_SHAPE, "%s: B=%d N=%d T_prefix=%d T_own=%d is too large for one call", name, B, N, T_prefix,
+                T_own);
+  if (ws == nullptr) return fail(KVD_ERR_WORKSPACE, "workspace is NULL (%zu bytes needed)", p.end);
+  if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return fail(KVD_ERR_ALIGN, "workspace is not 256-byte aligned");
+  if (ws_bytes < p.end) return fail(KVD_ERR_WORKSPACE, "workspace holds %zu bytes, %zu needed", ws_bytes, p.end);
+  char* base = static_cast<char*>(ws);
+  kvd::RowsArgs a{};
+  a.q = q;
+  if (T_prefix > 0) {
+    a.pk = prefix->k;
+    a.pv = prefix->v;
+    a.p_cap = prefix->t_cap;
+    a.p_off = prefix->t_off;
+  }
+  if (T_own > 0) {
+    a.k = own->k;
+    a.v = own->v;
+    a.t_cap = own->t_cap;
+    a.t_off = own->t_off;
+  }
+  a.own_len = own_len;
+  a.n_new = n_new;
+  a.out = out;
+  a.weight = weight;
+  a.decay = decay;
+  a.ml = reinterpret_cast<float*>(base + p.ml);
+  a.acc = reinterpret_cast<float*>(base + p.acc);
+  if (weight != nullptr) {
+    if (p.own_stream) {
+      a.sc = reinterpret_cast<float*>(base + p.sc);
+    } else {
+      a.lse = reinterpret_cast<float*>(base + p.lse);
+      a.wpart = reinterpret_cast<float*>(base + p.wpart);
+    }
+  }
+  a.T_prefix = T_prefix;
+  a.T_own = T_own;
+  a.B = B;
+  a.N = N;
+  a.n_q = shape->n_q_heads;
+  a.n_kv = shape->n_kv_heads;
+  a.g = shape->n_q_heads / shape->n_kv_heads;
+  a.R = p.R;
+  a.S_prefix = p.S_prefix;
+  a.C_prefix = p.C_prefix;
+  a.S_own = p.S_own;
+  a.C_own = p.C_own;
+  a.S_w = p.S_w;
+  a.sc_ld = p.sc_ld;
+  a.joint = p.joint;
+  a.prefix_stream = p.prefix_stream;
+  a.own_stream = p.own_stream;
+  return device_status(kvd::launch_rows(a, shape->dtype == KVD_BF16, shape->head_dim, (hipStream_t)stream), name);
+}
+
+// Workspace of kvd_evict: ranks, moves, move counts.
+struct EvictPlan {
+  size_t moves, count, end;
+};
+bool evict_plan(const kvd_attn_shape* s, int32_t B, int32_t T, EvictPlan* p) {
+  const size_t units = (size_t)B * s->n_kv_heads;
+  if (units > INT32_MAX / 2) return false;
+  p->moves = kvd::align_up(4 * units * T, 256);
+  p->count = p->moves + kvd::align_up(8 * units * (T / 2 + 1), 256);  // at most min(T - keep, keep) moves
+  p->end = p->count + kvd::align_up(4 * units, 256);
+  return true;
+}
+
+}  // namespace
+
+kvd_status kvd_prefix_attn(const kvd_attn_shape* shape, const void* q, int32_t N, const kvd_kv_view* prefix,
+                           int32_t T_prefix, const kvd_kv_view* own, const int32_t* own_len, const int32_t* n_new,
+                           int32_t B, int32_t T_own, void* out, float* weight, float decay, void* ws,
+                           size_t ws_bytes, void* stream) {
+  return rows_call(shape, q, N, prefix, T_prefix, own, "own", own_len, n_new, B, T_own, out, weight, decay, ws,
+                   ws_bytes, stream, "kvd_prefix_attn");
+}
+
+kvd_status kvd_weighted_attn(const kvd_attn_shape* shape, const void* q, int32_t N, const kvd_kv_view* kv,
+                             const int32_t* kv_len, const int32_t* n_new, int32_t B, int32_t T, void* out,
+                             float* weight, float decay, void* ws, size_t ws_bytes, void* stream) {
+  KVD_TRY(check_shape(shape));
+  if (B != 0 && N != 0 && weight == nullptr) return fail(KVD_ERR_NULL, "weight is NULL");
+  return rows_call(shape, q, N, nullptr, 0, kv, "kv", kv_len, n_new, B, T, out, weight, decay, ws, ws_bytes, stream,
+                   "kvd_weighted_attn");
+}
+
+size_t kvd_prefix_workspace_bytes(const kvd_attn_shape* shape, int32_t B, int32_t N, int32_t T_prefix, int32_t T_own,
+                                  int32_t weights) {
+  RowsPlan p;
+  if (check_shape(shape) != KVD_OK || check_batch(B) != KVD_OK) return 0;
+  if (B < 1 || N < 1 || T_prefix < 0 || T_own < 0 || (int64_t)T_prefix + T_own < 1 || (weights != 0 && T_own < 1)) {
+    fail(KVD_ERR_SHAPE, "B=%d N=%d T_prefix=%d T_own=%d weights=%d", B, N, T_prefix, T_own, weights);
+    return 0;
+  }
+  return rows_plan(shape, B, N, T_prefix, T_own, weights != 0, &p) ? p.end : 0;
+}
+
+kvd_status kvd_evict(const kvd_attn_shape* shape, const kvd_kv_view* kv, int32_t* kv_len, int32_t B, int32_t T,
+                     int32_t keep, float* weight, int32_t* pos, const int32_t* last_pos, int32_t sink, int32_t recent,
+                     void* ws, size_t ws_bytes, void* stream) {
+  KVD_TRY(check_shape(shape));
+  KVD_TRY(check_batch(B));
+  if (T < 1 || keep < 1) return fail(KVD_ERR_SHAPE, "T=%d keep=%d must be >= 1", T, keep);
+  if (sink < 0 || recent < 0) return fail(KVD_ERR_SHAPE, "sink=%d recent=%d must be >= 0", sink, recent);
+  if (B == 0) return KVD_OK;
+  KVD_TRY(check_view(kv, T, "kv"));
+  KVD_TRY(check_ptr(weight, "weight"));
+  if (pos != nullptr || sink > 0 || recent > 0) KVD_TRY(check_ptr(pos, "pos"));
+  if (recent > 0 && last_pos == nullptr) return fail(KVD_ERR_NULL, "last_pos is NULL (recent=%d)", recent);
+  EvictPlan p;
+  if (!evict_plan(shape, B, T, &p)) return fail(KVD_ERR_SHAPE, "kvd_evict: B=%d is too large for one call", B);
+  if (ws == nullptr) return fail(KVD_ERR_WORKSPACE, "workspace is NULL (%zu bytes needed)", p.end);
+  if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return fail(KVD_ERR_ALIGN, "workspace is not 256-byte aligned");
+  if (ws_bytes < p.end) return fail(KVD_ERR_WORKSPACE, "workspace holds %zu bytes, %zu needed", ws_bytes, p.end);
+  if (keep >= T && kv_len == nullptr) return KVD_OK;  // no sequence holds more than it may keep
+  char* base = static_cast<char*>(ws);
+  kvd::EvictArgs a{};
+  a.k = kv->k;
+  a.v = kv->v;
+  a.t_cap = kv->t_cap;
+  a.t_off = kv->t_off;
+  a.weight = weight;
+  a.pos = pos;
+  a.last_pos = recent > 0 ? last_pos : nullptr;
+  a.len = kv_len;
+  a.keys = reinterpret_cast<uint32_t*>(base);
+  a.moves = reinterpret_cast<int2*>(base + p.moves);
+  a.n_moves = reinterpret_cast<int*>(base + p.count);
+  a.T = T;
+  a.keep = keep;
+  a.sink = sink;
+  a.recent = recent;
+  a.B = B;
+  a.n_kv = shape->n_kv_heads;
+  a.max_moves = T / 2 + 1;
+  a.row_bytes = shape->head_dim * (int)elem_size(shape);
+  return device_status(kvd::launch_evict(a, (hipStream_t)stream), "kvd_evict");
+}
+
+size_t kvd_evict_workspace_bytes(const kvd_attn_shape* shape, int32_t B, int32_t T) {
+  EvictPlan p;
+  if (check_shape(shape) != KVD_OK || check_batch(B) != KVD_OK) return 0;
+  if (B < 1 || T < 1) {
+    fail(KVD_ERR_SHAPE, "B=%d T=%d must be >= 1", B, T);
+    return 0;
+  }
+  return evict_plan(shape, B, T, &p) ? p.end : 0;
+}
+
 namespace {
 
 // Block-forward workspace: q [B][T][n_q][hd], K and V [B][n_kv][T][hd], attention

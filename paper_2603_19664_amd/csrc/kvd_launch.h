@@ -198,6 +198,51 @@ PrefillSplit prefill_split(int B, int T, int n_q);
 size_t prefill_part_floats(int hd);
 hipError_t launch_prefill_attn(const PrefillArgs& a, int hd, hipStream_t st);
 
+// Attention of several query rows over stored keys (kvd_rows.hip): N new tokens of each
+// of B sequences, R = N g rows per (sequence, KV head), over T_prefix keys that all
+// sequences share and up to T_own rows of their own.  Key ranges are slots of the
+// partial states: S_prefix of C_prefix keys of the prefix, S_own of C_own own keys; in a
+// joint call S_own ranges of C_own keys of both one after the other (S_prefix = 0).
+// With one slot the attention kernel writes out itself.  The streaming kernel (at most
+// 16 rows: prefix_stream, own_stream) cuts a range by its own length into equal slots.
+struct RowsArgs {
+  const void* q;
+  const void* pk;
+  const void* pv;
+  const void* k;
+  const void* v;
+  const int32_t* own_len;  // nullptr: T_own
+  const int32_t* n_new;    // nullptr: N
+  void* out;
+  float* weight;           // nullptr: no weights
+  float* acc;
+  float* ml;
+  float* lse;              // [n_kv][B R] max + log2(sum): weights of tiles; else nullptr
+  float* sc;               // [B][n_kv][R][sc_ld] streamed scores; else nullptr
+  float* wpart;            // [S_w][B][n_kv][T_own], S_w > 1
+  float decay;
+  int p_cap, p_off, T_prefix, t_cap, t_off, T_own;
+  int B, N, n_q, n_kv, g, R;
+  int S_prefix, C_prefix, S_own, C_own, S_w, sc_ld;
+  int joint, prefix_stream, own_stream;
+};
+hipError_t launch_rows(const RowsArgs& a, int dtype_bf16, int hd, hipStream_t st);
+
+// Eviction by weight (kvd_evict.hip) of the T rows of B n_kv caches down to keep.
+struct EvictArgs {
+  void* k;
+  void* v;
+  float* weight;
+  int32_t* pos;             // nullptr: no positions
+  const int32_t* last_pos;  // [B]; nullptr unless recent > 0
+  int32_t* len;             // [B] updated; nullptr: T
+  uint32_t* keys;           // [B n_kv][T] ranks of the rows
+  int2* moves;              // [B n_kv][max_moves] (destination, source)
+  int* n_moves;             // [B n_kv]
+  int t_cap, t_off, T, keep, sink, recent, B, n_kv, max_moves, row_bytes;
+};
+hipError_t launch_evict(const EvictArgs& a, hipStream_t st);
+
 // dst[i] = 1.0 (bf16) for i < n.
 hipError_t launch_fill_ones_bf16(void* dst, int n, hipStream_t st);
 // dst[i] = 0 (64-bit words) for i < n.

@@ -389,6 +389,14 @@ constexpr SaLds sa_lds(int hd, int G) {
   return L;
 }
 
+// Several query rows over stored keys (kvd_rows.hip).
+constexpr int kRowsTile = 128;    // rows per workgroup of the tile kernel
+constexpr int kRowsWave = 16;     // rows per wave of the fp32 kernel
+constexpr int kRowsStream = 16;   // rows the streaming kernel takes (one MFMA column block)
+constexpr int kRowsTargetWgs = 512;
+constexpr int kRowsLeastKeys = 256;  // keys per slot of the tile and fp32 kernels, at least
+constexpr int kRowsMostSlots = 64;
+
 // Value-absorbed fused attention (AbsorbArgs; head_dim 256).  Score tiles: K rows
 // x tokens per workgroup.
 enum ScoreTile { kScore512x64 = 0, kScore256x128 = 1, kScore256x64 = 2, kScoreTiles = 3 };

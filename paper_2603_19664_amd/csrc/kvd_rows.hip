@@ -1,0 +1,1104 @@
+// Attention of several query rows over stored keys that rows may share:
+// kvd_prefix_attn (a prefix that the whole batch attends, then each sequence's own
+// rows) and kvd_weighted_attn (the weight every cached key received).
+//
+//   rows_stream_kernel  bf16, at most 16 rows per key range (single tokens): one
+//                       workgroup streams 16-key blocks, scores on MFMA, P V on the
+//                       vector ALUs in fp32.
+//   rows_tile_kernel    bf16, more rows: 128 rows per workgroup, key tiles in LDS,
+//                       scores and P V on MFMA.
+//   rows_f32_kernel     fp32: 16 rows per wave, both products on MFMA 16x16x4 f32.
+//   rows_finish_kernel  merges the key ranges' softmax states into out, and adds up
+//                       the streamed scores' weights.
+//   weight_tile_kernel, weight_f32_kernel
+//                       weights of a key tile: its scores once more against every
+//                       row that sees it, weighed with the rows' final sums.
+//
+// Rows.  The rows that read KV head j are (sequence b, token i, head h of the group),
+// flat index fr = (b N + i) g + h: a prefix range takes them all, an own range the R =
+// N g of one sequence.  Every key range is one slot s of the partial states
+//   acc [S][n_kv][B R][hd], ml [S][n_kv][B R][2]  (sum 2^(s - max) V; max, sum),
+// in the log2 domain.  A state with sum 0 has no acc.
+#include <hip/hip_runtime.h>
+
+#include "kvd_device.hpp"
+#include "kvd_launch.h"
+
+namespace kvd {
+
+// v_exp_f32: one ulp, results below 2^-126 become 0 (weights that no sum feels).
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// What sequence b brings: own rows len, new tokens n (both clamped to the call's sizes).
+struct Seq {
+  int len, n;
+};
+__device__ __forceinline__ Seq seq_of(const RowsArgs& a, int b) {
+  Seq s;
+  s.len = a.own_len != nullptr ? min(max(a.own_len[b], 0), a.T_own) : a.T_own;
+  s.n = a.n_new != nullptr ? min(max(a.n_new[b], 0), a.N) : a.N;
+  return s;
+}
+// Own rows that token i of n sees: those up to its own.
+__device__ __forceinline__ int rows_seen(const Seq& s, int i) { return i < s.n ? max(s.len - s.n + i + 1, 0) : 0; }
+
+// Whether flat row fr belongs to a new token (the rows behind a sequence's n are left alone).
+__device__ __forceinline__ bool row_wanted(const RowsArgs& a, int fr) {
+  if (a.n_new == nullptr) return true;
+  const int b = fr / a.R;
+  return (fr - b * a.R) / a.g < seq_of(a, b).n;
+}
+
+__device__ __forceinline__ size_t slot_row(const RowsArgs& a, int s, int j, int fr) {
+  return ((size_t)s * a.n_kv + j) * ((size_t)a.B * a.R) + fr;
+}
+// Element offset of flat row fr of KV head j in q and out.
+__device__ __forceinline__ size_t q_off(const RowsArgs& a, int j, int fr, int hd) {
+  const unsigned tok = (unsigned)fr / (unsigned)a.g;
+  return ((size_t)tok * a.n_q + (size_t)j * a.g + (fr - (int)tok * a.g)) * hd;
+}
+
+// A range of keys [k0, k1) of KV head j: of the prefix, or of sequence b's own rows.
+struct KeyRange {
+  size_t row;  // first key's row in the K and V arrays
+  int n;
+};
+__device__ __forceinline__ KeyRange prefix_range(const RowsArgs& a, int j, int k0, int k1) {
+  return KeyRange{(size_t)j * a.p_cap + a.p_off + k0, max(k1 - k0, 0)};
+}
+__device__ __forceinline__ KeyRange own_range(const RowsArgs& a, int b, int j, int k0, int k1) {
+  return KeyRange{((size_t)b * a.n_kv + j) * a.t_cap + a.t_off + k0, max(k1 - k0, 0)};
+}
+
+// ------------------------------------------------------------------ streaming, at most 16 rows (bf16)
+
+// One workgroup of kSaWaves waves per (unit, split): units 0 .. B n_kv - 1 are the
+// own rows of (b, j) in So splits, the rest the prefix of KV head j in Sp splits.
+// stream_attn_kernel's scheme (16-key blocks to waves in turn, the next block's rows
+// loading while this one is attended, scores S^T = K q^T on MFMA 16x16x32, one row
+// per column, P V in fp32 on the vector ALUs) with rows that see different numbers of
+// keys.  CAUSAL (N > 1): a masked key's value is skipped, not multiplied by zero (it
+// may be infinite or NaN).  With a.sc the scores of own keys are kept for the weights.
+template <int HD, int G, bool CAUSAL>
+__global__ __launch_bounds__(64 * kSaWaves) __attribute__((amdgpu_waves_per_eu(2))) void rows_stream_kernel(
+    RowsArgs a) {
+  __shared__ __align__(16) char lds[sa_lds(HD, G).end];
+  constexpr int NW = kSaWaves, NT = 64 * NW;
+  constexpr int NC = HD / 32;
+  constexpr int CPK = HD / 8;
+  constexpr int KPI = 64 / CPK;
+  constexpr SaLds SL = sa_lds(HD, G);
+  const int tid = threadIdx.x, lane = tid & 63, w = wave_id();
+  const int own_items = a.own_stream ? a.B * a.n_kv * a.S_own : 0;
+  const bool own = (int)blockIdx.x < own_items;
+  const int item = own ? (int)blockIdx.x : (int)blockIdx.x - own_items;
+  const int units = own ? a.B * a.n_kv : a.n_kv;
+  const int S = own ? a.S_own : a.S_prefix;
+  const int s = item / units, u = item - s * units;
+  const int j = u % a.n_kv, b = u / a.n_kv;
+  const int slot = own ? a.S_prefix + s : s;
+  const int nr = own ? a.R : a.B * a.R;
+  const int fr0 = own ? b * a.R : 0;
+  Seq sq{0, 0};
+  if (own) sq = seq_of(a, b);
+  if (own && sq.n == 0) return;  // no row of this sequence is asked for
+  const int T = own ? sq.len : a.T_prefix;
+  const int nblk_all = (T + kSaBlock - 1) / kSaBlock;
+  const int k0 = kSaBlock * sa_first_block(s, nblk_all, S);
+  const int nk = min(T, kSaBlock * sa_first_block(s + 1, nblk_all, S)) - k0;  // keys of this split
+  const int nblk = nk > 0 ? (nk + kSaBlock - 1) / kSaBlock : 0;
+  const int nb = nblk > w ? (nblk - 1 - w) / NW + 1 : 0;
+  const KeyRange kr = own ? own_range(a, b, j, k0, k0 + nk) : prefix_range(a, j, k0, k0 + nk);
+  const uint16_t* Kp = static_cast<const uint16_t*>(own ? a.k : a.pk) + kr.row * HD;
+  const uint16_t* Vp = static_cast<const uint16_t*>(own ? a.v : a.pv) + kr.row * HD;
+  const int hq = lane & 15;  // this lane's row
+  // keys of this split that the row sees
+  int lim = 0;
+  if (hq < nr) lim = own ? min(rows_seen(sq, hq / a.g) - k0, nk) : nk;
+
+  bf16x8_t qf[NC];
+  {
+    const uint16_t* qs =
+        static_cast<const uint16_t*>(a.q) + q_off(a, j, fr0 + min(hq, nr - 1), HD) + 8 * (lane >> 4);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      u32x4_t v = *reinterpret_cast<const u32x4_t*>(qs + 32 * c);
+      if (hq >= nr) v = u32x4_t{0u, 0u, 0u, 0u};
+      qf[c] = __builtin_bit_cast(bf16x8_t, v);
+    }
+  }
+
+  auto load = [&](u32x4_t (&kv)[NC], u32x4_t (&vv)[NC], int i) {
+    const int kb = kSaBlock * (w + NW * min(i, nb - 1));
+    const uint16_t* kp = Kp + (size_t)min(kb + hq, nk - 1) * HD + 8 * (lane >> 4);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) kv[c] = *reinterpret_cast<const u32x4_t*>(kp + 32 * c);
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+      vv[c] = *reinterpret_cast<const u32x4_t*>(Vp + (size_t)min(kb + KPI * c + lane / CPK, nk - 1) * HD +
+                                                8 * (lane % CPK));
+  };
+
+  float m_run = -INFINITY, l_run = 0.0f;
+  float acc[G][8];
+#pragma unroll
+  for (int h = 0; h < G; ++h)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[h][e] = 0.0f;
+  float* Pw = reinterpret_cast<float*>(lds + SL.p) + w * (G + 1) * kSaBlock;  // [G][16] probabilities
+  float* Aw = Pw + G * kSaBlock;                                                // [G] rescale factors
+  float* sc_row = a.sc != nullptr && own && hq < nr
+                      ? a.sc + (((size_t)b * a.n_kv + j) * a.R + hq) * a.sc_ld + k0 + 4 * (lane >> 4)
+                      : nullptr;
+
+  auto attend = [&](const u32x4_t (&kv)[NC], const u32x4_t (&vv)[NC], int i) {
+    const int kb = kSaBlock * (w + NW * i);
+    f32x4_t sc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+      sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kv[c]), qf[c], sc, 0, 0, 0);
+    // sc[r]: key kb + 4 (lane / 16) + r, row hq
+    float sv[4], bm = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      sv[r] = kb + 4 * (lane >> 4) + r < lim ? sc[r] * ScoreScale<HD>::v : -INFINITY;
+      bm = fmaxf(bm, sv[r]);
+    }
+    if (sc_row != nullptr && i < nb) *reinterpret_cast<float4*>(sc_row + kb) = make_float4(sv[0], sv[1], sv[2], sv[3]);
+    bm = fmaxf(bm, __shfl_xor(bm, 16, 64));
+    bm = fmaxf(bm, __shfl_xor(bm, 32, 64));
+    const float m_new = fmaxf(m_run, bm);
+    const float m_use = m_new == -INFINITY ? 0.0f : m_new;  // no key seen yet: weights 0
+    const float alpha = exp2_hw(m_run - m_use);
+    float p[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) p[r] = exp2_hw(sv[r] - m_use);
+    l_run = fmaf(l_run, alpha, (p[0] + p[1]) + (p[2] + p[3]));
+    m_run = m_new;
+    if (hq < G) *reinterpret_cast<float4*>(Pw + hq * kSaBlock + 4 * (lane >> 4)) = make_float4(p[0], p[1], p[2], p[3]);
+    if (lane < G) Aw[lane] = alpha;
+    __builtin_amdgcn_wave_barrier();  // the wave's LDS writes are ordered before its reads below
+#pragma unroll
+    for (int h = 0; h < G; ++h) {
+      const float al = Aw[h];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[h][e] *= al;
+    }
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int kk = KPI * c + lane / CPK;
+      const bool in = kb + kk < nk;  // past the range: 0, so that a weight of 0 gives 0
+      const uint32_t vw[4] = {in ? vv[c].x : 0u, in ? vv[c].y : 0u, in ? vv[c].z : 0u, in ? vv[c].w : 0u};
+      float v8[8];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v8[2 * e] = bf_lo(vw[e]);
+        v8[2 * e + 1] = bf_hi(vw[e]);
+      }
+#pragma unroll
+      for (int h = 0; h < G; ++h) {
+        const float pr = Pw[h * kSaBlock + kk];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float x = fmaf(pr, v8[e], acc[h][e]);
+          acc[h][e] = !CAUSAL || pr != 0.0f ? x : acc[h][e];
+        }
+      }
+    }
+    __builtin_amdgcn_wave_barrier();  // reads of this block's slot before the next block's writes
+  };
+
+  // the pipeline of stream_attn_kernel: blocks in pairs, straight-line, each refill
+  // kept behind the last use of the registers that it overwrites
+  if (nb > 0) {
+    u32x4_t kr0[NC], vr0[NC], kr1[NC], vr1[NC];
+    load(kr0, vr0, 0);
+    for (int i = 0; i < nb; i += 2) {
+      __builtin_amdgcn_sched_barrier(0);
+      load(kr1, vr1, i + 1);
+      attend(kr0, vr0, i);
+      __builtin_amdgcn_sched_barrier(0);
+      load(kr0, vr0, i + 2);
+      attend(kr1, vr1, i + 1);
+    }
+  }
+
+  l_run += __shfl_xor(l_run, 16, 64);
+  l_run += __shfl_xor(l_run, 32, 64);
+#pragma unroll
+  for (int o = CPK; o < 64; o <<= 1)
+#pragma unroll
+    for (int h = 0; h < G; ++h)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[h][e] += __shfl_xor(acc[h][e], o, 64);
+
+  float* ms = reinterpret_cast<float*>(lds + SL.ml);   // [NW][G][2]
+  float* as = reinterpret_cast<float*>(lds + SL.acc);  // [NW][G][HD]
+  if (lane < G) {
+    ms[(w * G + lane) * 2] = m_run;
+    ms[(w * G + lane) * 2 + 1] = l_run;
+  }
+  if (lane < CPK) {
+#pragma unroll
+    for (int h = 0; h < G; ++h) {
+      float* dst = as + ((size_t)w * G + h) * HD + 8 * lane;
+      *reinterpret_cast<float4*>(dst) = make_float4(acc[h][0], acc[h][1], acc[h][2], acc[h][3]);
+      *reinterpret_cast<float4*>(dst + 4) = make_float4(acc[h][4], acc[h][5], acc[h][6], acc[h][7]);
+    }
+  }
+  __syncthreads();
+
+  // merge of the waves in wave order: the slot's state, or with one slot the output
+  const bool direct = a.S_prefix + a.S_own == 1;
+  for (int i = tid; i < nr * HD; i += NT) {
+    const int h = i / HD, c = i - h * HD;
+    float M = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < NW; ++v) M = fmaxf(M, ms[(v * G + h) * 2]);
+    const float Mu = M == -INFINITY ? 0.0f : M;
+    float o = 0.0f, L = 0.0f;
+#pragma unroll
+    for (int v = 0; v < NW; ++v) {
+      const float wt = exp2_hw(ms[(v * G + h) * 2] - Mu);
+      o = fmaf(wt, as[((size_t)v * G + h) * HD + c], o);
+      L = fmaf(wt, ms[(v * G + h) * 2 + 1], L);
+    }
+    const size_t row = slot_row(a, slot, j, fr0 + h);
+    if (direct) {
+      if (row_wanted(a, fr0 + h))
+        static_cast<uint16_t*>(a.out)[q_off(a, j, fr0 + h, HD) + c] = from_f<uint16_t>(L != 0.0f ? o / L : 0.0f);
+    } else {
+      a.acc[row * HD + c] = o;
+    }
+    if (c == 0) {
+      a.ml[row * 2] = Mu;
+      a.ml[row * 2 + 1] = L;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ 128-row tiles (bf16)
+
+// Keys per LDS tile: 32 KiB of K and V.
+constexpr int rows_kt(int hd) { return hd == 256 ? 32 : 64; }
+
+// Direct global-to-LDS copy of KT key rows of K and V (rows past n - 1 repeat row n -
+// 1).  Row r's 16-byte chunk c lies at chunk c ^ (r % CPR) of its LDS row for K, at c ^
+// 2 (r % 4) for V: the score operand reads the same chunk of 32 rows, the transposing
+// V reads 64 bytes of 4 rows; both then touch every bank evenly.
+template <int HD>
+__device__ __forceinline__ void load_tile_lds(const uint16_t* K, const uint16_t* V, int k0, int n, uint16_t* ks,
+                                              uint16_t* vs) {
+  constexpr int KT = rows_kt(HD), CPR = HD / 8, CH = KT * CPR / 256;
+  const int tid = threadIdx.x, w = wave_id();
+#pragma unroll
+  for (int i = 0; i < CH; ++i) {
+    const int c = tid + 256 * i, row = c / CPR, ch = c - row * CPR;
+    const size_t key = (size_t)min(k0 + row, n - 1) * HD;
+    const int dst = 8 * (64 * w + 256 * i);  // wave-uniform; lane l's 16 bytes follow at 16 l
+    __builtin_amdgcn_global_load_lds(
+        (const __attribute__((address_space(1))) void*)(K + key + 8 * (ch ^ (row & (CPR - 1)))),
+        (__attribute__((address_space(3))) void*)(ks + dst), 16, 0, 0);
+    __builtin_amdgcn_global_load_lds(
+        (const __attribute__((address_space(1))) void*)(V + key + 8 * (ch ^ (2 * (row & 3)))),
+        (__attribute__((address_space(3))) void*)(vs + dst), 16, 0, 0);
+  }
+}
+
+typedef short i16x4_t __attribute__((ext_vector_type(4)));
+
+// V^T operand of a 32-row block db of O^T for the 16 keys at k0 of the LDS tile: two
+// transposing reads (in a group of 16 lanes, lane s names 4 columns of row s / 4 of a
+// 4-key group, and lane i receives column i of the 4 keys).  Lane half hl gets keys
+// k0 + 4 hl + {0..3, 8..11}, the ones whose scores it holds.
+template <int HD>
+__device__ __forceinline__ bf16x8_t v_operand(const uint16_t* vs, int k0, int db, int lane) {
+  const int hl = lane >> 5;
+  const int row = k0 + 4 * hl + ((lane & 15) >> 2);
+  const int ch = (4 * db + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ (2 * (row & 3));
+  const uint16_t* p = vs + row * HD + 8 * ch + 4 * (lane & 1);
+  const i16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4_t*)p);
+  const i16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4_t*)(p + 8 * HD));
+  return __builtin_bit_cast(bf16x8_t, make_uint4(__builtin_bit_cast(uint2, lo).x, __builtin_bit_cast(uint2, lo).y,
+                                                 __builtin_bit_cast(uint2, hi).x, __builtin_bit_cast(uint2, hi).y));
+}
+
+// Two bf16 in a word: nonzero where one is infinite or NaN (the exponent's carry).
+__device__ __forceinline__ uint32_t nonfinite2(uint32_t x) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+// Non-finite halves replaced by 0, and by a code that a sum over up to 127 keys keeps
+// apart: +inf 1, -inf 128, NaN 16384.
+__device__ __forceinline__ float code_of(float v) {
+  return v == INFINITY ? 1.0f : v == -INFINITY ? 128.0f : 16384.0f;
+}
+__device__ __forceinline__ float poison_of(float codes) {
+  if (codes == 0.0f) return 0.0f;
+  const int c = (int)codes;
+  const bool pos = (c & 127) != 0, neg = ((c >> 7) & 127) != 0;
+  return c >= 16384 || (pos && neg) ? __uint_as_float(0x7fc00000u) : pos ? INFINITY : -INFINITY;
+}
+__device__ __forceinline__ void split_nonfinite(bf16x8_t v, bf16x8_t& fin, bf16x8_t& code) {
+  const uint4 x = __builtin_bit_cast(uint4, v);
+  const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
+  uint32_t f[4], c[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t nf = nonfinite2(xs[i]);
+    const float lo = bf_lo(xs[i]), hi = bf_hi(xs[i]);
+    f[i] = xs[i] & ((nf & 0x8000u ? 0u : 0xffffu) | (nf & 0x80000000u ? 0u : 0xffff0000u));
+    c[i] = pack_bf16x2(nf & 0x8000u ? code_of(lo) : 0.0f, nf & 0x80000000u ? code_of(hi) : 0.0f);
+  }
+  fin = __builtin_bit_cast(bf16x8_t, make_uint4(f[0], f[1], f[2], f[3]));
+  code = __builtin_bit_cast(bf16x8_t, make_uint4(c[0], c[1], c[2], c[3]));
+}
+
+// One workgroup of 4 waves per (128-row block, key range), 32 rows per wave, through
+// the range's key tiles: first its prefix keys, then its own ones (one of them empty
+// unless the call is joint).  Tile t + 1 is copied into the other LDS buffer while tile
+// t is computed.  S^T = K Q^T (A: 32 keys from LDS, B: the wave's rows, in registers):
+// a lane holds scores of one row, so its running maximum and sum need one exchange with
+// lane ^ 32.  The maximum moves only by steps of more than 2^8, so that O is rescaled
+// in few tiles.  O^T += V^T P^T with P^T straight from the score registers, rounded to
+// bf16 (each weight off by at most 2^-9 of itself, as much as the output's own
+// rounding; the sum is taken before the rounding).
+template <int HD>
+__global__ __launch_bounds__(256, 2) void rows_tile_kernel(RowsArgs a) {
+  constexpr int KT = rows_kt(HD), KH = KT / 32, KS = HD / 16, DB = HD / 32, CPR = HD / 8;
+  __shared__ __align__(16) uint16_t lds[2][2][KT * HD];
+  const int tid = threadIdx.x, lane = tid & 63, w = wave_id(), hl = lane >> 5;
+  // the item: own (or joint) row blocks first, then the prefix's
+  const int nbo = (a.R + kRowsTile - 1) / kRowsTile;
+  const int own_items = a.own_stream ? 0 : a.B * a.n_kv * nbo * a.S_own;
+  const bool own = (int)blockIdx.x < own_items;
+  int blk, s, j, b;
+  if (own) {
+    const int units = a.B * a.n_kv, x = (int)blockIdx.x / units, u = (int)blockIdx.x - x * units;
+    j = u % a.n_kv;
+    b = u / a.n_kv;
+    s = x % a.S_own;
+    blk = nbo - 1 - x / a.S_own;  // the last rows see the most keys: first
+  } else {
+    const int item = (int)blockIdx.x - own_items, units = a.n_kv * a.S_prefix;
+    blk = item / units;
+    const int u = item - blk * units;
+    j = u % a.n_kv;
+    s = u / a.n_kv;
+    b = 0;
+  }
+  const int nr = own ? a.R : a.B * a.R;
+  const int fr0 = own ? b * a.R : 0;
+  Seq sq{0, 0};
+  if (own) sq = seq_of(a, b);
+  const int slot = own ? a.S_prefix + s : s;
+  const int r_blk = blk * kRowsTile;
+  if (own && r_blk >= sq.n * a.g) return;  // no row of this block is asked for
+  // key range of the item
+  int p0 = 0, p1 = 0, o0 = 0, o1 = 0;
+  if (!own) {
+    p0 = s * a.C_prefix;
+    p1 = min(p0 + a.C_prefix, a.T_prefix);
+  } else {
+    const int last = min(r_blk + kRowsTile, sq.n * a.g) - 1;
+    const int seen = rows_seen(sq, last / a.g);  // the block's longest row
+    const int base = a.joint ? a.T_prefix : 0;
+    const long long k0 = (long long)s * a.C_own, k1 = k0 + a.C_own;
+    p0 = (int)min(k0, (long long)base);
+    p1 = (int)min(k1, (long long)base);
+    o0 = (int)max(k0 - base, 0ll);
+    o1 = (int)min(max(k1 - base, 0ll), (long long)seen);
+  }
+  const KeyRange kp = prefix_range(a, j, p0, p1), ko = own_range(a, b, j, o0, o1);
+  const int np = (kp.n + KT - 1) / KT, nt = np + (ko.n + KT - 1) / KT;
+  const uint16_t* Kp = static_cast<const uint16_t*>(a.pk) + kp.row * HD;
+  const uint16_t* Vp = static_cast<const uint16_t*>(a.pv) + kp.row * HD;
+  const uint16_t* Ko = static_cast<const uint16_t*>(a.k) + ko.row * HD;
+  const uint16_t* Vo = static_cast<const uint16_t*>(a.v) + ko.row * HD;
+
+  // this lane's row
+  const int rl = r_blk + 32 * w + (lane & 31);
+  const bool wave_on = r_blk + 32 * w < (own ? sq.n * a.g : nr);
+  const int fr = fr0 + min(rl, nr - 1);
+  // keys of the item's own range that the row sees; every prefix key is seen
+  const int lim = own && rl < nr ? min(rows_seen(sq, rl / a.g) - o0, ko.n) : 0;
+  // own keys that every row of the wave's block sees
+  const int all = own ? min(rows_seen(sq, min(r_blk + 32 * w, nr - 1) / a.g) - o0, ko.n) : 0;
+  bf16x8_t qf[KS];
+  {
+    const uint16_t* qs = static_cast<const uint16_t*>(a.q) + q_off(a, j, fr, HD) + 8 * hl;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8_t*>(qs + 16 * ks);
+  }
+  f32x16_t o[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[db][i] = 0.0f;
+  float m_run = -INFINITY, l_run = 0.0f;  // in units of the scaled score
+
+  auto load = [&](int t) {
+    uint16_t* ks = lds[t & 1][0];
+    uint16_t* vs = lds[t & 1][1];
+    if (t < np)
+      load_tile_lds<HD>(Kp, Vp, t * KT, kp.n, ks, vs);
+    else
+      load_tile_lds<HD>(Ko, Vo, (t - np) * KT, ko.n, ks, vs);
+  };
+  if (nt > 0) load(0);
+  for (int t = 0; t < nt; ++t) {
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's share of tile t is in LDS
+    __syncthreads();                     // every wave's share, and tile t - 1 is no longer read
+    if (t + 1 < nt) load(t + 1);
+    if (!wave_on) continue;
+    const uint16_t* ks = lds[t & 1][0];
+    const uint16_t* vs = lds[t & 1][1];
+    const bool is_own = t >= np;
+    const int k0 = (is_own ? t - np : t) * KT;
+    const int row_lim = is_own ? lim : kp.n;
+    const bool masked = k0 + KT > (is_own ? all : kp.n);
+
+    f32x16_t st[KH];
+#pragma unroll
+    for (int kh = 0; kh < KH; ++kh)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) st[kh][i] = 0.0f;
+#pragma unroll
+    for (int kk = 0; kk < KS; ++kk) {
+#pragma unroll
+      for (int kh = 0; kh < KH; ++kh) {
+        const int row = 32 * kh + (lane & 31);
+        const bf16x8_t kf =
+            *reinterpret_cast<const bf16x8_t*>(ks + row * HD + 8 * ((2 * kk + hl) ^ (row & (CPR - 1))));
+        st[kh] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[kk], st[kh], 0, 0, 0);
+      }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int kh = 0; kh < KH; ++kh)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        if (masked) {
+          const int key = k0 + 32 * kh + 8 * (r >> 2) + 4 * hl + (r & 3);
+          st[kh][r] = key < row_lim ? st[kh][r] : -INFINITY;
+        }
+        mx = fmaxf(mx, st[kh][r]);
+      }
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * ScoreScale<HD>::v;
+    const bool grow = mx > m_run + 8.0f;
+    if (__any(grow)) {
+      const float m_new = grow ? mx : m_run;
+      const float alpha = exp2_hw(grow ? m_run - m_new : 0.0f);
+      m_run = m_new;
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
+    }
+    const float m_use = m_run == -INFINITY ? 0.0f : m_run;
+    bf16x8_t pf[2 * KH];
+    float sum = 0.0f;
+#pragma unroll
+    for (int tt = 0; tt < 2 * KH; ++tt) {
+      uint32_t pw[4];
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        const int r = 8 * (tt & 1) + e;
+        const float pa = exp2_hw(fmaf(st[tt >> 1][r], ScoreScale<HD>::v, -m_use));
+        const float pb = exp2_hw(fmaf(st[tt >> 1][r + 1], ScoreScale<HD>::v, -m_use));
+        sum += pa + pb;
+        pw[e >> 1] = pack_bf16x2(pa, pb);
+      }
+      pf[tt] = __builtin_bit_cast(bf16x8_t, make_uint4(pw[0], pw[1], pw[2], pw[3]));
+    }
+    l_run += sum;  // this lane's keys; lane ^ 32 holds the others
+    bool odd = false;  // an infinite or NaN value where some row is masked
+    if (masked) {
+      uint32_t nf = 0;
+#pragma unroll
+      for (int tt = 0; tt < 2 * KH; ++tt)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          const uint4 x = __builtin_bit_cast(uint4, v_operand<HD>(vs, 16 * tt, db, lane));
+          nf |= nonfinite2(x.x) | nonfinite2(x.y) | nonfinite2(x.z) | nonfinite2(x.w);
+        }
+      odd = __any(nf != 0);
+    }
+    if (!odd) {
+#pragma unroll
+      for (int tt = 0; tt < 2 * KH; ++tt)
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand<HD>(vs, 16 * tt, db, lane), pf[tt], o[db], 0, 0, 0);
+    } else {
+      // the finite part, and which rows see which infinities: 0 * inf never arises
+      bf16x8_t seen[2 * KH];
+#pragma unroll
+      for (int tt = 0; tt < 2 * KH; ++tt) {
+        uint32_t sw[4];
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+          const int key = k0 + 32 * (tt >> 1) + 16 * (tt & 1) + 8 * (e >> 2) + 4 * hl + (e & 3);
+          sw[e >> 1] = (key < row_lim ? 0x3f80u : 0u) | (key + 1 < row_lim ? 0x3f800000u : 0u);
+        }
+        seen[tt] = __builtin_bit_cast(bf16x8_t, make_uint4(sw[0], sw[1], sw[2], sw[3]));
+      }
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        f32x16_t codes;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) codes[i] = 0.0f;
+#pragma unroll
+        for (int tt = 0; tt < 2 * KH; ++tt) {
+          bf16x8_t fin, code;
+          split_nonfinite(v_operand<HD>(vs, 16 * tt, db, lane), fin, code);
+          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fin, pf[tt], o[db], 0, 0, 0);
+          codes = __builtin_amdgcn_mfma_f32_32x32x16_bf16(code, seen[tt], codes, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[db][i] += poison_of(codes[i]);
+      }
+    }
+  }
+
+  l_run += __shfl_xor(l_run, 32, 64);
+  if (rl >= nr || !row_wanted(a, fr)) return;
+  const float m_out = m_run == -INFINITY ? 0.0f : m_run;
+  const bool direct = a.S_prefix + a.S_own == 1;
+  const size_t row = slot_row(a, slot, j, fr);
+  if (hl == 0) {
+    a.ml[2 * row] = m_out;
+    a.ml[2 * row + 1] = l_run;
+  }
+  if (direct) {
+    const float inv = l_run != 0.0f ? 1.0f / l_run : 0.0f;
+    uint16_t* dst = static_cast<uint16_t*>(a.out) + q_off(a, j, fr, HD);
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4) {
+        uint2 v = make_uint2(0u, 0u);
+        if (l_run != 0.0f) {
+          v.x = pack_bf16x2(o[db][4 * q4 + 0] * inv, o[db][4 * q4 + 1] * inv);
+          v.y = pack_bf16x2(o[db][4 * q4 + 2] * inv, o[db][4 * q4 + 3] * inv);
+        }
+        *reinterpret_cast<uint2*>(dst + 32 * db + 8 * q4 + 4 * hl) = v;
+      }
+  } else if (l_run != 0.0f) {
+    float* dst = a.acc + row * HD;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int q4 = 0; q4 < 4; ++q4)
+        *reinterpret_cast<float4*>(dst + 32 * db + 8 * q4 + 4 * hl) =
+            make_float4(o[db][4 * q4 + 0], o[db][4 * q4 + 1], o[db][4 * q4 + 2], o[db][4 * q4 + 3]);
+  }
+}
+
+// ------------------------------------------------------------------ fp32
+
+// One wave per (16-row block, key range), 16 keys at a step, on v_mfma_f32_16x16x4_f32.
+// Scores S^T = K Q^T: lane (row lane % 16, group lg = lane / 16) holds elements 16 c + 4
+// lg .. + 3 of a key (A) and of its query row (B); MFMA e of chunk c takes element e.
+// P V: O^T = V^T P^T, step t takes the keys 4 lg + t, whose weights the lanes hold; a
+// lane's 16 bytes of V row 4 lg + t (dims 64 u + 4 (lane % 16) ..) are the A operands of
+// four MFMAs, MFMA e giving dims 64 u + 4 i + e.  No LDS.  Masked keys: score -inf;
+// a non-finite value that some row does not see is split off (split_nonfinite's codes).
+template <int HD>
+__global__ __launch_bounds__(64) void rows_f32_kernel(RowsArgs a) {
+  constexpr int KC = HD / 16, VU = HD / 64;
+  const int lane = threadIdx.x, rq = lane & 15, lg = lane >> 4;
+  const int nbo = (a.R + kRowsWave - 1) / kRowsWave;
+  const int own_items = a.B * a.n_kv * nbo * a.S_own;
+  const bool own = (int)blockIdx.x < own_items;
+  int blk, s, j, b;
+  if (own) {
+    const int units = a.B * a.n_kv, x = (int)blockIdx.x / units, u = (int)blockIdx.x - x * units;
+    j = u % a.n_kv;
+    b = u / a.n_kv;
+    s = x % a.S_own;
+    blk = nbo - 1 - x / a.S_own;
+  } else {
+    const int item = (int)blockIdx.x - own_items, units = a.n_kv * a.S_prefix;
+    blk = item / units;
+    const int u = item - blk * units;
+    j = u % a.n_kv;
+    s = u / a.n_kv;
+    b = 0;
+  }
+  const int nr = own ? a.R : a.B * a.R;
+  const int fr0 = own ? b * a.R : 0;
+  Seq sq{0, 0};
+  if (own) sq = seq_of(a, b);
+  const int slot = own ? a.S_prefix + s : s;
+  const int r_blk = blk * kRowsWave;
+  if (own && r_blk >= sq.n * a.g) return;
+  int p0 = 0, p1 = 0, o0 = 0, o1 = 0;
+  if (!own) {
+    p0 = s * a.C_prefix;
+    p1 = min(p0 + a.C_prefix, a.T_prefix);
+  } else {
+    const int last = min(r_blk + kRowsWave, sq.n * a.g) - 1;
+    const int seen = rows_seen(sq, last / a.g);
+    const int base = a.joint ? a.T_prefix : 0;
+    const long long k0 = (long long)s * a.C_own, k1 = k0 + a.C_own;
+    p0 = (int)min(k0, (long long)base);
+    p1 = (int)min(k1, (long long)base);
+    o0 = (int)max(k0 - base, 0ll);
+    o1 = (int)min(max(k1 - base, 0ll), (long long)seen);
+  }
+  const KeyRange kp = prefix_range(a, j, p0, p1), ko = own_range(a, b, j, o0, o1);
+  const int np = (kp.n + 15) / 16, nt = np + (ko.n + 15) / 16;
+  const int rl = r_blk + rq;
+  const int fr = fr0 + min(rl, nr - 1);
+  const int lim = own && rl < nr ? min(rows_seen(sq, rl / a.g) - o0, ko.n) : 0;
+
+  f32x4_t q[KC];
+  {
+    const float* qs = static_cast<const float*>(a.q) + q_off(a, j, fr, HD) + 4 * lg;
+#pragma unroll
+    for (int c = 0; c < KC; ++c) q[c] = *reinterpret_cast<const f32x4_t*>(qs + 16 * c);
+  }
+  f32x4_t o[VU][4];
+#pragma unroll
+  for (int u = 0; u < VU; ++u)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[u][e] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+  float m_run = -INFINITY, l_run = 0.0f;
+
+  for (int t = 0; t < nt; ++t) {
+    const bool is_own = t >= np;
+    const KeyRange& kr = is_own ? ko : kp;
+    const float* K = static_cast<const float*>(is_own ? a.k : a.pk) + kr.row * HD;
+    const float* V = static_cast<const float*>(is_own ? a.v : a.pv) + kr.row * HD;
+    const int k0 = 16 * (is_own ? t - np : t);
+    const int row_lim = is_own ? lim : kp.n;
+    f32x4_t kf[KC], vf[4][VU];
+    const float* ks = K + (size_t)min(k0 + rq, kr.n - 1) * HD + 4 * lg;
+#pragma unroll
+    for (int c = 0; c < KC; ++c) kf[c] = *reinterpret_cast<const f32x4_t*>(ks + 16 * c);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float* vs = V + (size_t)min(k0 + 4 * lg + i, kr.n - 1) * HD + 4 * rq;
+#pragma unroll
+      for (int u = 0; u < VU; ++u) vf[i][u] = *reinterpret_cast<const f32x4_t*>(vs + 64 * u);
+    }
+    f32x4_t s0 = {0.0f, 0.0f, 0.0f, 0.0f}, s1 = s0;
+#pragma unroll
+    for (int c = 0; c < KC; ++c)
+#pragma unroll
+      for (int e = 0; e < 4; e += 2) {
+        s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[c][e], q[c][e], s0, 0, 0, 0);
+        s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[c][e + 1], q[c][e + 1], s1, 0, 0, 0);
+      }
+    // key k0 + 4 lg + r, row rq
+    float sv[4], mx = -INFINITY;
+    bool unseen = false;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const bool in = k0 + 4 * lg + r < row_lim;
+      unseen |= !in;
+      sv[r] = in ? (s0[r] + s1[r]) * ScoreScale<HD>::v : -INFINITY;
+      mx = fmaxf(mx, sv[r]);
+    }
+    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    const float m_new = fmaxf(m_run, mx);
+    const float m_use = m_new == -INFINITY ? 0.0f : m_new;
+    const float alpha = exp2_hw(m_run - m_use);
+    m_run = m_new;
+    float p[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) p[r] = exp2_hw(sv[r] - m_use);
+    l_run = fmaf(l_run, alpha, (p[0] + p[1]) + (p[2] + p[3]));
+#pragma unroll
+    for (int u = 0; u < VU; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[u][e] *= alpha;
+    bool odd = false;
+    if (__any(unseen)) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int u = 0; u < VU; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) odd |= !(fabsf(vf[i][u][e]) < INFINITY);
+      odd = __any(odd);
+    }
+    if (!odd) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int u = 0; u < VU; ++u)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            o[u][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[i][u][e], p[i], o[u][e], 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int u = 0; u < VU; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          f32x4_t codes = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float v = vf[i][u][e];
+            const bool fin = fabsf(v) < INFINITY;
+            o[u][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(fin ? v : 0.0f, p[i], o[u][e], 0, 0, 0);
+            codes = __builtin_amdgcn_mfma_f32_16x16x4f32(fin ? 0.0f : code_of(v), k0 + 4 * lg + i < row_lim ? 1.0f : 0.0f,
+                                                         codes, 0, 0, 0);
+          }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[u][e][r] += poison_of(codes[r]);
+        }
+    }
+  }
+  l_run += __shfl_xor(l_run, 16, 64);
+  l_run += __shfl_xor(l_run, 32, 64);
+  if (rl >= nr || !row_wanted(a, fr)) return;
+  const bool direct = a.S_prefix + a.S_own == 1;
+  const size_t row = slot_row(a, slot, j, fr);
+  if (lg == 0) {
+    a.ml[2 * row] = m_run == -INFINITY ? 0.0f : m_run;
+    a.ml[2 * row + 1] = l_run;
+  }
+  // o[u][e][r]: dim 64 u + 16 lg + 4 r + e
+  if (direct || l_run != 0.0f) {
+    float* dst = direct ? static_cast<float*>(a.out) + q_off(a, j, fr, HD) : a.acc + row * HD;
+#pragma unroll
+    for (int u = 0; u < VU; ++u)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float4 v = make_float4(o[u][0][r], o[u][1][r], o[u][2][r], o[u][3][r]);
+        if (direct)
+          v = l_run != 0.0f ? make_float4(v.x / l_run, v.y / l_run, v.z / l_run, v.w / l_run)
+                            : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        *reinterpret_cast<float4*>(dst + 64 * u + 16 * lg + 4 * r) = v;
+      }
+  }
+}
+
+// ------------------------------------------------------------------ merge and streamed weights
+
+// Merged (max, sum) of a row's S states, by one wave: lane s takes states s, s + 64, ...
+__device__ __forceinline__ void merge_ml(const RowsArgs& a, int S, int j, int fr, int lane, float& M, float& L) {
+  M = -INFINITY;
+  for (int s = lane; s < S; s += 64) {
+    const float2 x = *reinterpret_cast<const float2*>(a.ml + 2 * slot_row(a, s, j, fr));
+    if (x.y != 0.0f) M = fmaxf(M, x.x);
+  }
+  M = wave_max(M);
+  L = 0.0f;
+  for (int s = lane; s < S; s += 64) {
+    const float2 x = *reinterpret_cast<const float2*>(a.ml + 2 * slot_row(a, s, j, fr));
+    if (x.y != 0.0f) L = fmaf(x.y, exp2_hw(x.x - M), L);
+  }
+  L = wave_sum(L);
+}
+
+constexpr int kFinishRows = 4;     // merged rows per workgroup (one per wave)
+constexpr int kFinishKeys = 256;   // keys per workgroup of the streamed weights
+
+// Workgroups 0 .. merge_wgs - 1 merge 4 rows each (out, and their max + log2(sum) where
+// the weights of tiles need them); the rest add up the weights of 256 own keys of one
+// (b, j) from the kept scores: weight = decay weight + sum_rows 2^(score - max) / sum.
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void rows_finish_kernel(RowsArgs a, int merge_wgs) {
+  constexpr int E = HD / 64;
+  const int lane = threadIdx.x & 63, w = wave_id();
+  const int S = a.S_prefix + a.S_own;
+  if ((int)blockIdx.x < merge_wgs) {
+    const long long idx = (long long)blockIdx.x * kFinishRows + w;
+    const int Rt = a.B * a.R;
+    if (idx >= (long long)Rt * a.n_kv) return;
+    const int j = (int)(idx / Rt), fr = (int)(idx - (long long)j * Rt);
+    const int tok = fr / a.g, b = tok / a.N;
+    if (tok - b * a.N >= seq_of(a, b).n) return;
+    float M, L;
+    merge_ml(a, S, j, fr, lane, M, L);
+    if (a.lse != nullptr && lane == 0) a.lse[(size_t)j * Rt + fr] = L != 0.0f ? M + __builtin_amdgcn_logf(L) : INFINITY;
+    if (S == 1) return;  // written by the attention kernel itself
+    float x[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = 0.0f;
+    for (int s = 0; s < S; ++s) {
+      const size_t row = slot_row(a, s, j, fr);
+      const float2 ml = *reinterpret_cast<const float2*>(a.ml + 2 * row);
+      if (ml.y == 0.0f) continue;
+      const float wt = exp2_hw(ml.x - M);
+      float y[E];
+      load_e<E>(a.acc + row * HD + E * lane, y);
+#pragma unroll
+      for (int e = 0; e < E; ++e) x[e] = fmaf(y[e], wt, x[e]);
+    }
+    T* dst = static_cast<T*>(a.out) + q_off(a, j, fr, HD) + E * lane;
+#pragma unroll
+    for (int e = 0; e < E; ++e) dst[e] = from_f<T>(L != 0.0f ? x[e] / L : 0.0f);
+    return;
+  }
+  __shared__ float lse[kMaxGroup];
+  const int item = (int)blockIdx.x - merge_wgs, units = a.B * a.n_kv;
+  const int c = item / units, u = item - c * units;
+  const int j = u % a.n_kv, b = u / a.n_kv;
+  const Seq sq = seq_of(a, b);
+  for (int r = w; r < sq.n * a.g; r += 4) {
+    float M, L;
+    merge_ml(a, S, j, b * a.R + r, lane, M, L);
+    if (lane == 0) lse[r] = L != 0.0f ? M + __builtin_amdgcn_logf(L) : INFINITY;
+  }
+  __syncthreads();
+  const int t = c * kFinishKeys + threadIdx.x;
+  if (t >= sq.len) return;
+  const float* sc = a.sc + ((size_t)b * a.n_kv + j) * a.R * a.sc_ld + t;
+  float sum = 0.0f;
+  for (int r = 0; r < sq.n * a.g; ++r) {
+    const float x = sc[(size_t)r * a.sc_ld];
+    sum += x == -INFINITY ? 0.0f : exp2_hw(x - lse[r]);
+  }
+  float* wp = a.weight + ((size_t)b * a.n_kv + j) * a.t_cap + a.t_off + t;
+  *wp = a.decay != 0.0f ? fmaf(a.decay, *wp, sum) : sum;
+}
+
+// ------------------------------------------------------------------ weights of a key tile
+
+// Rows [r0, r1) of part c of C of the rows that see key k0 of sequence sq.
+struct RowSpan {
+  int r0, r1;
+};
+__device__ __forceinline__ RowSpan rows_of_part(const Seq& sq, int g, int k0, int c, int C) {
+  const int i0 = min(max(k0 - (sq.len - sq.n), 0), sq.n);  // the first token that sees key k0
+  const long long first = (long long)i0 * g, n = (long long)(sq.n - i0) * g;
+  return RowSpan{(int)(first + n * c / C), (int)(first + n * (c + 1) / C)};
+}
+__device__ __forceinline__ void put_weight(const RowsArgs& a, int c, int b, int j, int t, float sum) {
+  const size_t bj = (size_t)b * a.n_kv + j;
+  if (a.S_w == 1) {
+    float* wp = a.weight + bj * a.t_cap + a.t_off + t;
+    *wp = a.decay != 0.0f ? fmaf(a.decay, *wp, sum) : sum;
+  } else {
+    a.wpart[((size_t)c * a.B * a.n_kv + bj) * a.T_own + t] = sum;
+  }
+}
+
+constexpr int kWtKeys = 128, kWtRows = 64;
+
+// bf16: one workgroup of 4 waves per (128 keys of (b, j), part of the rows).  A wave
+// keeps its 32 keys as MFMA A operands; the rows pass through LDS 64 at a time (tile
+// layout of load_tile_lds's K), two buffers.  A lane holds the scores of one row and
+// adds 2^(score - lse) into 16 sums, one per key; lanes are added at the end.
+template <int HD>
+__global__ __launch_bounds__(256, 2) void weight_tile_kernel(RowsArgs a) {
+  constexpr int KS = HD / 16, CPR = HD / 8, CH = kWtRows * CPR / 256;
+  __shared__ __align__(16) uint16_t lds[2][kWtRows * HD];
+  const int tid = threadIdx.x, lane = tid & 63, w = wave_id(), hl = lane >> 5;
+  const int units = a.B * a.n_kv, x = (int)blockIdx.x / units, u = (int)blockIdx.x - x * units;
+  const int j = u % a.n_kv, b = u / a.n_kv;
+  const int c = x % a.S_w, tile = x / a.S_w;
+  const Seq sq = seq_of(a, b);
+  const int k0 = tile * kWtKeys;
+  if (k0 >= sq.len) return;
+  const RowSpan rs = rows_of_part(sq, a.g, k0, c, a.S_w);
+  const KeyRange kr = own_range(a, b, j, 0, sq.len);
+  bf16x8_t kf[KS];
+  {
+    const uint16_t* ks = static_cast<const uint16_t*>(a.k) +
+                         (kr.row + min(k0 + 32 * w + (lane & 31), sq.len - 1)) * HD + 8 * hl;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) kf[i] = *reinterpret_cast<const bf16x8_t*>(ks + 16 * i);
+  }
+  float sum[16];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) sum[r] = 0.0f;
+  const int fr0 = b * a.R;
+  const int nt = rs.r1 > rs.r0 ? (rs.r1 - rs.r0 + kWtRows - 1) / kWtRows : 0;
+  auto load = [&](int t) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const int cc = tid + 256 * i, row = cc / CPR, ch = cc - row * CPR;
+      const int fr = fr0 + min(rs.r0 + t * kWtRows + row, rs.r1 - 1);
+      __builtin_amdgcn_global_load_lds(
+          (const __attribute__((address_space(1))) void*)(static_cast<const uint16_t*>(a.q) + q_off(a, j, fr, HD) +
+                                                           8 * (ch ^ (row & (CPR - 1)))),
+          (__attribute__((address_space(3))) void*)(lds[t & 1] + 8 * (64 * w + 256 * i)), 16, 0, 0);
+    }
+  };
+  if (nt > 0) load(0);
+  for (int t = 0; t < nt; ++t) {
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+    __syncthreads();
+    if (t + 1 < nt) load(t + 1);
+#pragma unroll
+    for (int h = 0; h < kWtRows / 32; ++h) {
+      const int row = 32 * h + (lane & 31), r = rs.r0 + t * kWtRows + row;
+      f32x16_t st;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) st[i] = 0.0f;
+      const float lse = r < rs.r1 ? a.lse[(size_t)j * a.B * a.R + fr0 + r] : INFINITY;
+      const int lim = r < rs.r1 ? rows_seen(sq, r / a.g) - k0 - 32 * w : 0;  // keys of the wave that the row sees
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        const bf16x8_t qf =
+            *reinterpret_cast<const bf16x8_t*>(lds[t & 1] + row * HD + 8 * ((2 * i + hl) ^ (row & (CPR - 1))));
+        st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf, st, 0, 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int key = 8 * (i >> 2) + 4 * hl + (i & 3);
+        const float p = exp2_hw(fmaf(st[i], ScoreScale<HD>::v, -lse));
+        sum[i] += key < lim ? p : 0.0f;
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) sum[i] += __shfl_xor(sum[i], o, 64);
+    const int t = k0 + 32 * w + 8 * (i >> 2) + 4 * hl + (i & 3);
+    if ((lane & 31) == 0 && t < sq.len) put_weight(a, c, b, j, t, sum[i]);
+  }
+}
+
+// fp32: one wave per (16 keys of (b, j), part of the rows), 16 rows at a step.
+template <int HD>
+__global__ __launch_bounds__(64) void weight_f32_kernel(RowsArgs a) {
+  constexpr int KC = HD / 16;
+  const int lane = threadIdx.x, rq = lane & 15, lg = lane >> 4;
+  const int units = a.B * a.n_kv, x = (int)blockIdx.x / units, u = (int)blockIdx.x - x * units;
+  const int j = u % a.n_kv, b = u / a.n_kv;
+  const int c = x % a.S_w, tile = x / a.S_w;
+  const Seq sq = seq_of(a, b);
+  const int k0 = tile * 16;
+  if (k0 >= sq.len) return;
+  const RowSpan rs = rows_of_part(sq, a.g, k0, c, a.S_w);
+  const KeyRange kr = own_range(a, b, j, 0, sq.len);
+  f32x4_t kf[KC];
+  const float* ks = static_cast<const float*>(a.k) + (kr.row + min(k0 + rq, sq.len - 1)) * HD + 4 * lg;
+#pragma unroll
+  for (int i = 0; i < KC; ++i) kf[i] = *reinterpret_cast<const f32x4_t*>(ks + 16 * i);
+  float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int r0 = rs.r0; r0 < rs.r1; r0 += 16) {
+    const int r = r0 + rq, fr = b * a.R + min(r, rs.r1 - 1);
+    const float* qs = static_cast<const float*>(a.q) + q_off(a, j, fr, HD) + 4 * lg;
+    f32x4_t s0 = {0.0f, 0.0f, 0.0f, 0.0f}, s1 = s0;
+#pragma unroll
+    for (int i = 0; i < KC; ++i) {
+      const f32x4_t qf = *reinterpret_cast<const f32x4_t*>(qs + 16 * i);
+#pragma unroll
+      for (int e = 0; e < 4; e += 2) {
+        s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[i][e], qf[e], s0, 0, 0, 0);
+        s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[i][e + 1], qf[e + 1], s1, 0, 0, 0);
+      }
+    }
+    const float lse = r < rs.r1 ? a.lse[(size_t)j * a.B * a.R + fr] : INFINITY;
+    const int lim = r < rs.r1 ? rows_seen(sq, r / a.g) - k0 : 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float p = exp2_hw((s0[i] + s1[i]) * ScoreScale<HD>::v - lse);
+      sum[i] += 4 * lg + i < lim ? p : 0.0f;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) sum[i] += __shfl_xor(sum[i], o, 64);
+    const int t = k0 + 4 * lg + i;
+    if (rq == 0 && t < sq.len) put_weight(a, c, b, j, t, sum[i]);
+  }
+}
+
+// weight = decay weight + the S_w parts' sums, in part order.
+__global__ __launch_bounds__(256) void weight_sum_kernel(RowsArgs a) {
+  const int chunks = (a.T_own + 255) / 256;
+  const int bj = (int)blockIdx.x / chunks, t = ((int)blockIdx.x - bj * chunks) * 256 + threadIdx.x;
+  if (t >= seq_of(a, bj / a.n_kv).len) return;
+  float sum = 0.0f;
+  for (int c = 0; c < a.S_w; ++c) sum += a.wpart[((size_t)c * a.B * a.n_kv + bj) * a.T_own + t];
+  float* wp = a.weight + (size_t)bj * a.t_cap + a.t_off + t;
+  *wp = a.decay != 0.0f ? fmaf(a.decay, *wp, sum) : sum;
+}
+
+// ------------------------------------------------------------------ launchers
+
+template <int HD, int G>
+static hipError_t stream_t(const RowsArgs& a, int items, hipStream_t st) {
+  if (a.N > 1)
+    hipLaunchKernelGGL((rows_stream_kernel<HD, G, true>), dim3(items), dim3(64 * kSaWaves), 0, st, a);
+  else
+    hipLaunchKernelGGL((rows_stream_kernel<HD, G, false>), dim3(items), dim3(64 * kSaWaves), 0, st, a);
+  return hipGetLastError();
+}
+
+template <int HD>
+static hipError_t stream_rows(const RowsArgs& a, int rows, int items, hipStream_t st) {
+  switch (sa_group(rows)) {
+    case 1: return stream_t<HD, 1>(a, items, st);
+    case 2: return stream_t<HD, 2>(a, items, st);
+    case 3: return stream_t<HD, 3>(a, items, st);
+    case 4: return stream_t<HD, 4>(a, items, st);
+    case 6: return stream_t<HD, 6>(a, items, st);
+    case 8: return stream_t<HD, 8>(a, items, st);
+    default: return stream_t<HD, 16>(a, items, st);
+  }
+}
+
+#define KVD_LAUNCH_TRY(expr)          \
+  do {                                \
+    hipError_t _e = (expr);           \
+    if (_e != hipSuccess) return _e;  \
+  } while (0)
+
+template <typename T, int HD>
+static hipError_t launch_rows_t(const RowsArgs& a, hipStream_t st) {
+  constexpr bool BF = sizeof(T) == 2;
+  const int RB = BF ? kRowsTile : kRowsWave;
+  const long long nbo = (a.R + RB - 1) / RB, nbp = ((long long)a.B * a.R + RB - 1) / RB;
+  const int S_prefix = a.S_prefix;
+  long long stream_items = 0, tile_items = 0;
+  (a.own_stream ? stream_items : tile_items) += (long long)a.B * a.n_kv * a.S_own * (a.own_stream ? 1 : nbo);
+  (a.prefix_stream ? stream_items : tile_items) += (long long)a.n_kv * S_prefix * (a.prefix_stream ? 1 : nbp);
+  if constexpr (BF) {
+    if (stream_items > 0) {
+      const int rows = a.prefix_stream && S_prefix > 0 ? a.B * a.R : a.R;
+      KVD_LAUNCH_TRY(stream_rows<HD>(a, rows, (int)stream_items, st));
+    }
+    if (tile_items > 0) {
+      hipLaunchKernelGGL(rows_tile_kernel<HD>, dim3((unsigned)tile_items), dim3(256), 0, st, a);
+      KVD_LAUNCH_TRY(hipGetLastError());
+    }
+  } else {
+    hipLaunchKernelGGL(rows_f32_kernel<HD>, dim3((unsigned)tile_items), dim3(64), 0, st, a);
+    KVD_LAUNCH_TRY(hipGetLastError());
+  }
+  const int S = S_prefix + a.S_own;
+  const bool sums = a.weight != nullptr && a.T_own > 0;
+  const long long rows = (long long)a.B * a.R * a.n_kv;
+  const int merge_wgs = S > 1 || a.lse != nullptr ? (int)((rows + kFinishRows - 1) / kFinishRows) : 0;
+  const int weight_wgs = sums && a.sc != nullptr ? a.B * a.n_kv * ((a.T_own + kFinishKeys - 1) / kFinishKeys) : 0;
+  if (merge_wgs + weight_wgs > 0) {
+    hipLaunchKernelGGL((rows_finish_kernel<T, HD>), dim3(merge_wgs + weight_wgs), dim3(256), 0, st, a, merge_wgs);
+    KVD_LAUNCH_TRY(hipGetLastError());
+  }
+  if (sums && a.sc == nullptr) {
+    const int keys = BF ? kWtKeys : 16;
+    const unsigned items = (unsigned)((long long)a.B * a.n_kv * a.S_w * ((a.T_own + keys - 1) / keys));
+    if constexpr (BF)
+      hipLaunchKernelGGL(weight_tile_kernel<HD>, dim3(items), dim3(256), 0, st, a);
+    else
+      hipLaunchKernelGGL(weight_f32_kernel<HD>, dim3(items), dim3(64), 0, st, a);
+    KVD_LAUNCH_TRY(hipGetLastError());
+    if (a.S_w > 1) {
+      hipLaunchKernelGGL(weight_sum_kernel, dim3((unsigned)(a.B * a.n_kv * ((a.T_own + 255) / 256))), dim3(256), 0, st,
+                         a);
+      KVD_LAUNCH_TRY(hipGetLastError());
+    }
+  }
+  return hipSuccess;
+}
+
+hipError_t launch_rows(const RowsArgs& a, int dtype_bf16, int hd, hipStream_t st) {
+  switch (hd) {
+    case 64: return dtype_bf16 ? launch_rows_t<uint16_t, 64>(a, st) : launch_rows_t<float, 64>(a, st);
+    case 128: return dtype_bf16 ? launch_rows_t<uint16_t, 128>(a, st) : launch_rows_t<float, 128>(a, st);
+    case 256: return dtype_bf16 ? launch_rows_t<uint16_t, 256>(a, st) : launch_rows_t<float, 256>(a, st);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+}  // namespace kvd

@@ -76,6 +76,9 @@ def _load() -> ctypes.CDLL:
         "kvd_fused_window_attn": [S, VP, VP, I32, VP, VP, VP, I32, I32, V, I32, I32, VP, VP, SZ, VP],
         "kvd_fused_recompute_attn_noalloc": [S, VP, VP, I32, VP, VP, VP, VP, I32, I32, V, I32, VP, VP],
     }
+    sig["kvd_prefix_attn"] = [S, VP, I32, V, I32, V, VP, VP, I32, I32, VP, VP, ctypes.c_float, VP, SZ, VP]
+    sig["kvd_weighted_attn"] = [S, VP, I32, V, VP, VP, I32, I32, VP, VP, ctypes.c_float, VP, SZ, VP]
+    sig["kvd_evict"] = [S, V, VP, I32, I32, I32, VP, VP, VP, I32, I32, VP, SZ, VP]
     for name, args in sig.items():
         f = getattr(lib, name)
         f.argtypes = args
@@ -92,6 +95,10 @@ def _load() -> ctypes.CDLL:
     lib.kvd_block_forward.restype = ctypes.c_int
     lib.kvd_block_workspace_bytes.argtypes = [S, I32, I32, I32]
     lib.kvd_block_workspace_bytes.restype = SZ
+    lib.kvd_prefix_workspace_bytes.argtypes = [S, I32, I32, I32, I32, I32]
+    lib.kvd_prefix_workspace_bytes.restype = SZ
+    lib.kvd_evict_workspace_bytes.argtypes = [S, I32, I32]
+    lib.kvd_evict_workspace_bytes.restype = SZ
     lib.kvd_combine.argtypes = [S, I32, I32, VP, SZ, VP, VP]
     lib.kvd_combine.restype = ctypes.c_int
     lib.kvd_workspace_bytes.argtypes = [S, I32, I32, I32, I32]
@@ -479,6 +486,143 @@ def kvd_fused_window_attn(shape: Shape, q, h, T_rec: int, gamma, w_k, w_v, windo
         _ptr(gamma, "gamma", dt), _ptr(w_k, "w_k", dt), _ptr(w_v, "w_v", dt), B, T_rec,
         ctypes.byref(tail) if tail is not None else None, T_tail, window,
         _ptr(out, "out", dt, 3) if out is not None else None, wp, wb, _stream()))
+
+
+def kvd_prefix_workspace_bytes(shape: Shape, B: int, N: int, T_prefix: int, T_own: int, weights: bool = False) -> int:
+    return lib.kvd_prefix_workspace_bytes(ctypes.byref(shape.c()), B, N, T_prefix, T_own, int(bool(weights)))
+
+
+def kvd_evict_workspace_bytes(shape: Shape, B: int, T: int) -> int:
+    return lib.kvd_evict_workspace_bytes(ctypes.byref(shape.c()), B, T)
+
+
+def _rows_extents(shape, q, out):
+    """B and N of q and out [B, N, n_q, hd] (or [B, n_q, hd]: one token per sequence)."""
+    if not isinstance(q, torch.Tensor) or q.dim() not in (3, 4):
+        raise ValueError("q must be a [B, N, n_q, head_dim] or [B, n_q, head_dim] tensor")
+    B, N = q.shape[0], q.shape[1] if q.dim() == 4 else 1
+    want = (B, N, shape.n_q_heads, shape.head_dim) if q.dim() == 4 else (B, shape.n_q_heads, shape.head_dim)
+    _extent(q, "q", want)
+    _extent(out, "out", want)
+    if out is None:
+        raise ValueError("out is required")
+    return B, N
+
+
+def _one_device(**tensors):
+    """The device all given tensors live on; ValueError when they differ."""
+    dev = None
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+            raise ValueError(f"{name} must be a torch tensor on the GPU")
+        if dev is not None and t.device != dev:
+            raise ValueError(f"{name} is on {t.device}, the other tensors on {dev}")
+        dev = t.device
+    return dev
+
+
+def _per_seq(t, name, B):
+    _extent(t, name, (B,))
+    return _ptr(t, name, torch.int32)
+
+
+def _prefix_call(fn, shape, q, prefix, T_prefix, own, T_own, own_t_off, out, ws, own_len, n_new, weight, decay,
+                 len_name, own_name):
+    dt = shape.torch_dtype
+    B, N = _rows_extents(shape, q, out)
+    pk, pv, p_off = prefix
+    if T_prefix > 0:
+        for n, t in (("prefix_k", pk), ("prefix_v", pv)):
+            if not isinstance(t, torch.Tensor) or t.dim() != 3:
+                raise ValueError(f"{n} must be a [n_kv, t_cap, head_dim] tensor")
+            _extent(t, n, (shape.n_kv_heads, pk.shape[1], shape.head_dim))
+        if p_off < 0 or p_off + T_prefix > pk.shape[1]:
+            raise ValueError(f"prefix: rows {p_off} .. {p_off + T_prefix - 1} exceed t_cap {pk.shape[1]}")
+    k, v = own
+    if T_own > 0:
+        if k is None or v is None:
+            raise ValueError(f"{own_name}: k and v are required")
+        _kv_extent(k, v, own_name, B, shape, T_own, own_t_off)
+    if weight is not None:
+        if T_own < 1:
+            raise ValueError("weights need own rows")
+        _extent(weight, "weight", (B, shape.n_kv_heads, k.shape[2]))
+    _extent(own_len, len_name, (B,))
+    _extent(n_new, "n_new", (B,))
+    if not T_prefix > 0:
+        pk = pv = None
+    if not T_own > 0:
+        k = v = None
+    dev = _one_device(q=q, out=out, prefix_k=pk, prefix_v=pv, k=k, v=v, weight=weight, ws=ws,
+                      **{len_name: own_len, "n_new": n_new})
+    own_view = _view(k, v, own_t_off, own_name, dt)
+    view = None if pk is None else KvView(_ptr(pk, "prefix_k", dt), _ptr(pv, "prefix_v", dt), pk.shape[1], p_off)
+    wp, wb = _ws(ws)
+    own_ref = ctypes.byref(own_view) if own_view is not None else None
+    head = [ctypes.byref(shape.c()), _ptr(q, "q", dt), N]
+    if fn is lib.kvd_prefix_attn:
+        head += [ctypes.byref(view) if view is not None else None, T_prefix]
+    args = head + [own_ref, _per_seq(own_len, len_name, B), _per_seq(n_new, "n_new", B), B, T_own,
+                   _ptr(out, "out", dt), _ptr(weight, "weight", torch.float32), decay, wp, wb]
+    with torch.cuda.device(dev):
+        _check(fn(*args, _stream()))
+
+
+def kvd_prefix_attn(shape: Shape, q, prefix_k, prefix_v, T_prefix: int, own_k, own_v, T_own: int, out, ws,
+                    own_len=None, n_new=None, weight=None, decay: float = 0.0, prefix_t_off: int = 0,
+                    own_t_off: int = 0):
+    """Attention of q [B, N, n_q, hd] (or [B, n_q, hd]) over T_prefix rows of prefix_k / prefix_v
+    [n_kv, t_cap, hd] that all sequences share, then over each sequence's own rows own_t_off.. of own_k / own_v
+    [B, n_kv, t_cap, hd]: own_len [B] int32 of them (T_own if None), of which the last n_new [B] (N if None)
+    belong to the new tokens, each seeing the rows up to its own.  With weight [B, n_kv, t_cap] fp32 the weight
+    each own row received is added to decay * weight.  Runs on the tensors' device and its current stream."""
+    _prefix_call(lib.kvd_prefix_attn, shape, q, (prefix_k, prefix_v, prefix_t_off), T_prefix, (own_k, own_v), T_own,
+                 own_t_off, out, ws, own_len, n_new, weight, decay, "own_len", "own")
+
+
+def kvd_weighted_attn(shape: Shape, q, k, v, T: int, weight, out, ws, kv_len=None, n_new=None, decay: float = 1.0,
+                      t_off: int = 0):
+    """Attention of q [B, N, n_q, hd] (or [B, n_q, hd]) over stored rows t_off.. of k / v [B, n_kv, t_cap, hd]
+    (kv_len [B] int32 of them, T if None; the last n_new [B], N if None, belong to the new tokens), adding the
+    weight each row received to decay * weight [B, n_kv, t_cap] fp32."""
+    if weight is None:
+        raise ValueError("weight is required")
+    _prefix_call(lib.kvd_weighted_attn, shape, q, (None, None, 0), 0, (k, v), T, t_off, out, ws, kv_len, n_new, weight,
+                 decay, "kv_len", "kv")
+
+
+def kvd_evict(shape: Shape, k, v, T: int, keep: int, weight, ws, pos=None, last_pos=None, kv_len=None, sink: int = 0,
+              recent: int = 0, t_off: int = 0):
+    """Keep, in place, the `keep` heaviest of the T rows (kv_len [B] int32, updated, of them if given) of every
+    (sequence, KV head) of k / v [B, n_kv, t_cap, hd]: rows with pos < sink or pos > last_pos[b] - recent first,
+    then by weight [B, n_kv, t_cap] fp32.  Rows that stay behind slot `keep` move into the freed slots, with
+    their weight and pos [B, n_kv, t_cap] int32."""
+    dt = shape.torch_dtype
+    if not isinstance(k, torch.Tensor) or k.dim() != 4:
+        raise ValueError("kv: k and v must both be [B, n_kv, t_cap, head_dim] tensors")
+    B = k.shape[0]
+    _kv_extent(k, v, "kv", B, shape, T, t_off)
+    per_row = (B, shape.n_kv_heads, k.shape[2])
+    if weight is None:
+        raise ValueError("weight is required")
+    _extent(weight, "weight", per_row)
+    _extent(pos, "pos", per_row)
+    _extent(last_pos, "last_pos", (B,))
+    _extent(kv_len, "kv_len", (B,))
+    if pos is None and (sink > 0 or recent > 0):
+        raise ValueError("pos is required when sink or recent is positive")
+    if last_pos is None and recent > 0:
+        raise ValueError("last_pos is required when recent is positive")
+    dev = _one_device(k=k, v=v, weight=weight, ws=ws, pos=pos, last_pos=last_pos, kv_len=kv_len)
+    view = _view(k, v, t_off, "kv", dt)
+    wp, wb = _ws(ws)
+    args = [ctypes.byref(shape.c()), ctypes.byref(view), _per_seq(kv_len, "kv_len", B), B, T, keep,
+            _ptr(weight, "weight", torch.float32), _ptr(pos, "pos", torch.int32), _per_seq(last_pos, "last_pos", B),
+            sink, recent, wp, wb]
+    with torch.cuda.device(dev):
+        _check(lib.kvd_evict(*args, _stream()))
 
 
 def kvd_pack_matrix(w):
