@@ -282,51 +282,67 @@ __global__ __launch_bounds__(64 * kSaWaves) __attribute__((amdgpu_waves_per_eu(2
 // Keys per LDS tile: 32 KiB of K and V.
 constexpr int rows_kt(int hd) { return hd == 256 ? 32 : 64; }
 
-// Direct global-to-LDS copy of KT key rows of K and V (rows past n - 1 repeat row n -
-// 1).  Row r's 16-byte chunk c lies at chunk c ^ (r % CPR) of its LDS row for K, at c ^
-// 2 (r % 4) for V: the score operand reads the same chunk of 32 rows, the transposing
-// V reads 64 bytes of 4 rows; both then touch every bank evenly.
-template <int HD>
-__device__ __forceinline__ void load_tile_lds(const uint16_t* K, const uint16_t* V, int k0, int n, uint16_t* ks,
-                                              uint16_t* vs) {
-  constexpr int KT = rows_kt(HD), CPR = HD / 8, CH = KT * CPR / 256;
+// Copies KT rows of HD elements from global memory straight into the LDS tile dst (rows
+// past n - 1 repeat row n - 1).  Row r's 16-byte chunk c lies at chunk c ^ swz(r) of its
+// LDS row: for the score operands (SCORE), whose lanes read one chunk of 32 rows, swz =
+// r % 8; for V, whose transposing reads take 64 bytes of 4 rows, swz = 2 (r % 4).  Both
+// then touch every bank evenly.  Thread tid copies chunk tid % CPR of rows tid / CPR +
+// 8192 / (4 HD) i, so that swz does not depend on i and a full tile needs no address
+// arithmetic: one offset per thread, the tile in the buffer resource, 4096 i as a scalar.
+template <int HD, int KT, bool SCORE>
+__device__ __forceinline__ void copy_tile(const uint16_t* src, int n, uint16_t* dst) {
+  constexpr int CPR = HD / 8, RPI = 256 / CPR, CH = KT / RPI;
   const int tid = threadIdx.x, w = wave_id();
+  const int r0 = tid / CPR;
+  const int col = 16 * ((tid % CPR) ^ (SCORE ? r0 & 7 : 2 * (r0 & 3)));
+  const __amdgpu_buffer_rsrc_t res =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(src), (short)0, KT * HD * 2, 0x00027000);
+  if (n >= KT) {
 #pragma unroll
-  for (int i = 0; i < CH; ++i) {
-    const int c = tid + 256 * i, row = c / CPR, ch = c - row * CPR;
-    const size_t key = (size_t)min(k0 + row, n - 1) * HD;
-    const int dst = 8 * (64 * w + 256 * i);  // wave-uniform; lane l's 16 bytes follow at 16 l
-    __builtin_amdgcn_global_load_lds(
-        (const __attribute__((address_space(1))) void*)(K + key + 8 * (ch ^ (row & (CPR - 1)))),
-        (__attribute__((address_space(3))) void*)(ks + dst), 16, 0, 0);
-    __builtin_amdgcn_global_load_lds(
-        (const __attribute__((address_space(1))) void*)(V + key + 8 * (ch ^ (2 * (row & 3)))),
-        (__attribute__((address_space(3))) void*)(vs + dst), 16, 0, 0);
+    for (int i = 0; i < CH; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (__attribute__((address_space(3))) void*)(dst + 512 * w + 2048 * i),
+                                               16, r0 * HD * 2 + col, 4096 * i, 0, 0);
+  } else {
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (__attribute__((address_space(3))) void*)(dst + 512 * w + 2048 * i),
+                                               16, min(r0 + RPI * i, n - 1) * HD * 2 + col, 0, 0, 0);
   }
 }
 
 typedef short i16x4_t __attribute__((ext_vector_type(4)));
 
-// V^T operand of a 32-row block db of O^T for the 16 keys at k0 of the LDS tile: two
-// transposing reads (in a group of 16 lanes, lane s names 4 columns of row s / 4 of a
-// 4-key group, and lane i receives column i of the 4 keys).  Lane half hl gets keys
-// k0 + 4 hl + {0..3, 8..11}, the ones whose scores it holds.
+// Byte offsets of a lane's operands in the LDS tiles.
+// Score operand: row lane % 32, elements 16 kk + 8 (lane / 32) ..; 32 rows on: + 64 HD.
 template <int HD>
-__device__ __forceinline__ bf16x8_t v_operand(const uint16_t* vs, int k0, int db, int lane) {
-  const int hl = lane >> 5;
-  const int row = k0 + 4 * hl + ((lane & 15) >> 2);
-  const int ch = (4 * db + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ (2 * (row & 3));
-  const uint16_t* p = vs + row * HD + 8 * ch + 4 * (lane & 1);
+__device__ __forceinline__ uint32_t score_base(int lane) {
+  return (lane & 31) * HD * 2 + (((lane >> 5) ^ (lane & 7)) << 4);
+}
+__device__ __forceinline__ bf16x8_t score_operand(const uint16_t* tile, uint32_t base, int kk, int rows) {
+  return *reinterpret_cast<const bf16x8_t*>(reinterpret_cast<const char*>(tile) + (base ^ (kk << 5)) + rows);
+}
+// V^T operand of a 32-row block db of O^T for the 16 keys at k0: two transposing reads
+// (in a group of 16 lanes, lane s names 4 columns of row s / 4 of a 4-key group, and lane
+// i receives column i of the 4 keys).  Lane half hl gets keys k0 + 4 hl + {0..3, 8..11},
+// the ones whose scores it holds.
+template <int HD>
+__device__ __forceinline__ uint32_t v_base(int lane) {
+  return (4 * (lane >> 5) + ((lane & 15) >> 2)) * HD * 2 +
+         (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ (2 * ((lane >> 2) & 3))) << 4) + 8 * (lane & 1);
+}
+template <int HD>
+__device__ __forceinline__ bf16x8_t v_operand(const uint16_t* vs, uint32_t base, int k0, int db) {
+  const char* p = reinterpret_cast<const char*>(vs) + (base ^ (db << 6)) + k0 * HD * 2;
   const i16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4_t*)p);
-  const i16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4_t*)(p + 8 * HD));
+  const i16x4_t hi =
+      __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4_t*)(p + 16 * HD));
   return __builtin_bit_cast(bf16x8_t, make_uint4(__builtin_bit_cast(uint2, lo).x, __builtin_bit_cast(uint2, lo).y,
                                                  __builtin_bit_cast(uint2, hi).x, __builtin_bit_cast(uint2, hi).y));
 }
 
 // Two bf16 in a word: nonzero where one is infinite or NaN (the exponent's carry).
 __device__ __forceinline__ uint32_t nonfinite2(uint32_t x) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
-// Non-finite halves replaced by 0, and by a code that a sum over up to 127 keys keeps
-// apart: +inf 1, -inf 128, NaN 16384.
+// A code for a non-finite value that sums over up to 127 keys keep apart, and back.
 __device__ __forceinline__ float code_of(float v) {
   return v == INFINITY ? 1.0f : v == -INFINITY ? 128.0f : 16384.0f;
 }
@@ -336,21 +352,6 @@ __device__ __forceinline__ float poison_of(float codes) {
   const bool pos = (c & 127) != 0, neg = ((c >> 7) & 127) != 0;
   return c >= 16384 || (pos && neg) ? __uint_as_float(0x7fc00000u) : pos ? INFINITY : -INFINITY;
 }
-__device__ __forceinline__ void split_nonfinite(bf16x8_t v, bf16x8_t& fin, bf16x8_t& code) {
-  const uint4 x = __builtin_bit_cast(uint4, v);
-  const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
-  uint32_t f[4], c[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t nf = nonfinite2(xs[i]);
-    const float lo = bf_lo(xs[i]), hi = bf_hi(xs[i]);
-    f[i] = xs[i] & ((nf & 0x8000u ? 0u : 0xffffu) | (nf & 0x80000000u ? 0u : 0xffff0000u));
-    c[i] = pack_bf16x2(nf & 0x8000u ? code_of(lo) : 0.0f, nf & 0x80000000u ? code_of(hi) : 0.0f);
-  }
-  fin = __builtin_bit_cast(bf16x8_t, make_uint4(f[0], f[1], f[2], f[3]));
-  code = __builtin_bit_cast(bf16x8_t, make_uint4(c[0], c[1], c[2], c[3]));
-}
-
 // One workgroup of 4 waves per (128-row block, key range), 32 rows per wave, through
 // the range's key tiles: first its prefix keys, then its own ones (one of them empty
 // unless the call is joint).  Tile t + 1 is copied into the other LDS buffer while tile
@@ -362,9 +363,9 @@ __device__ __forceinline__ void split_nonfinite(bf16x8_t v, bf16x8_t& fin, bf16x
 // rounding; the sum is taken before the rounding).
 template <int HD>
 __global__ __launch_bounds__(256, 2) void rows_tile_kernel(RowsArgs a) {
-  constexpr int KT = rows_kt(HD), KH = KT / 32, KS = HD / 16, DB = HD / 32, CPR = HD / 8;
+  constexpr int KT = rows_kt(HD), KH = KT / 32, KS = HD / 16, DB = HD / 32;
   __shared__ __align__(16) uint16_t lds[2][2][KT * HD];
-  const int tid = threadIdx.x, lane = tid & 63, w = wave_id(), hl = lane >> 5;
+  const int lane = threadIdx.x & 63, w = wave_id(), hl = lane >> 5;
   // the item: own (or joint) row blocks first, then the prefix's
   const int nbo = (a.R + kRowsTile - 1) / kRowsTile;
   const int own_items = a.own_stream ? 0 : a.B * a.n_kv * nbo * a.S_own;
@@ -428,28 +429,43 @@ __global__ __launch_bounds__(256, 2) void rows_tile_kernel(RowsArgs a) {
     for (int ks = 0; ks < KS; ++ks) qf[ks] = *reinterpret_cast<const bf16x8_t*>(qs + 16 * ks);
   }
   f32x16_t o[DB];
+  float m_run, l_run;  // in units of the scaled score
+
+  const uint32_t kbase = score_base<HD>(lane), vbase = v_base<HD>(lane);
+  auto load = [&](int t) {
+    uint16_t* ks = lds[t & 1][0];
+    uint16_t* vs = lds[t & 1][1];
+    const int k = (t < np ? t : t - np) * KT, n = (t < np ? kp.n : ko.n) - k;
+    copy_tile<HD, KT, true>((t < np ? Kp : Ko) + (size_t)k * HD, n, ks);
+    copy_tile<HD, KT, false>((t < np ? Vp : Vo) + (size_t)k * HD, n, vs);
+  };
+  // A second pass where an infinite or NaN value met a weight of 0 (a row that does not
+  // see it): such values count as 0 there and are added afterwards where they are seen.
+  int pass = 0;
+again:
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[db][i] = 0.0f;
-  float m_run = -INFINITY, l_run = 0.0f;  // in units of the scaled score
-
-  auto load = [&](int t) {
-    uint16_t* ks = lds[t & 1][0];
-    uint16_t* vs = lds[t & 1][1];
-    if (t < np)
-      load_tile_lds<HD>(Kp, Vp, t * KT, kp.n, ks, vs);
-    else
-      load_tile_lds<HD>(Ko, Vo, (t - np) * KT, ko.n, ks, vs);
-  };
+  m_run = -INFINITY;
+  l_run = 0.0f;
+  bool odd = false;
   if (nt > 0) load(0);
   for (int t = 0; t < nt; ++t) {
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's share of tile t is in LDS
     __syncthreads();                     // every wave's share, and tile t - 1 is no longer read
     if (t + 1 < nt) load(t + 1);
-    if (!wave_on) continue;
     const uint16_t* ks = lds[t & 1][0];
     const uint16_t* vs = lds[t & 1][1];
+    if (pass == 1) {
+      for (int i = threadIdx.x; i < KT * HD / 2; i += 256) {
+        uint32_t* x = reinterpret_cast<uint32_t*>(lds[t & 1][1]) + i;
+        const uint32_t nf = nonfinite2(*x);
+        if (nf != 0) *x &= (nf & 0x8000u ? 0u : 0xffffu) | (nf & 0x80000000u ? 0u : 0xffff0000u);
+      }
+      __syncthreads();
+    }
+    if (!wave_on) continue;
     const bool is_own = t >= np;
     const int k0 = (is_own ? t - np : t) * KT;
     const int row_lim = is_own ? lim : kp.n;
@@ -464,9 +480,7 @@ __global__ __launch_bounds__(256, 2) void rows_tile_kernel(RowsArgs a) {
     for (int kk = 0; kk < KS; ++kk) {
 #pragma unroll
       for (int kh = 0; kh < KH; ++kh) {
-        const int row = 32 * kh + (lane & 31);
-        const bf16x8_t kf =
-            *reinterpret_cast<const bf16x8_t*>(ks + row * HD + 8 * ((2 * kk + hl) ^ (row & (CPR - 1))));
+        const bf16x8_t kf = score_operand(ks, kbase, kk, 64 * HD * kh);
         st[kh] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[kk], st[kh], 0, 0, 0);
       }
     }
@@ -510,56 +524,45 @@ __global__ __launch_bounds__(256, 2) void rows_tile_kernel(RowsArgs a) {
       pf[tt] = __builtin_bit_cast(bf16x8_t, make_uint4(pw[0], pw[1], pw[2], pw[3]));
     }
     l_run += sum;  // this lane's keys; lane ^ 32 holds the others
-    bool odd = false;  // an infinite or NaN value where some row is masked
-    if (masked) {
+#pragma unroll
+    for (int tt = 0; tt < 2 * KH; ++tt)
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand<HD>(vs, vbase, 16 * tt, db), pf[tt], o[db], 0, 0, 0);
+    if (masked && pass == 0) {
       uint32_t nf = 0;
-#pragma unroll
-      for (int tt = 0; tt < 2 * KH; ++tt)
-#pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          const uint4 x = __builtin_bit_cast(uint4, v_operand<HD>(vs, 16 * tt, db, lane));
-          nf |= nonfinite2(x.x) | nonfinite2(x.y) | nonfinite2(x.z) | nonfinite2(x.w);
-        }
-      odd = __any(nf != 0);
-    }
-    if (!odd) {
-#pragma unroll
-      for (int tt = 0; tt < 2 * KH; ++tt)
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand<HD>(vs, 16 * tt, db, lane), pf[tt], o[db], 0, 0, 0);
-    } else {
-      // the finite part, and which rows see which infinities: 0 * inf never arises
-      bf16x8_t seen[2 * KH];
-#pragma unroll
-      for (int tt = 0; tt < 2 * KH; ++tt) {
-        uint32_t sw[4];
-#pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-          const int key = k0 + 32 * (tt >> 1) + 16 * (tt & 1) + 8 * (e >> 2) + 4 * hl + (e & 3);
-          sw[e >> 1] = (key < row_lim ? 0x3f80u : 0u) | (key + 1 < row_lim ? 0x3f800000u : 0u);
-        }
-        seen[tt] = __builtin_bit_cast(bf16x8_t, make_uint4(sw[0], sw[1], sw[2], sw[3]));
+#pragma unroll 1
+      for (int i = lane; i < KT * HD / 8; i += 64) {
+        const uint4 x = *reinterpret_cast<const uint4*>(vs + 8 * i);
+        nf |= nonfinite2(x.x) | nonfinite2(x.y) | nonfinite2(x.z) | nonfinite2(x.w);
       }
-#pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        f32x16_t codes;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) codes[i] = 0.0f;
-#pragma unroll
-        for (int tt = 0; tt < 2 * KH; ++tt) {
-          bf16x8_t fin, code;
-          split_nonfinite(v_operand<HD>(vs, 16 * tt, db, lane), fin, code);
-          o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fin, pf[tt], o[db], 0, 0, 0);
-          codes = __builtin_amdgcn_mfma_f32_32x32x16_bf16(code, seen[tt], codes, 0, 0, 0);
-        }
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[db][i] += poison_of(codes[i]);
-      }
+      odd |= __any(nf != 0);
     }
   }
-
+  if (pass == 0 && __syncthreads_or(odd)) {
+    pass = 1;
+    goto again;
+  }
   l_run += __shfl_xor(l_run, 32, 64);
+
+  if (pass == 1) {
+    // the infinite and NaN values that pass 1 took as 0, for the rows that see them
+#pragma unroll 1
+    for (int t = 0; t < kp.n + ko.n; ++t) {
+      const bool is_own = t >= kp.n;
+      if (!wave_on || (is_own && t - kp.n >= lim)) continue;
+      const uint16_t* vr = (is_own ? Vo + (size_t)(t - kp.n) * HD : Vp + (size_t)t * HD) + 4 * hl;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int q4 = 0; q4 < 4; ++q4) {
+          const uint2 y = *reinterpret_cast<const uint2*>(vr + 32 * db + 8 * q4);
+          const float v[4] = {bf_lo(y.x), bf_hi(y.x), bf_lo(y.y), bf_hi(y.y)};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[db][4 * q4 + e] += fabsf(v[e]) < INFINITY ? 0.0f : v[e];
+        }
+    }
+  }
   if (rl >= nr || !row_wanted(a, fr)) return;
   const float m_out = m_run == -INFINITY ? 0.0f : m_run;
   const bool direct = a.S_prefix + a.S_own == 1;
@@ -601,7 +604,8 @@ __global__ __launch_bounds__(256, 2) void rows_tile_kernel(RowsArgs a) {
 // P V: O^T = V^T P^T, step t takes the keys 4 lg + t, whose weights the lanes hold; a
 // lane's 16 bytes of V row 4 lg + t (dims 64 u + 4 (lane % 16) ..) are the A operands of
 // four MFMAs, MFMA e giving dims 64 u + 4 i + e.  No LDS.  Masked keys: score -inf;
-// a non-finite value that some row does not see is split off (split_nonfinite's codes).
+// a non-finite value that some row does not see is taken out of the product, and its code
+// (code_of), summed over the keys a row does see, puts it back.
 template <int HD>
 __global__ __launch_bounds__(64) void rows_f32_kernel(RowsArgs a) {
   constexpr int KC = HD / 16, VU = HD / 64;
@@ -881,7 +885,7 @@ constexpr int kWtKeys = 128, kWtRows = 64;
 
 // bf16: one workgroup of 4 waves per (128 keys of (b, j), part of the rows).  A wave
 // keeps its 32 keys as MFMA A operands; the rows pass through LDS 64 at a time (tile
-// layout of load_tile_lds's K), two buffers.  A lane holds the scores of one row and
+// layout of copy_tile's score operands), two buffers.  A lane holds the scores of one row and
 // adds 2^(score - lse) into 16 sums, one per key; lanes are added at the end.
 template <int HD>
 __global__ __launch_bounds__(256, 2) void weight_tile_kernel(RowsArgs a) {
@@ -907,6 +911,7 @@ __global__ __launch_bounds__(256, 2) void weight_tile_kernel(RowsArgs a) {
 #pragma unroll
   for (int r = 0; r < 16; ++r) sum[r] = 0.0f;
   const int fr0 = b * a.R;
+  const uint32_t qbase = score_base<HD>(lane);
   const int nt = rs.r1 > rs.r0 ? (rs.r1 - rs.r0 + kWtRows - 1) / kWtRows : 0;
   auto load = [&](int t) {
 #pragma unroll
@@ -915,7 +920,7 @@ __global__ __launch_bounds__(256, 2) void weight_tile_kernel(RowsArgs a) {
       const int fr = fr0 + min(rs.r0 + t * kWtRows + row, rs.r1 - 1);
       __builtin_amdgcn_global_load_lds(
           (const __attribute__((address_space(1))) void*)(static_cast<const uint16_t*>(a.q) + q_off(a, j, fr, HD) +
-                                                           8 * (ch ^ (row & (CPR - 1)))),
+                                                           8 * (ch ^ (row & 7))),
           (__attribute__((address_space(3))) void*)(lds[t & 1] + 8 * (64 * w + 256 * i)), 16, 0, 0);
     }
   };
@@ -934,8 +939,7 @@ __global__ __launch_bounds__(256, 2) void weight_tile_kernel(RowsArgs a) {
       const int lim = r < rs.r1 ? rows_seen(sq, r / a.g) - k0 - 32 * w : 0;  // keys of the wave that the row sees
 #pragma unroll
       for (int i = 0; i < KS; ++i) {
-        const bf16x8_t qf =
-            *reinterpret_cast<const bf16x8_t*>(lds[t & 1] + row * HD + 8 * ((2 * i + hl) ^ (row & (CPR - 1))));
+        const bf16x8_t qf = score_operand(lds[t & 1], qbase, i, 64 * HD * h);
         st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf, st, 0, 0, 0);
       }
 #pragma unroll
