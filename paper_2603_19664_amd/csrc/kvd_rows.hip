@@ -781,20 +781,24 @@ __global__ __launch_bounds__(64) void rows_f32_kernel(RowsArgs a) {
 
 // ------------------------------------------------------------------ merge and streamed weights
 
-// Merged (max, sum) of a row's S states, by one wave: lane s takes states s, s + 64, ...
-__device__ __forceinline__ void merge_ml(const RowsArgs& a, int S, int j, int fr, int lane, float& M, float& L) {
-  M = -INFINITY;
-  for (int s = lane; s < S; s += 64) {
-    const float2 x = *reinterpret_cast<const float2*>(a.ml + 2 * slot_row(a, s, j, fr));
-    if (x.y != 0.0f) M = fmaxf(M, x.x);
-  }
-  M = wave_max(M);
-  L = 0.0f;
-  for (int s = lane; s < S; s += 64) {
-    const float2 x = *reinterpret_cast<const float2*>(a.ml + 2 * slot_row(a, s, j, fr));
-    if (x.y != 0.0f) L = fmaf(x.y, exp2_hw(x.x - M), L);
-  }
-  L = wave_sum(L);
+// A row's S <= 128 states, by one wave: lane s takes the (max, sum) of states s and s + 64.
+// Their merged max M and sum L, and the weights 2^(max - M) (0 for an empty state).
+struct Merge {
+  float M, L, w0, w1;
+};
+__device__ __forceinline__ Merge merge_states(const RowsArgs& a, int S, int j, int fr, int lane) {
+  float2 x = make_float2(-INFINITY, 0.0f), y = x;
+  if (lane < S) x = *reinterpret_cast<const float2*>(a.ml + 2 * slot_row(a, lane, j, fr));
+  if (lane + 64 < S) y = *reinterpret_cast<const float2*>(a.ml + 2 * slot_row(a, lane + 64, j, fr));
+  if (x.y == 0.0f) x.x = -INFINITY;
+  if (y.y == 0.0f) y.x = -INFINITY;
+  Merge m;
+  m.M = wave_max(fmaxf(x.x, y.x));
+  const float Mu = m.M == -INFINITY ? 0.0f : m.M;
+  m.w0 = exp2_hw(x.x - Mu);
+  m.w1 = exp2_hw(y.x - Mu);
+  m.L = wave_sum(fmaf(x.y, m.w0, y.y * m.w1));
+  return m;
 }
 
 constexpr int kFinishRows = 4;     // merged rows per workgroup (one per wave)
@@ -815,23 +819,30 @@ __global__ __launch_bounds__(256) void rows_finish_kernel(RowsArgs a, int merge_
     const int j = (int)(idx / Rt), fr = (int)(idx - (long long)j * Rt);
     const int tok = fr / a.g, b = tok / a.N;
     if (tok - b * a.N >= seq_of(a, b).n) return;
-    float M, L;
-    merge_ml(a, S, j, fr, lane, M, L);
-    if (a.lse != nullptr && lane == 0) a.lse[(size_t)j * Rt + fr] = L != 0.0f ? M + __builtin_amdgcn_logf(L) : INFINITY;
+    const Merge m = merge_states(a, S, j, fr, lane);
+    if (a.lse != nullptr && lane == 0)
+      a.lse[(size_t)j * Rt + fr] = m.L != 0.0f ? m.M + __builtin_amdgcn_logf(m.L) : INFINITY;
     if (S == 1) return;  // written by the attention kernel itself
     float x[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] = 0.0f;
-    for (int s = 0; s < S; ++s) {
-      const size_t row = slot_row(a, s, j, fr);
-      const float2 ml = *reinterpret_cast<const float2*>(a.ml + 2 * row);
-      if (ml.y == 0.0f) continue;
-      const float wt = exp2_hw(ml.x - M);
-      float y[E];
-      load_e<E>(a.acc + row * HD + E * lane, y);
+    // 8 states' loads in flight; an empty state's acc was never written and counts as 0
+    const float* src = a.acc + slot_row(a, 0, j, fr) * HD + E * lane;
+    const size_t step = (size_t)a.n_kv * Rt * HD;
+    for (int s0 = 0; s0 < S; s0 += 8) {
+      float y[8][E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) x[e] = fmaf(y[e], wt, x[e]);
+      for (int i = 0; i < 8; ++i) load_e<E>(src + (size_t)min(s0 + i, S - 1) * step, y[i]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int s = min(s0 + i, 127);
+        const float wt = __builtin_bit_cast(
+            float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, s < 64 ? m.w0 : m.w1), s & 63));
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = s0 + i < S && wt != 0.0f ? fmaf(y[i][e], wt, x[e]) : x[e];
+      }
     }
+    const float L = m.L;
     T* dst = static_cast<T*>(a.out) + q_off(a, j, fr, HD) + E * lane;
 #pragma unroll
     for (int e = 0; e < E; ++e) dst[e] = from_f<T>(L != 0.0f ? x[e] / L : 0.0f);
@@ -843,9 +854,8 @@ __global__ __launch_bounds__(256) void rows_finish_kernel(RowsArgs a, int merge_
   const int j = u % a.n_kv, b = u / a.n_kv;
   const Seq sq = seq_of(a, b);
   for (int r = w; r < sq.n * a.g; r += 4) {
-    float M, L;
-    merge_ml(a, S, j, b * a.R + r, lane, M, L);
-    if (lane == 0) lse[r] = L != 0.0f ? M + __builtin_amdgcn_logf(L) : INFINITY;
+    const Merge m = merge_states(a, S, j, b * a.R + r, lane);
+    if (lane == 0) lse[r] = m.L != 0.0f ? m.M + __builtin_amdgcn_logf(m.L) : INFINITY;
   }
   __syncthreads();
   const int t = c * kFinishKeys + threadIdx.x;

@@ -496,78 +496,103 @@ def kvd_evict_workspace_bytes(shape: Shape, B: int, T: int) -> int:
     return lib.kvd_evict_workspace_bytes(ctypes.byref(shape.c()), B, T)
 
 
-def _rows_extents(shape, q, out):
-    """B and N of q and out [B, N, n_q, hd] (or [B, n_q, hd]: one token per sequence)."""
-    if not isinstance(q, torch.Tensor) or q.dim() not in (3, 4):
-        raise ValueError("q must be a [B, N, n_q, head_dim] or [B, n_q, head_dim] tensor")
-    B, N = q.shape[0], q.shape[1] if q.dim() == 4 else 1
-    want = (B, N, shape.n_q_heads, shape.head_dim) if q.dim() == 4 else (B, shape.n_q_heads, shape.head_dim)
-    _extent(q, "q", want)
-    _extent(out, "out", want)
-    if out is None:
-        raise ValueError("out is required")
-    return B, N
+def _dims(t, name, want):
+    """ValueError unless tensor t has exactly the extents `want`."""
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name} must be a torch tensor")
+    if t.shape != want:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(want)}")
 
 
-def _one_device(**tensors):
-    """The device all given tensors live on; ValueError when they differ."""
-    dev = None
-    for name, t in tensors.items():
-        if t is None:
-            continue
-        if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+def _dev_ptr(t, name, dtype, dev):
+    """t's pointer, once its device, dtype and layout are checked (None for None)."""
+    if t is None:
+        return None
+    if t.device != dev:
+        if t.device.type != "cuda":
             raise ValueError(f"{name} must be a torch tensor on the GPU")
-        if dev is not None and t.device != dev:
-            raise ValueError(f"{name} is on {t.device}, the other tensors on {dev}")
-        dev = t.device
-    return dev
+        raise ValueError(f"{name} is on {t.device}, q or k on {dev}")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
 
 
-def _per_seq(t, name, B):
-    _extent(t, name, (B,))
-    return _ptr(t, name, torch.int32)
+def _device_of(t, name):
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} must be a torch tensor on the GPU")
+    return t.device
+
+
+def _run_on(dev, fn, *args):
+    """fn(*args, stream) on device dev and its current stream."""
+    i = dev.index
+    if torch.cuda.current_device() == i:
+        return _check(fn(*args, torch._C._cuda_getCurrentRawStream(i)))
+    with torch.cuda.device(i):
+        _check(fn(*args, torch._C._cuda_getCurrentRawStream(i)))
+
+
+def _own_dims(k, v, name, B, shape, T, t_off):
+    if k is None or v is None:
+        raise ValueError(f"{name}: k and v are required")
+    if not isinstance(k, torch.Tensor) or k.dim() != 4:
+        raise ValueError(f"{name}: k and v must both be [B, n_kv, t_cap, head_dim] tensors")
+    want = (B, shape.n_kv_heads, k.shape[2], shape.head_dim)
+    _dims(k, name + "_k", want)
+    _dims(v, name + "_v", want)
+    if t_off < 0 or t_off + T > want[2]:
+        raise ValueError(f"{name}: rows {t_off} .. {t_off + T - 1} exceed t_cap {want[2]}")
+    return want[2]
 
 
 def _prefix_call(fn, shape, q, prefix, T_prefix, own, T_own, own_t_off, out, ws, own_len, n_new, weight, decay,
                  len_name, own_name):
-    dt = shape.torch_dtype
-    B, N = _rows_extents(shape, q, out)
-    pk, pv, p_off = prefix
+    # extents first, of everything; then devices, dtypes and layouts; then the call
+    if not isinstance(q, torch.Tensor) or q.dim() not in (3, 4):
+        raise ValueError("q must be a [B, N, n_q, head_dim] or [B, n_q, head_dim] tensor")
+    B, N = q.shape[0], q.shape[1] if q.dim() == 4 else 1
+    if q.shape[-2:] != (shape.n_q_heads, shape.head_dim):
+        raise ValueError(f"q has shape {tuple(q.shape)}, expected [.., {shape.n_q_heads}, {shape.head_dim}]")
+    if out is None:
+        raise ValueError("out is required")
+    _dims(out, "out", q.shape)
+    pk = pv = k = v = None
+    t_cap = 0
     if T_prefix > 0:
-        for n, t in (("prefix_k", pk), ("prefix_v", pv)):
-            if not isinstance(t, torch.Tensor) or t.dim() != 3:
-                raise ValueError(f"{n} must be a [n_kv, t_cap, head_dim] tensor")
-            _extent(t, n, (shape.n_kv_heads, pk.shape[1], shape.head_dim))
-        if p_off < 0 or p_off + T_prefix > pk.shape[1]:
-            raise ValueError(f"prefix: rows {p_off} .. {p_off + T_prefix - 1} exceed t_cap {pk.shape[1]}")
-    k, v = own
+        pk, pv, p_off = prefix
+        if not isinstance(pk, torch.Tensor) or pk.dim() != 3:
+            raise ValueError("prefix_k must be a [n_kv, t_cap, head_dim] tensor")
+        want = (shape.n_kv_heads, pk.shape[1], shape.head_dim)
+        _dims(pk, "prefix_k", want)
+        _dims(pv, "prefix_v", want)
+        if p_off < 0 or p_off + T_prefix > want[1]:
+            raise ValueError(f"prefix: rows {p_off} .. {p_off + T_prefix - 1} exceed t_cap {want[1]}")
     if T_own > 0:
-        if k is None or v is None:
-            raise ValueError(f"{own_name}: k and v are required")
-        _kv_extent(k, v, own_name, B, shape, T_own, own_t_off)
+        k, v = own
+        t_cap = _own_dims(k, v, own_name, B, shape, T_own, own_t_off)
     if weight is not None:
         if T_own < 1:
             raise ValueError("weights need own rows")
-        _extent(weight, "weight", (B, shape.n_kv_heads, k.shape[2]))
-    _extent(own_len, len_name, (B,))
-    _extent(n_new, "n_new", (B,))
-    if not T_prefix > 0:
-        pk = pv = None
-    if not T_own > 0:
-        k = v = None
-    dev = _one_device(q=q, out=out, prefix_k=pk, prefix_v=pv, k=k, v=v, weight=weight, ws=ws,
-                      **{len_name: own_len, "n_new": n_new})
-    own_view = _view(k, v, own_t_off, own_name, dt)
-    view = None if pk is None else KvView(_ptr(pk, "prefix_k", dt), _ptr(pv, "prefix_v", dt), pk.shape[1], p_off)
-    wp, wb = _ws(ws)
-    own_ref = ctypes.byref(own_view) if own_view is not None else None
-    head = [ctypes.byref(shape.c()), _ptr(q, "q", dt), N]
+        _dims(weight, "weight", (B, shape.n_kv_heads, t_cap))
+    if own_len is not None:
+        _dims(own_len, len_name, (B,))
+    if n_new is not None:
+        _dims(n_new, "n_new", (B,))
+    if not isinstance(ws, torch.Tensor):
+        raise ValueError("ws must be a torch tensor")
+    dt, dev, i32 = shape.torch_dtype, _device_of(q, "q"), torch.int32
+    args = [ctypes.byref(shape.c()), _dev_ptr(q, "q", dt, dev), N]
     if fn is lib.kvd_prefix_attn:
-        head += [ctypes.byref(view) if view is not None else None, T_prefix]
-    args = head + [own_ref, _per_seq(own_len, len_name, B), _per_seq(n_new, "n_new", B), B, T_own,
-                   _ptr(out, "out", dt), _ptr(weight, "weight", torch.float32), decay, wp, wb]
-    with torch.cuda.device(dev):
-        _check(fn(*args, _stream()))
+        args.append(None if pk is None else ctypes.byref(
+            KvView(_dev_ptr(pk, "prefix_k", dt, dev), _dev_ptr(pv, "prefix_v", dt, dev), pk.shape[1], p_off)))
+        args.append(T_prefix)
+    args.append(None if k is None else ctypes.byref(
+        KvView(_dev_ptr(k, own_name + "_k", dt, dev), _dev_ptr(v, own_name + "_v", dt, dev), t_cap, own_t_off)))
+    _run_on(dev, fn, *args, _dev_ptr(own_len, len_name, i32, dev), _dev_ptr(n_new, "n_new", i32, dev), B, T_own,
+            _dev_ptr(out, "out", dt, dev), _dev_ptr(weight, "weight", torch.float32, dev), decay,
+            _dev_ptr(ws, "ws", ws.dtype, dev), ws.nbytes)
 
 
 def kvd_prefix_attn(shape: Shape, q, prefix_k, prefix_v, T_prefix: int, own_k, own_v, T_own: int, out, ws,
@@ -599,30 +624,31 @@ def kvd_evict(shape: Shape, k, v, T: int, keep: int, weight, ws, pos=None, last_
     (sequence, KV head) of k / v [B, n_kv, t_cap, hd]: rows with pos < sink or pos > last_pos[b] - recent first,
     then by weight [B, n_kv, t_cap] fp32.  Rows that stay behind slot `keep` move into the freed slots, with
     their weight and pos [B, n_kv, t_cap] int32."""
-    dt = shape.torch_dtype
     if not isinstance(k, torch.Tensor) or k.dim() != 4:
         raise ValueError("kv: k and v must both be [B, n_kv, t_cap, head_dim] tensors")
     B = k.shape[0]
-    _kv_extent(k, v, "kv", B, shape, T, t_off)
-    per_row = (B, shape.n_kv_heads, k.shape[2])
+    t_cap = _own_dims(k, v, "kv", B, shape, T, t_off)
+    per_row = (B, shape.n_kv_heads, t_cap)
     if weight is None:
         raise ValueError("weight is required")
-    _extent(weight, "weight", per_row)
-    _extent(pos, "pos", per_row)
-    _extent(last_pos, "last_pos", (B,))
-    _extent(kv_len, "kv_len", (B,))
-    if pos is None and (sink > 0 or recent > 0):
+    _dims(weight, "weight", per_row)
+    if pos is not None:
+        _dims(pos, "pos", per_row)
+    elif sink > 0 or recent > 0:
         raise ValueError("pos is required when sink or recent is positive")
-    if last_pos is None and recent > 0:
+    if last_pos is not None:
+        _dims(last_pos, "last_pos", (B,))
+    elif recent > 0:
         raise ValueError("last_pos is required when recent is positive")
-    dev = _one_device(k=k, v=v, weight=weight, ws=ws, pos=pos, last_pos=last_pos, kv_len=kv_len)
-    view = _view(k, v, t_off, "kv", dt)
-    wp, wb = _ws(ws)
-    args = [ctypes.byref(shape.c()), ctypes.byref(view), _per_seq(kv_len, "kv_len", B), B, T, keep,
-            _ptr(weight, "weight", torch.float32), _ptr(pos, "pos", torch.int32), _per_seq(last_pos, "last_pos", B),
-            sink, recent, wp, wb]
-    with torch.cuda.device(dev):
-        _check(lib.kvd_evict(*args, _stream()))
+    if kv_len is not None:
+        _dims(kv_len, "kv_len", (B,))
+    if not isinstance(ws, torch.Tensor):
+        raise ValueError("ws must be a torch tensor")
+    dt, dev, i32 = shape.torch_dtype, _device_of(k, "k"), torch.int32
+    view = KvView(_dev_ptr(k, "kv_k", dt, dev), _dev_ptr(v, "kv_v", dt, dev), t_cap, t_off)
+    _run_on(dev, lib.kvd_evict, ctypes.byref(shape.c()), ctypes.byref(view), _dev_ptr(kv_len, "kv_len", i32, dev), B, T,
+            keep, _dev_ptr(weight, "weight", torch.float32, dev), _dev_ptr(pos, "pos", i32, dev),
+            _dev_ptr(last_pos, "last_pos", i32, dev), sink, recent, _dev_ptr(ws, "ws", ws.dtype, dev), ws.nbytes)
 
 
 def kvd_pack_matrix(w):
