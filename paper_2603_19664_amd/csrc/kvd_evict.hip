@@ -1,10 +1,12 @@
 // Eviction from a cache by accumulated attention weight (kvd_evict): every (sequence,
 // KV head) keeps its n' = min(len, keep) foremost rows.
 //
-//   evict_select_kernel  one workgroup per (b, j): the rows' ranks, the rank of the last
-//                        row kept (radix selection), and who moves where; weights and
-//                        positions are moved here.
-//   evict_move_kernel    the K and V rows.
+//   evict_one_kernel     keep = T - 1, a decode step's call: the lightest row of each
+//                        cache, and the move of its last one, in one launch.
+//   evict_select_kernel  otherwise, one workgroup per (b, j): the rows' ranks, the rank of
+//                        the last row kept, and who moves where; weights and positions
+//                        are moved here.
+//   evict_move_kernel    then the K and V rows.
 //
 // Kept rows in slots >= n' move into the freed slots < n', both in slot order: sources
 // and destinations are disjoint sets, so the copies need no order, and no fewer rows
@@ -30,18 +32,47 @@ __device__ __forceinline__ uint32_t rank_of(const EvictArgs& a, float w, int pos
   return x ^ ((x >> 31) != 0 ? 0xffffffffu : 0x80000000u);
 }
 
-// Number of lanes below this one whose predicate holds, and in the whole wave.
-__device__ __forceinline__ int lanes_below(unsigned long long m, int lane) {
-  return __popcll(m & ((1ull << lane) - 1));
+// Inclusive sum over the workgroup's threads of v, in thread order, and the total;
+// `buf` holds one word per wave.  Ends with a barrier.
+__device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* buf, uint32_t& total) {
+  const int lane = threadIdx.x & 63, w = wave_id();
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t x = __shfl_up(v, o, 64);
+    if (lane >= o) v += x;
+  }
+  if (lane == 63) buf[w] = v;
+  __syncthreads();
+  uint32_t before = 0;
+  total = 0;
+#pragma unroll
+  for (int i = 0; i < kNtEvict / 64; ++i) {
+    const uint32_t x = buf[i];
+    before += i < w ? x : 0u;
+    total += x;
+  }
+  __syncthreads();
+  return v + before;
 }
 
+constexpr int kEvictBins = 2 * kNtEvict;
+
+// The rank of the last row kept: each pass spreads the ranks that can still be it, [lo,
+// hi], over 2048 equal bins (a first pass over the ranks that occur, so that weights of
+// like size do not share a bin, whose counter they would take turns at; protected and
+// NaN rows are counted apart) and goes on with the bin that holds it.  At most three
+// passes.  Then rows are taken thread by thread in slot order: c consecutive slots each, c
+// odd (LDS banks), one prefix sum for the rows that tie with the last rank and one for
+// freed slots and movers.  KEYS: ranks that fit in LDS; 0: they stay in the workspace.
+// 8 x 2 caches of 8192 .. 16385 rows to 2048: 88 us with 8-bit digits of the whole rank and
+// serial bin walks.
+template <int KEYS>
 __global__ __launch_bounds__(kNtEvict) void evict_select_kernel(EvictArgs a) {
-  constexpr int NW = kNtEvict / 64;
-  __shared__ int hist[256];
-  __shared__ int wsum[2][NW];
-  __shared__ uint32_t s_prefix;
-  __shared__ int s_need;
-  const int tid = threadIdx.x, lane = tid & 63, w = wave_id();
+  __shared__ uint32_t lkeys[KEYS > 0 ? KEYS : 1];
+  __shared__ uint32_t hist[kEvictBins];
+  __shared__ uint32_t buf[kNtEvict / 64];
+  __shared__ uint32_t s_lo, s_hi, s_top, s_bin, s_need;
+  const int tid = threadIdx.x, lane = tid & 63;
   const int bj = blockIdx.x, b = bj / a.n_kv;
   const int n = a.len != nullptr ? min(max(a.len[b], 0), a.T) : a.T;
   const int left = min(n, a.keep);
@@ -51,83 +82,209 @@ __global__ __launch_bounds__(kNtEvict) void evict_select_kernel(EvictArgs a) {
   }
   float* wt = a.weight + (size_t)bj * a.t_cap + a.t_off;
   int32_t* ps = a.pos != nullptr ? a.pos + (size_t)bj * a.t_cap + a.t_off : nullptr;
-  uint32_t* keys = a.keys + (size_t)bj * a.T;
+  uint32_t* keys = KEYS > 0 ? lkeys : a.keys + (size_t)bj * a.T;
   const int newest = a.last_pos != nullptr ? a.last_pos[b] : 0;
-  for (int t = tid; t < n; t += kNtEvict) keys[t] = rank_of(a, wt[t], ps != nullptr ? ps[t] : 0, newest);
-  // the left-th largest rank, 8 bits at a time
   if (tid == 0) {
-    s_prefix = 0;
-    s_need = left;
+    s_lo = 0xffffffffu;
+    s_hi = 0u;
+    s_top = 0u;
   }
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    if (tid < 256) hist[tid] = 0;
-    __syncthreads();
-    const uint32_t prefix = s_prefix;
-    const uint32_t mask = shift == 24 ? 0u : 0xffffffffu << (shift + 8);
-    for (int t = tid; t < n; t += kNtEvict) {
-      const uint32_t k = keys[t];
-      if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & 255], 1);
+  __syncthreads();
+  uint32_t lo = 0xffffffffu, hi = 0u, top = 0u;
+  for (int t0 = tid; t0 < n; t0 += 4 * kNtEvict) {
+    float x[4];
+    int p[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = min(t0 + i * kNtEvict, n - 1);
+      x[i] = wt[t];
+      p[i] = ps != nullptr ? ps[t] : 0;
     }
-    __syncthreads();
-    if (tid == 0) {
-      int need = s_need, d = 255;
-      for (; d > 0 && hist[d] < need; --d) need -= hist[d];
-      s_need = need;
-      s_prefix = prefix | ((uint32_t)d << shift);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = t0 + i * kNtEvict;
+      if (t >= n) continue;
+      const uint32_t k = rank_of(a, x[i], p[i], newest);
+      keys[t] = k;
+      if (k == 0xffffffffu) {
+        ++top;
+      } else if (k != 0u) {
+        lo = min(lo, k);
+        hi = max(hi, k);
+      }
     }
-    __syncthreads();
   }
-  const uint32_t last = s_prefix;  // rank of the last row kept
-  const int ties = s_need;         // rows of that rank that stay: the lowest slots
-  // slots in order: freed ones below `left`, kept ones from there on
-  int eq0 = 0, holes = 0, movers = 0;
-  int2* mv = a.moves + (size_t)bj * a.max_moves;
-  for (int t0 = 0; t0 < n; t0 += kNtEvict) {
-    const int t = t0 + tid;
-    const uint32_t k = t < n ? keys[t] : 0u;
-    const bool eq = t < n && k == last;
-    const unsigned long long me = __ballot(eq);
-    __syncthreads();
-    if (lane == 0) wsum[0][w] = __popcll(me);
-    __syncthreads();
-    int before = eq0, total = 0;
-    for (int i = 0; i < NW; ++i) {
-      before += i < w ? wsum[0][i] : 0;
-      total += wsum[0][i];
-    }
-    before += lanes_below(me, lane);
-    eq0 += total;
-    const bool kept = t < n && (k > last || (eq && before < ties));
-    const bool hole = t < left && !kept, mover = t >= left && kept;
-    const unsigned long long mh = __ballot(hole), mm = __ballot(mover);
-    __syncthreads();
-    if (lane == 0) {
-      wsum[0][w] = __popcll(mh);
-      wsum[1][w] = __popcll(mm);
-    }
-    __syncthreads();
-    int hb = holes, mb = movers, ht = 0, mt = 0;
-    for (int i = 0; i < NW; ++i) {
-      hb += i < w ? wsum[0][i] : 0;
-      mb += i < w ? wsum[1][i] : 0;
-      ht += wsum[0][i];
-      mt += wsum[1][i];
-    }
-    if (hole) mv[hb + lanes_below(mh, lane)].x = t;
-    if (mover) mv[mb + lanes_below(mm, lane)].y = t;
-    holes += ht;
-    movers += mt;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    lo = min(lo, (uint32_t)__shfl_xor(lo, o, 64));
+    hi = max(hi, (uint32_t)__shfl_xor(hi, o, 64));
+    top += __shfl_xor(top, o, 64);
+  }
+  if (lane == 0) {
+    atomicMin(&s_lo, lo);
+    atomicMax(&s_hi, hi);
+    atomicAdd(&s_top, top);
   }
   __threadfence_block();
   __syncthreads();
-  if (tid == 0) a.n_moves[bj] = movers;
-  for (int i = tid; i < movers; i += kNtEvict) {
-    const int2 m = mv[i];
-    wt[m.x] = wt[m.y];
-    if (ps != nullptr) ps[m.x] = ps[m.y];
+  lo = s_lo;
+  hi = s_hi;
+  uint32_t need = (uint32_t)left;  // rows still to be kept among those of rank <= hi
+  uint32_t last = 0u;              // rank of the last row kept
+  bool found = false;
+  if (need <= s_top) {
+    last = 0xffffffffu;
+    found = true;
+  } else {
+    need -= s_top;
+    if (lo > hi) found = true;  // nothing but NaN left
+  }
+  while (!found) {
+    // bin width 2^shift: the least that covers [lo, hi] with 2048 bins
+    const uint32_t range = hi - lo;
+    const int shift = range < (uint32_t)kEvictBins ? 0 : 21 - __clz(range);
+    for (int i = tid; i < kEvictBins; i += kNtEvict) hist[i] = 0u;
+    if (tid == 0) s_bin = 0xffffffffu;
+    __syncthreads();
+    for (int t = tid; t < n; t += kNtEvict) {
+      const uint32_t k = keys[t];
+      if (k >= lo && k <= hi) atomicAdd(&hist[(k - lo) >> shift], 1u);
+    }
+    __syncthreads();
+    // thread i takes the i-th pair of bins from the top
+    const uint32_t h1 = hist[kEvictBins - 1 - 2 * tid], h0 = hist[kEvictBins - 2 - 2 * tid];
+    uint32_t total;
+    const uint32_t upto = block_scan(h0 + h1, buf, total);
+    const uint32_t before = upto - h0 - h1;
+    if (before < need && need <= upto) {
+      const bool first = need <= before + h1;
+      s_bin = kEvictBins - 1 - 2 * tid - (first ? 0 : 1);
+      s_need = need - before - (first ? 0u : h1);
+    }
+    __syncthreads();
+    if (s_bin == 0xffffffffu) {  // every number stays, and some NaN
+      need -= total;
+      found = true;
+    } else {
+      need = s_need;
+      lo += s_bin << shift;
+      hi = lo + ((1u << shift) - 1u);
+      if (shift == 0) {
+        last = lo;
+        found = true;
+      }
+    }
+    __syncthreads();
+  }
+  const uint32_t ties = need;  // rows of rank `last` that stay: the lowest slots
+  const int c = ((n + kNtEvict - 1) / kNtEvict) | 1;
+  const int t0 = (int)min((long long)tid * c, (long long)n), t1 = min(t0 + c, n);
+  uint32_t eq = 0, total;
+  for (int t = t0; t < t1; ++t) eq += keys[t] == last ? 1u : 0u;
+  const uint32_t eq0 = block_scan(eq, buf, total) - eq;
+  uint32_t holes = 0, movers = 0, e = eq0;
+  for (int t = t0; t < t1; ++t) {
+    const uint32_t k = keys[t];
+    const bool kept = k > last || (k == last && e++ < ties);
+    holes += !kept && t < left ? 1u : 0u;
+    movers += kept && t >= left ? 1u : 0u;
+  }
+  uint32_t n_holes, n_movers;
+  uint32_t h = block_scan(holes, buf, n_holes) - holes;
+  uint32_t m = block_scan(movers, buf, n_movers) - movers;
+  int2* mv = a.moves + (size_t)bj * a.max_moves;
+  e = eq0;
+  for (int t = t0; t < t1; ++t) {
+    const uint32_t k = keys[t];
+    const bool kept = k > last || (k == last && e++ < ties);
+    if (!kept && t < left) mv[h++].x = t;
+    if (kept && t >= left) mv[m++].y = t;
+  }
+  __threadfence_block();
+  __syncthreads();
+  if (tid == 0) a.n_moves[bj] = (int)n_movers;
+  for (int i = tid; i < (int)n_movers; i += kNtEvict) {
+    const int2 d = mv[i];
+    wt[d.x] = wt[d.y];
+    if (ps != nullptr) ps[d.x] = ps[d.y];
   }
   __syncthreads();
   for (int t = left + tid; t < n; t += kNtEvict) wt[t] = 0.0f;
+}
+
+// keep = T - 1: a cache of T rows loses its lightest one (of equal ones the highest slot),
+// and row T - 1 takes its place.  A workgroup takes `heads` caches of one sequence, 16 /
+// heads waves each: all of a sequence's where its length has to be set (nothing may read it
+// after that), one otherwise.
+__global__ __launch_bounds__(kNtEvict) void evict_one_kernel(EvictArgs a, int heads) {
+  constexpr int NW = kNtEvict / 64;
+  __shared__ unsigned long long best[NW];
+  const int lane = threadIdx.x & 63, w = wave_id();
+  const int wph = heads >= NW ? 1 : NW / heads;  // waves per head
+  const int groups = a.n_kv / heads;
+  const int b = (int)blockIdx.x / groups, j0 = ((int)blockIdx.x - b * groups) * heads;
+  const int n = a.len != nullptr ? min(max(a.len[b], 0), a.T) : a.T;
+  const int newest = a.last_pos != nullptr ? a.last_pos[b] : 0;
+  if (n < a.T) {  // this sequence keeps all of its rows
+    if (a.len != nullptr && threadIdx.x == 0) a.len[b] = n;
+    return;
+  }
+  const int hw = w / wph, part = w - hw * wph;
+  for (int h0 = 0; h0 < heads; h0 += NW / wph) {
+    const bool on = hw < NW / wph && h0 + hw < heads;
+    const size_t row0 = ((size_t)b * a.n_kv + j0 + h0 + hw) * a.t_cap + a.t_off;
+    // the least rank, of equal ones the highest slot
+    unsigned long long least = ~0ull;
+    if (on) {
+      const float* wt = a.weight + row0;
+      const int32_t* ps = a.pos != nullptr ? a.pos + row0 : nullptr;
+      for (int t0 = part * 64 + lane; t0 < n; t0 += 8 * 64 * wph) {
+        float x[8];
+        int p[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int t = min(t0 + i * 64 * wph, n - 1);
+          x[i] = wt[t];
+          p[i] = ps != nullptr ? ps[t] : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int t = min(t0 + i * 64 * wph, n - 1);  // the last row again: the same candidate
+          const unsigned long long k =
+              ((unsigned long long)rank_of(a, x[i], p[i], newest) << 32) | (0xffffffffu - (uint32_t)t);
+          least = k < least ? k : least;
+        }
+      }
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+      const unsigned long long x = __shfl_xor(least, o, 64);
+      least = x < least ? x : least;
+    }
+    __syncthreads();
+    if (lane == 0) best[w] = least;
+    __syncthreads();
+    if (on && part == 0) {
+      for (int i = 1; i < wph; ++i) least = best[w + i] < least ? best[w + i] : least;
+      const int gone = (int)(0xffffffffu - (uint32_t)least), from = n - 1;
+      const int cpr = a.row_bytes / 16;
+      if (gone != from) {
+        uint4* k = reinterpret_cast<uint4*>(a.k) + row0 * cpr;
+        uint4* v = reinterpret_cast<uint4*>(a.v) + row0 * cpr;
+        if (lane < cpr) {
+          const uint4 x = k[(size_t)from * cpr + lane], y = v[(size_t)from * cpr + lane];
+          k[(size_t)gone * cpr + lane] = x;
+          v[(size_t)gone * cpr + lane] = y;
+        }
+        if (lane == 0) {
+          a.weight[row0 + gone] = a.weight[row0 + from];
+          if (a.pos != nullptr) a.pos[row0 + gone] = a.pos[row0 + from];
+        }
+      }
+      if (lane == 0) a.weight[row0 + from] = 0.0f;
+    }
+  }
+  if (a.len != nullptr && threadIdx.x == 0) a.len[b] = a.keep;
 }
 
 // `parts` workgroups per (b, j) copy its moves, 16 bytes per lane.  Also the lengths.
@@ -153,7 +310,17 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, int parts)
 
 hipError_t launch_evict(const EvictArgs& a, hipStream_t st) {
   const int bjs = a.B * a.n_kv;
-  hipLaunchKernelGGL(evict_select_kernel, dim3(bjs), dim3(kNtEvict), 0, st, a);
+  if (a.keep == a.T - 1) {
+    const int heads = a.len != nullptr ? a.n_kv : 1;
+    hipLaunchKernelGGL(evict_one_kernel, dim3(bjs / heads), dim3(kNtEvict), 0, st, a, heads);
+    return hipGetLastError();
+  }
+  if (a.T <= 8192)
+    hipLaunchKernelGGL(evict_select_kernel<8192>, dim3(bjs), dim3(kNtEvict), 0, st, a);
+  else if (a.T <= 32768)
+    hipLaunchKernelGGL(evict_select_kernel<32768>, dim3(bjs), dim3(kNtEvict), 0, st, a);
+  else
+    hipLaunchKernelGGL(evict_select_kernel<0>, dim3(bjs), dim3(kNtEvict), 0, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const long long work = (long long)a.max_moves * (a.row_bytes / 16);
