@@ -880,11 +880,20 @@ struct RowsPlan {
   long long items;                      // workgroups of the largest launch
 };
 
-// Slots of a key range that `units` workgroups share: about kRowsTargetWgs workgroups, each
-// of at least `least` keys, at most `most` slots.  Grows with keys only.
+// Slots of a key range that `units` items share, each of at least `least` keys and at most
+// `most`: the count with the shortest rounds of kRowsTargetWgs workgroups, a slot's fixed
+// cost (first loads, state written and merged) taken as kRowsSlotKeys keys of a nominal
+// 4096.  Grows with keys only (the candidates grow, their order does not change).
 int32_t row_slots(long long units, long long keys, int32_t least, int32_t most) {
-  const long long want = std::max(1ll, (kvd::kRowsTargetWgs + units - 1) / units);
-  return (int32_t)std::max(1ll, std::min({want, (keys + least - 1) / least, (long long)most}));
+  const long long top = std::max(1ll, std::min<long long>((keys + least - 1) / least, most));
+  int32_t best = 1;
+  double best_cost = 0;
+  for (int32_t S = 1; S <= top; ++S) {
+    const double rounds = (double)((units * S + kvd::kRowsTargetWgs - 1) / kvd::kRowsTargetWgs);
+    const double cost = rounds * (4096.0 / S + kvd::kRowsSlotKeys);
+    if (S == 1 || cost < best_cost) best = S, best_cost = cost;
+  }
+  return best;
 }
 int32_t slot_keys(long long keys, int32_t slots) {
   return (int32_t)((((keys + slots - 1) / slots) + 63) / 64 * 64);

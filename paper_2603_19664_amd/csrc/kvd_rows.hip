@@ -282,31 +282,35 @@ __global__ __launch_bounds__(64 * kSaWaves) __attribute__((amdgpu_waves_per_eu(2
 // Keys per LDS tile: 32 KiB of K and V.
 constexpr int rows_kt(int hd) { return hd == 256 ? 32 : 64; }
 
+// LDS tiles hold rows of HD elements with their 16-byte chunks permuted, row r's chunk c at
+// chunk c ^ swz(r), so that every read touches all 64 banks evenly.  The score operand is
+// one chunk of 32 rows, 16 rows at a time: swz = r % 16 (two 128-byte rows of head_dim 64
+// fill the banks: r / 2 % 8).  The transposing V reads take 64 bytes of 4 rows: swz = 4 (r %
+// 4) (head_dim 64: 4 (r / 2 % 2)).  (With 8 rows, or 32 bytes of 4, half of the cycles were
+// conflicts.)
+template <int HD>
+__device__ __forceinline__ int score_swz(int r) { return HD == 64 ? (r >> 1) & 7 : r & 15; }
+template <int HD>
+__device__ __forceinline__ int v_swz(int r) { return HD == 64 ? 4 * ((r >> 1) & 1) : 4 * (r & 3); }
+
 // Copies KT rows of HD elements from global memory straight into the LDS tile dst (rows
-// past n - 1 repeat row n - 1).  Row r's 16-byte chunk c lies at chunk c ^ swz(r) of its
-// LDS row: for the score operands (SCORE), whose lanes read one chunk of 32 rows, swz =
-// r % 8; for V, whose transposing reads take 64 bytes of 4 rows, swz = 2 (r % 4).  Both
-// then touch every bank evenly.  Thread tid copies chunk tid % CPR of rows tid / CPR +
-// 8192 / (4 HD) i, so that swz does not depend on i and a full tile needs no address
-// arithmetic: one offset per thread, the tile in the buffer resource, 4096 i as a scalar.
+// past n - 1 repeat row n - 1).  Thread tid copies chunk tid % CPR of rows r0 + RPI i, r0 =
+// tid / CPR: a full tile takes its rows' offsets from the thread once, 4096 i as a scalar.
 template <int HD, int KT, bool SCORE>
 __device__ __forceinline__ void copy_tile(const uint16_t* src, int n, uint16_t* dst) {
   constexpr int CPR = HD / 8, RPI = 256 / CPR, CH = KT / RPI;
   const int tid = threadIdx.x, w = wave_id();
-  const int r0 = tid / CPR;
-  const int col = 16 * ((tid % CPR) ^ (SCORE ? r0 & 7 : 2 * (r0 & 3)));
+  const int r0 = tid / CPR, ch = tid % CPR;
   const __amdgpu_buffer_rsrc_t res =
       __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(src), (short)0, KT * HD * 2, 0x00027000);
-  if (n >= KT) {
+  const bool full = n >= KT;
 #pragma unroll
-    for (int i = 0; i < CH; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (__attribute__((address_space(3))) void*)(dst + 512 * w + 2048 * i),
-                                               16, r0 * HD * 2 + col, 4096 * i, 0, 0);
-  } else {
-#pragma unroll
-    for (int i = 0; i < CH; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (__attribute__((address_space(3))) void*)(dst + 512 * w + 2048 * i),
-                                               16, min(r0 + RPI * i, n - 1) * HD * 2 + col, 0, 0, 0);
+  for (int i = 0; i < CH; ++i) {
+    const int r = r0 + RPI * i;
+    const int col = 16 * (ch ^ (SCORE ? score_swz<HD>(r) : v_swz<HD>(r)));
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (__attribute__((address_space(3))) void*)(dst + 512 * w + 2048 * i), 16,
+                                             (full ? r0 * HD * 2 : min(r, n - 1) * HD * 2) + col, full ? 4096 * i : 0,
+                                             0, 0);
   }
 }
 
@@ -316,7 +320,7 @@ typedef short i16x4_t __attribute__((ext_vector_type(4)));
 // Score operand: row lane % 32, elements 16 kk + 8 (lane / 32) ..; 32 rows on: + 64 HD.
 template <int HD>
 __device__ __forceinline__ uint32_t score_base(int lane) {
-  return (lane & 31) * HD * 2 + (((lane >> 5) ^ (lane & 7)) << 4);
+  return (lane & 31) * HD * 2 + (((lane >> 5) ^ score_swz<HD>(lane & 31)) << 4);
 }
 __device__ __forceinline__ bf16x8_t score_operand(const uint16_t* tile, uint32_t base, int kk, int rows) {
   return *reinterpret_cast<const bf16x8_t*>(reinterpret_cast<const char*>(tile) + (base ^ (kk << 5)) + rows);
@@ -327,8 +331,8 @@ __device__ __forceinline__ bf16x8_t score_operand(const uint16_t* tile, uint32_t
 // the ones whose scores it holds.
 template <int HD>
 __device__ __forceinline__ uint32_t v_base(int lane) {
-  return (4 * (lane >> 5) + ((lane & 15) >> 2)) * HD * 2 +
-         (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ (2 * ((lane >> 2) & 3))) << 4) + 8 * (lane & 1);
+  const int row = 4 * (lane >> 5) + ((lane & 15) >> 2);
+  return row * HD * 2 + (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ v_swz<HD>(row)) << 4) + 8 * (lane & 1);
 }
 template <int HD>
 __device__ __forceinline__ bf16x8_t v_operand(const uint16_t* vs, uint32_t base, int k0, int db) {
@@ -364,7 +368,9 @@ __device__ __forceinline__ float poison_of(float codes) {
 template <int HD>
 __global__ __launch_bounds__(256, 2) void rows_tile_kernel(RowsArgs a) {
   constexpr int KT = rows_kt(HD), KH = KT / 32, KS = HD / 16, DB = HD / 32;
-  __shared__ __align__(16) uint16_t lds[2][2][KT * HD];
+  // Four objects, each access naming one: a copy in flight into one buffer is then known
+  // not to touch the other (of one array, every LDS read waited for all copies: 20% slower).
+  __shared__ __align__(1024) uint16_t k_a[KT * HD], v_a[KT * HD], k_b[KT * HD], v_b[KT * HD];
   const int lane = threadIdx.x & 63, w = wave_id(), hl = lane >> 5;
   // the item: own (or joint) row blocks first, then the prefix's
   const int nbo = (a.R + kRowsTile - 1) / kRowsTile;
@@ -432,9 +438,7 @@ __global__ __launch_bounds__(256, 2) void rows_tile_kernel(RowsArgs a) {
   float m_run, l_run;  // in units of the scaled score
 
   const uint32_t kbase = score_base<HD>(lane), vbase = v_base<HD>(lane);
-  auto load = [&](int t) {
-    uint16_t* ks = lds[t & 1][0];
-    uint16_t* vs = lds[t & 1][1];
+  auto load = [&](int t, uint16_t* ks, uint16_t* vs) {
     const int k = (t < np ? t : t - np) * KT, n = (t < np ? kp.n : ko.n) - k;
     copy_tile<HD, KT, true>((t < np ? Kp : Ko) + (size_t)k * HD, n, ks);
     copy_tile<HD, KT, false>((t < np ? Vp : Vo) + (size_t)k * HD, n, vs);
@@ -450,28 +454,26 @@ again:
   m_run = -INFINITY;
   l_run = 0.0f;
   bool odd = false;
-  if (nt > 0) load(0);
-  for (int t = 0; t < nt; ++t) {
+  auto step = [&](int t, uint16_t* ks, uint16_t* vs, uint16_t* ks_next, uint16_t* vs_next) {
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's share of tile t is in LDS
     __syncthreads();                     // every wave's share, and tile t - 1 is no longer read
-    if (t + 1 < nt) load(t + 1);
-    const uint16_t* ks = lds[t & 1][0];
-    const uint16_t* vs = lds[t & 1][1];
+    if (t + 1 < nt) load(t + 1, ks_next, vs_next);
     if (pass == 1) {
       for (int i = threadIdx.x; i < KT * HD / 2; i += 256) {
-        uint32_t* x = reinterpret_cast<uint32_t*>(lds[t & 1][1]) + i;
+        uint32_t* x = reinterpret_cast<uint32_t*>(vs) + i;
         const uint32_t nf = nonfinite2(*x);
         if (nf != 0) *x &= (nf & 0x8000u ? 0u : 0xffffu) | (nf & 0x80000000u ? 0u : 0xffff0000u);
       }
       __syncthreads();
     }
-    if (!wave_on) continue;
+    if (!wave_on) return;
     const bool is_own = t >= np;
     const int k0 = (is_own ? t - np : t) * KT;
     const int row_lim = is_own ? lim : kp.n;
     const bool masked = k0 + KT > (is_own ? all : kp.n);
 
     f32x16_t st[KH];
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int kh = 0; kh < KH; ++kh)
 #pragma unroll
@@ -484,17 +486,22 @@ again:
         st[kh] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[kk], st[kh], 0, 0, 0);
       }
     }
+    __builtin_amdgcn_s_setprio(0);
+    if (masked) {
+      asm volatile("");  // a branch: as selects they ran for every tile (a third of its VALU work)
+#pragma unroll
+      for (int kh = 0; kh < KH; ++kh)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = k0 + 32 * kh + 8 * (r >> 2) + 4 * hl + (r & 3);
+          st[kh][r] = key < row_lim ? st[kh][r] : -INFINITY;
+        }
+    }
     float mx = -INFINITY;
 #pragma unroll
     for (int kh = 0; kh < KH; ++kh)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        if (masked) {
-          const int key = k0 + 32 * kh + 8 * (r >> 2) + 4 * hl + (r & 3);
-          st[kh][r] = key < row_lim ? st[kh][r] : -INFINITY;
-        }
-        mx = fmaxf(mx, st[kh][r]);
-      }
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, st[kh][r]);
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * ScoreScale<HD>::v;
     const bool grow = mx > m_run + 8.0f;
     if (__any(grow)) {
@@ -538,6 +545,11 @@ again:
       }
       odd |= __any(nf != 0);
     }
+  };
+  if (nt > 0) load(0, k_a, v_a);
+  for (int t = 0; t < nt; t += 2) {
+    step(t, k_a, v_a, k_b, v_b);
+    if (t + 1 < nt) step(t + 1, k_b, v_b, k_a, v_a);
   }
   if (pass == 0 && __syncthreads_or(odd)) {
     pass = 1;
@@ -900,7 +912,7 @@ constexpr int kWtKeys = 128, kWtRows = 64;
 template <int HD>
 __global__ __launch_bounds__(256, 2) void weight_tile_kernel(RowsArgs a) {
   constexpr int KS = HD / 16, CPR = HD / 8, CH = kWtRows * CPR / 256;
-  __shared__ __align__(16) uint16_t lds[2][kWtRows * HD];
+  __shared__ __align__(1024) uint16_t q_a[kWtRows * HD], q_b[kWtRows * HD];  // two objects: see rows_tile_kernel
   const int tid = threadIdx.x, lane = tid & 63, w = wave_id(), hl = lane >> 5;
   const int units = a.B * a.n_kv, x = (int)blockIdx.x / units, u = (int)blockIdx.x - x * units;
   const int j = u % a.n_kv, b = u / a.n_kv;
@@ -923,22 +935,21 @@ __global__ __launch_bounds__(256, 2) void weight_tile_kernel(RowsArgs a) {
   const int fr0 = b * a.R;
   const uint32_t qbase = score_base<HD>(lane);
   const int nt = rs.r1 > rs.r0 ? (rs.r1 - rs.r0 + kWtRows - 1) / kWtRows : 0;
-  auto load = [&](int t) {
+  auto load = [&](int t, uint16_t* dst) {
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
       const int cc = tid + 256 * i, row = cc / CPR, ch = cc - row * CPR;
       const int fr = fr0 + min(rs.r0 + t * kWtRows + row, rs.r1 - 1);
       __builtin_amdgcn_global_load_lds(
           (const __attribute__((address_space(1))) void*)(static_cast<const uint16_t*>(a.q) + q_off(a, j, fr, HD) +
-                                                           8 * (ch ^ (row & 7))),
-          (__attribute__((address_space(3))) void*)(lds[t & 1] + 8 * (64 * w + 256 * i)), 16, 0, 0);
+                                                           8 * (ch ^ score_swz<HD>(row))),
+          (__attribute__((address_space(3))) void*)(dst + 8 * (64 * w + 256 * i)), 16, 0, 0);
     }
   };
-  if (nt > 0) load(0);
-  for (int t = 0; t < nt; ++t) {
+  auto step = [&](int t, const uint16_t* qs, uint16_t* next) {
     __builtin_amdgcn_s_waitcnt(0x0f70);
     __syncthreads();
-    if (t + 1 < nt) load(t + 1);
+    if (t + 1 < nt) load(t + 1, next);
 #pragma unroll
     for (int h = 0; h < kWtRows / 32; ++h) {
       const int row = 32 * h + (lane & 31), r = rs.r0 + t * kWtRows + row;
@@ -949,7 +960,7 @@ __global__ __launch_bounds__(256, 2) void weight_tile_kernel(RowsArgs a) {
       const int lim = r < rs.r1 ? rows_seen(sq, r / a.g) - k0 - 32 * w : 0;  // keys of the wave that the row sees
 #pragma unroll
       for (int i = 0; i < KS; ++i) {
-        const bf16x8_t qf = score_operand(lds[t & 1], qbase, i, 64 * HD * h);
+        const bf16x8_t qf = score_operand(qs, qbase, i, 64 * HD * h);
         st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf, st, 0, 0, 0);
       }
 #pragma unroll
@@ -959,6 +970,11 @@ __global__ __launch_bounds__(256, 2) void weight_tile_kernel(RowsArgs a) {
         sum[i] += key < lim ? p : 0.0f;
       }
     }
+  };
+  if (nt > 0) load(0, q_a);
+  for (int t = 0; t < nt; t += 2) {
+    step(t, q_a, q_b);
+    if (t + 1 < nt) step(t + 1, q_b, q_a);
   }
 #pragma unroll
   for (int i = 0; i < 16; ++i) {
