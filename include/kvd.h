@@ -15,7 +15,8 @@
  * Conventions shared by every call
  * --------------------------------
  * Memory.   Every tensor pointer is a DEVICE pointer, owned by the caller and
- *           aligned to 16 bytes.  The library never allocates, frees or
+ *           aligned to 16 bytes (int32 arrays and kvd_prefix_attn's, kvd_weighted_attn's
+ *           and kvd_evict's weight: to 4).  The library never allocates, frees or
  *           synchronises: each call validates its arguments on the host,
  *           enqueues its kernels on `stream` (a hipStream_t; NULL means the
  *           null stream) and returns.  Outputs must not alias inputs.

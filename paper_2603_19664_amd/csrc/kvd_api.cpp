@@ -64,6 +64,13 @@ kvd_status check_ptr(const void* p, const char* name) {
   return KVD_OK;
 }
 
+// fp32 and int32 arrays that the kernels take one element at a time.
+kvd_status check_ptr4(const void* p, const char* name) {
+  if (p == nullptr) return fail(KVD_ERR_NULL, "%s is NULL", name);
+  if ((reinterpret_cast<uintptr_t>(p) & 3u) != 0) return fail(KVD_ERR_ALIGN, "%s is not 4-byte aligned", name);
+  return KVD_OK;
+}
+
 // gamma is read unless the weights have it folded in (KVD_W_PACKED_GAMMA).
 kvd_status check_gamma(const kvd_attn_shape* s, const void* gamma) {
   return s->w_layout == KVD_W_PACKED_GAMMA ? KVD_OK : check_ptr(gamma, "gamma");
@@ -870,12 +877,12 @@ namespace {
 
 // Launch geometry and workspace of a kvd_prefix_attn / kvd_weighted_attn call.
 //
-// bf16 rows go to the streaming kernel while one MFMA column block (16) holds them,
-// else to 128-row tiles; fp32 to waves of 16 rows.  A sequence whose own rows fill half
+// bf16 rows stream their keys while one MFMA column block (16) holds them, else share
+// 128-row tiles; fp32 to waves of 16 rows.  A sequence whose own rows fill half
 // a block takes prefix and own keys in one pass (joint): the prefix is then shared by
 // its own rows, and neither half leaves a partial state.
 struct RowsPlan {
-  int32_t R, joint, prefix_stream, own_stream, S_prefix, C_prefix, S_own, C_own, S_w, sc_ld;
+  int32_t R, joint, prefix_few, own_few, S_prefix, C_prefix, S_own, C_own, S_w, sc_ld;
   size_t ml, acc, lse, sc, wpart, end;  // byte offsets in the workspace
   long long items;                      // workgroups of the largest launch
 };
@@ -917,18 +924,18 @@ bool rows_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T_prefix, 
     p->items = units * nbo * p->S_own;
   } else {
     if (T_prefix > 0) {
-      p->prefix_stream = bf && Rt <= kvd::kRowsStream;
-      const long long u = p->prefix_stream ? s->n_kv_heads : s->n_kv_heads * nbp;
-      p->S_prefix = row_slots(u, T_prefix, p->prefix_stream ? kvd::kSaBlock : kvd::kRowsLeastKeys,
-                              p->prefix_stream ? kvd::kSaMaxSplits : kvd::kRowsMostSlots);
+      p->prefix_few = bf && Rt <= kvd::kRowsFew;
+      const long long u = p->prefix_few ? s->n_kv_heads : s->n_kv_heads * nbp;
+      p->S_prefix = row_slots(u, T_prefix, p->prefix_few ? kvd::kSaBlock : kvd::kRowsLeastKeys,
+                              p->prefix_few ? kvd::kSaMaxSplits : kvd::kRowsMostSlots);
       p->C_prefix = slot_keys(T_prefix, p->S_prefix);
       p->items += u * p->S_prefix;
     }
     if (T_own > 0) {
-      p->own_stream = bf && R <= kvd::kRowsStream;
-      const long long u = p->own_stream ? units : units * nbo;
-      p->S_own = row_slots(u, T_own, p->own_stream ? kvd::kSaBlock : kvd::kRowsLeastKeys,
-                           p->own_stream ? kvd::kSaMaxSplits : kvd::kRowsMostSlots);
+      p->own_few = bf && R <= kvd::kRowsFew;
+      const long long u = p->own_few ? units : units * nbo;
+      p->S_own = row_slots(u, T_own, p->own_few ? kvd::kSaBlock : kvd::kRowsLeastKeys,
+                           p->own_few ? kvd::kSaMaxSplits : kvd::kRowsMostSlots);
       p->C_own = slot_keys(T_own, p->S_own);
       p->items += u * p->S_own;
     }
@@ -943,7 +950,7 @@ bool rows_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T_prefix, 
   p->ml = take(8 * S * rows);
   p->acc = take(S > 1 ? 4 * S * rows * s->head_dim : 0);
   if (weights && T_own > 0) {
-    if (p->own_stream) {
+    if (p->own_few) {
       p->sc_ld = (T_own + 15) / 16 * 16;
       p->sc = take(4 * (size_t)units * R * p->sc_ld);
       p->items = std::max(p->items, (long long)rows + units * ((T_own + 255) / 256));
@@ -979,7 +986,9 @@ kvd_status rows_call(const kvd_attn_shape* shape, const void* q, int32_t N, cons
   KVD_TRY(check_ptr(out, "out"));
   if (T_prefix > 0) KVD_TRY(check_view(prefix, T_prefix, "prefix"));
   if (T_own > 0) KVD_TRY(check_view(own, T_own, own_name));
-  if (weight != nullptr) KVD_TRY(check_ptr(weight, "weight"));
+  if (weight != nullptr) KVD_TRY(check_ptr4(weight, "weight"));
+  if (own_len != nullptr) KVD_TRY(check_ptr4(own_len, "the lengths"));
+  if (n_new != nullptr) KVD_TRY(check_ptr4(n_new, "n_new"));
   RowsPlan p;
   if (!rows_plan(shape, B, N, T_prefix, T_own, weight != nullptr, &p))
     return fail(KVD_ERR_SHAPE, "%s: B=%d N=%d T_prefix=%d T_own=%d is too large for one call", name, B, N, T_prefix,
@@ -1010,7 +1019,7 @@ kvd_status rows_call(const kvd_attn_shape* shape, const void* q, int32_t N, cons
   a.ml = reinterpret_cast<float*>(base + p.ml);
   a.acc = reinterpret_cast<float*>(base + p.acc);
   if (weight != nullptr) {
-    if (p.own_stream) {
+    if (p.own_few) {
       a.sc = reinterpret_cast<float*>(base + p.sc);
     } else {
       a.lse = reinterpret_cast<float*>(base + p.lse);
@@ -1032,8 +1041,8 @@ kvd_status rows_call(const kvd_attn_shape* shape, const void* q, int32_t N, cons
   a.S_w = p.S_w;
   a.sc_ld = p.sc_ld;
   a.joint = p.joint;
-  a.prefix_stream = p.prefix_stream;
-  a.own_stream = p.own_stream;
+  a.prefix_few = p.prefix_few;
+  a.own_few = p.own_few;
   return device_status(kvd::launch_rows(a, shape->dtype == KVD_BF16, shape->head_dim, (hipStream_t)stream), name);
 }
 
@@ -1089,9 +1098,11 @@ kvd_status kvd_evict(const kvd_attn_shape* shape, const kvd_kv_view* kv, int32_t
   if (sink < 0 || recent < 0) return fail(KVD_ERR_SHAPE, "sink=%d recent=%d must be >= 0", sink, recent);
   if (B == 0) return KVD_OK;
   KVD_TRY(check_view(kv, T, "kv"));
-  KVD_TRY(check_ptr(weight, "weight"));
-  if (pos != nullptr || sink > 0 || recent > 0) KVD_TRY(check_ptr(pos, "pos"));
+  KVD_TRY(check_ptr4(weight, "weight"));
+  if (pos != nullptr || sink > 0 || recent > 0) KVD_TRY(check_ptr4(pos, "pos"));
   if (recent > 0 && last_pos == nullptr) return fail(KVD_ERR_NULL, "last_pos is NULL (recent=%d)", recent);
+  if (kv_len != nullptr) KVD_TRY(check_ptr4(kv_len, "kv_len"));
+  if (last_pos != nullptr) KVD_TRY(check_ptr4(last_pos, "last_pos"));
   EvictPlan p;
   if (!evict_plan(shape, B, T, &p)) return fail(KVD_ERR_SHAPE, "kvd_evict: B=%d is too large for one call", B);
   if (ws == nullptr) return fail(KVD_ERR_WORKSPACE, "workspace is NULL (%zu bytes needed)", p.end);

@@ -203,8 +203,8 @@ hipError_t launch_prefill_attn(const PrefillArgs& a, int hd, hipStream_t st);
 // sequences share and up to T_own rows of their own.  Key ranges are slots of the
 // partial states: S_prefix of C_prefix keys of the prefix, S_own of C_own own keys; in a
 // joint call S_own ranges of C_own keys of both one after the other (S_prefix = 0).
-// With one slot the attention kernel writes out itself.  The streaming kernel (at most
-// 16 rows: prefix_stream, own_stream) cuts a range by its own length into equal slots.
+// With one slot the attention kernel writes out itself.  Ranges of at most 16 rows
+// (prefix_few, own_few; bf16) are cut by their own length into equal slots.
 struct RowsArgs {
   const void* q;
   const void* pk;
@@ -224,7 +224,7 @@ struct RowsArgs {
   int p_cap, p_off, T_prefix, t_cap, t_off, T_own;
   int B, N, n_q, n_kv, g, R;
   int S_prefix, C_prefix, S_own, C_own, S_w, sc_ld;
-  int joint, prefix_stream, own_stream;
+  int joint, prefix_few, own_few;
 };
 hipError_t launch_rows(const RowsArgs& a, int dtype_bf16, int hd, hipStream_t st);
 

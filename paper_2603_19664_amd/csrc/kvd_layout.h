@@ -392,7 +392,7 @@ constexpr SaLds sa_lds(int hd, int G) {
 // Several query rows over stored keys (kvd_rows.hip).
 constexpr int kRowsTile = 128;    // rows per workgroup of the tile kernel
 constexpr int kRowsWave = 16;     // rows per wave of the fp32 kernel
-constexpr int kRowsStream = 16;   // rows the streaming kernel takes (one MFMA column block)
+constexpr int kRowsFew = 16;      // rows rows_few takes (one MFMA column block)
 constexpr int kRowsTargetWgs = 512;
 constexpr int kRowsLeastKeys = 128;  // keys per slot of the tile and fp32 kernels, at least
 constexpr int kRowsSlotKeys = 256;   // a slot's fixed cost in keys

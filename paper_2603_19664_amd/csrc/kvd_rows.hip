@@ -2,11 +2,10 @@
 // kvd_prefix_attn (a prefix that the whole batch attends, then each sequence's own
 // rows) and kvd_weighted_attn (the weight every cached key received).
 //
-//   rows_stream_kernel  bf16, at most 16 rows per key range (single tokens): one
-//                       workgroup streams 16-key blocks, scores on MFMA, P V on the
-//                       vector ALUs in fp32.
-//   rows_tile_kernel    bf16, more rows: 128 rows per workgroup, key tiles in LDS,
-//                       scores and P V on MFMA.
+//   rows_bf16_kernel    bf16, one launch for both kinds of items: rows_few, at most 16
+//                       rows per key range (single tokens), whose waves stream 16-key
+//                       blocks each on its own; rows_tile, 128 rows per workgroup that
+//                       share key tiles in LDS.  Both products on MFMA.
 //   rows_f32_kernel     fp32: 16 rows per wave, both products on MFMA 16x16x4 f32.
 //   rows_finish_kernel  merges the key ranges' softmax states into out, and adds up
 //                       the streamed scores' weights.
@@ -68,213 +67,6 @@ __device__ __forceinline__ KeyRange prefix_range(const RowsArgs& a, int j, int k
 }
 __device__ __forceinline__ KeyRange own_range(const RowsArgs& a, int b, int j, int k0, int k1) {
   return KeyRange{((size_t)b * a.n_kv + j) * a.t_cap + a.t_off + k0, max(k1 - k0, 0)};
-}
-
-// ------------------------------------------------------------------ streaming, at most 16 rows (bf16)
-
-// One workgroup of kSaWaves waves per (unit, split): units 0 .. B n_kv - 1 are the
-// own rows of (b, j) in So splits, the rest the prefix of KV head j in Sp splits.
-// stream_attn_kernel's scheme (16-key blocks to waves in turn, the next block's rows
-// loading while this one is attended, scores S^T = K q^T on MFMA 16x16x32, one row
-// per column, P V in fp32 on the vector ALUs) with rows that see different numbers of
-// keys.  CAUSAL (N > 1): a masked key's value is skipped, not multiplied by zero (it
-// may be infinite or NaN).  With a.sc the scores of own keys are kept for the weights.
-template <int HD, int G, bool CAUSAL>
-__global__ __launch_bounds__(64 * kSaWaves) __attribute__((amdgpu_waves_per_eu(2))) void rows_stream_kernel(
-    RowsArgs a) {
-  __shared__ __align__(16) char lds[sa_lds(HD, G).end];
-  constexpr int NW = kSaWaves, NT = 64 * NW;
-  constexpr int NC = HD / 32;
-  constexpr int CPK = HD / 8;
-  constexpr int KPI = 64 / CPK;
-  constexpr SaLds SL = sa_lds(HD, G);
-  const int tid = threadIdx.x, lane = tid & 63, w = wave_id();
-  const int own_items = a.own_stream ? a.B * a.n_kv * a.S_own : 0;
-  const bool own = (int)blockIdx.x < own_items;
-  const int item = own ? (int)blockIdx.x : (int)blockIdx.x - own_items;
-  const int units = own ? a.B * a.n_kv : a.n_kv;
-  const int S = own ? a.S_own : a.S_prefix;
-  const int s = item / units, u = item - s * units;
-  const int j = u % a.n_kv, b = u / a.n_kv;
-  const int slot = own ? a.S_prefix + s : s;
-  const int nr = own ? a.R : a.B * a.R;
-  const int fr0 = own ? b * a.R : 0;
-  Seq sq{0, 0};
-  if (own) sq = seq_of(a, b);
-  if (own && sq.n == 0) return;  // no row of this sequence is asked for
-  const int T = own ? sq.len : a.T_prefix;
-  const int nblk_all = (T + kSaBlock - 1) / kSaBlock;
-  const int k0 = kSaBlock * sa_first_block(s, nblk_all, S);
-  const int nk = min(T, kSaBlock * sa_first_block(s + 1, nblk_all, S)) - k0;  // keys of this split
-  const int nblk = nk > 0 ? (nk + kSaBlock - 1) / kSaBlock : 0;
-  const int nb = nblk > w ? (nblk - 1 - w) / NW + 1 : 0;
-  const KeyRange kr = own ? own_range(a, b, j, k0, k0 + nk) : prefix_range(a, j, k0, k0 + nk);
-  const uint16_t* Kp = static_cast<const uint16_t*>(own ? a.k : a.pk) + kr.row * HD;
-  const uint16_t* Vp = static_cast<const uint16_t*>(own ? a.v : a.pv) + kr.row * HD;
-  const int hq = lane & 15;  // this lane's row
-  // keys of this split that the row sees
-  int lim = 0;
-  if (hq < nr) lim = own ? min(rows_seen(sq, hq / a.g) - k0, nk) : nk;
-
-  bf16x8_t qf[NC];
-  {
-    const uint16_t* qs =
-        static_cast<const uint16_t*>(a.q) + q_off(a, j, fr0 + min(hq, nr - 1), HD) + 8 * (lane >> 4);
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      u32x4_t v = *reinterpret_cast<const u32x4_t*>(qs + 32 * c);
-      if (hq >= nr) v = u32x4_t{0u, 0u, 0u, 0u};
-      qf[c] = __builtin_bit_cast(bf16x8_t, v);
-    }
-  }
-
-  auto load = [&](u32x4_t (&kv)[NC], u32x4_t (&vv)[NC], int i) {
-    const int kb = kSaBlock * (w + NW * min(i, nb - 1));
-    const uint16_t* kp = Kp + (size_t)min(kb + hq, nk - 1) * HD + 8 * (lane >> 4);
-#pragma unroll
-    for (int c = 0; c < NC; ++c) kv[c] = *reinterpret_cast<const u32x4_t*>(kp + 32 * c);
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-      vv[c] = *reinterpret_cast<const u32x4_t*>(Vp + (size_t)min(kb + KPI * c + lane / CPK, nk - 1) * HD +
-                                                8 * (lane % CPK));
-  };
-
-  float m_run = -INFINITY, l_run = 0.0f;
-  float acc[G][8];
-#pragma unroll
-  for (int h = 0; h < G; ++h)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc[h][e] = 0.0f;
-  float* Pw = reinterpret_cast<float*>(lds + SL.p) + w * (G + 1) * kSaBlock;  // [G][16] probabilities
-  float* Aw = Pw + G * kSaBlock;                                                // [G] rescale factors
-  float* sc_row = a.sc != nullptr && own && hq < nr
-                      ? a.sc + (((size_t)b * a.n_kv + j) * a.R + hq) * a.sc_ld + k0 + 4 * (lane >> 4)
-                      : nullptr;
-
-  auto attend = [&](const u32x4_t (&kv)[NC], const u32x4_t (&vv)[NC], int i) {
-    const int kb = kSaBlock * (w + NW * i);
-    f32x4_t sc = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-    for (int c = 0; c < NC; ++c)
-      sc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kv[c]), qf[c], sc, 0, 0, 0);
-    // sc[r]: key kb + 4 (lane / 16) + r, row hq
-    float sv[4], bm = -INFINITY;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      sv[r] = kb + 4 * (lane >> 4) + r < lim ? sc[r] * ScoreScale<HD>::v : -INFINITY;
-      bm = fmaxf(bm, sv[r]);
-    }
-    if (sc_row != nullptr && i < nb) *reinterpret_cast<float4*>(sc_row + kb) = make_float4(sv[0], sv[1], sv[2], sv[3]);
-    bm = fmaxf(bm, __shfl_xor(bm, 16, 64));
-    bm = fmaxf(bm, __shfl_xor(bm, 32, 64));
-    const float m_new = fmaxf(m_run, bm);
-    const float m_use = m_new == -INFINITY ? 0.0f : m_new;  // no key seen yet: weights 0
-    const float alpha = exp2_hw(m_run - m_use);
-    float p[4];
-#pragma unroll
-    for (int r = 0; r < 4; ++r) p[r] = exp2_hw(sv[r] - m_use);
-    l_run = fmaf(l_run, alpha, (p[0] + p[1]) + (p[2] + p[3]));
-    m_run = m_new;
-    if (hq < G) *reinterpret_cast<float4*>(Pw + hq * kSaBlock + 4 * (lane >> 4)) = make_float4(p[0], p[1], p[2], p[3]);
-    if (lane < G) Aw[lane] = alpha;
-    __builtin_amdgcn_wave_barrier();  // the wave's LDS writes are ordered before its reads below
-#pragma unroll
-    for (int h = 0; h < G; ++h) {
-      const float al = Aw[h];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc[h][e] *= al;
-    }
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const int kk = KPI * c + lane / CPK;
-      const bool in = kb + kk < nk;  // past the range: 0, so that a weight of 0 gives 0
-      const uint32_t vw[4] = {in ? vv[c].x : 0u, in ? vv[c].y : 0u, in ? vv[c].z : 0u, in ? vv[c].w : 0u};
-      float v8[8];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v8[2 * e] = bf_lo(vw[e]);
-        v8[2 * e + 1] = bf_hi(vw[e]);
-      }
-#pragma unroll
-      for (int h = 0; h < G; ++h) {
-        const float pr = Pw[h * kSaBlock + kk];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float x = fmaf(pr, v8[e], acc[h][e]);
-          acc[h][e] = !CAUSAL || pr != 0.0f ? x : acc[h][e];
-        }
-      }
-    }
-    __builtin_amdgcn_wave_barrier();  // reads of this block's slot before the next block's writes
-  };
-
-  // the pipeline of stream_attn_kernel: blocks in pairs, straight-line, each refill
-  // kept behind the last use of the registers that it overwrites
-  if (nb > 0) {
-    u32x4_t kr0[NC], vr0[NC], kr1[NC], vr1[NC];
-    load(kr0, vr0, 0);
-    for (int i = 0; i < nb; i += 2) {
-      __builtin_amdgcn_sched_barrier(0);
-      load(kr1, vr1, i + 1);
-      attend(kr0, vr0, i);
-      __builtin_amdgcn_sched_barrier(0);
-      load(kr0, vr0, i + 2);
-      attend(kr1, vr1, i + 1);
-    }
-  }
-
-  l_run += __shfl_xor(l_run, 16, 64);
-  l_run += __shfl_xor(l_run, 32, 64);
-#pragma unroll
-  for (int o = CPK; o < 64; o <<= 1)
-#pragma unroll
-    for (int h = 0; h < G; ++h)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc[h][e] += __shfl_xor(acc[h][e], o, 64);
-
-  float* ms = reinterpret_cast<float*>(lds + SL.ml);   // [NW][G][2]
-  float* as = reinterpret_cast<float*>(lds + SL.acc);  // [NW][G][HD]
-  if (lane < G) {
-    ms[(w * G + lane) * 2] = m_run;
-    ms[(w * G + lane) * 2 + 1] = l_run;
-  }
-  if (lane < CPK) {
-#pragma unroll
-    for (int h = 0; h < G; ++h) {
-      float* dst = as + ((size_t)w * G + h) * HD + 8 * lane;
-      *reinterpret_cast<float4*>(dst) = make_float4(acc[h][0], acc[h][1], acc[h][2], acc[h][3]);
-      *reinterpret_cast<float4*>(dst + 4) = make_float4(acc[h][4], acc[h][5], acc[h][6], acc[h][7]);
-    }
-  }
-  __syncthreads();
-
-  // merge of the waves in wave order: the slot's state, or with one slot the output
-  const bool direct = a.S_prefix + a.S_own == 1;
-  for (int i = tid; i < nr * HD; i += NT) {
-    const int h = i / HD, c = i - h * HD;
-    float M = -INFINITY;
-#pragma unroll
-    for (int v = 0; v < NW; ++v) M = fmaxf(M, ms[(v * G + h) * 2]);
-    const float Mu = M == -INFINITY ? 0.0f : M;
-    float o = 0.0f, L = 0.0f;
-#pragma unroll
-    for (int v = 0; v < NW; ++v) {
-      const float wt = exp2_hw(ms[(v * G + h) * 2] - Mu);
-      o = fmaf(wt, as[((size_t)v * G + h) * HD + c], o);
-      L = fmaf(wt, ms[(v * G + h) * 2 + 1], L);
-    }
-    const size_t row = slot_row(a, slot, j, fr0 + h);
-    if (direct) {
-      if (row_wanted(a, fr0 + h))
-        static_cast<uint16_t*>(a.out)[q_off(a, j, fr0 + h, HD) + c] = from_f<uint16_t>(L != 0.0f ? o / L : 0.0f);
-    } else {
-      a.acc[row * HD + c] = o;
-    }
-    if (c == 0) {
-      a.ml[row * 2] = Mu;
-      a.ml[row * 2 + 1] = L;
-    }
-  }
 }
 
 // ------------------------------------------------------------------ 128-row tiles (bf16)
@@ -366,25 +158,23 @@ __device__ __forceinline__ float poison_of(float codes) {
 // bf16 (each weight off by at most 2^-9 of itself, as much as the output's own
 // rounding; the sum is taken before the rounding).
 template <int HD>
-__global__ __launch_bounds__(256, 2) void rows_tile_kernel(RowsArgs a) {
+__device__ __forceinline__ void rows_tile(const RowsArgs& a, int item, uint16_t* buf0, uint16_t* buf1) {
   constexpr int KT = rows_kt(HD), KH = KT / 32, KS = HD / 16, DB = HD / 32;
-  // Four objects, each access naming one: a copy in flight into one buffer is then known
-  // not to touch the other (of one array, every LDS read waited for all copies: 20% slower).
-  __shared__ __align__(1024) uint16_t k_a[KT * HD], v_a[KT * HD], k_b[KT * HD], v_b[KT * HD];
   const int lane = threadIdx.x & 63, w = wave_id(), hl = lane >> 5;
   // the item: own (or joint) row blocks first, then the prefix's
   const int nbo = (a.R + kRowsTile - 1) / kRowsTile;
-  const int own_items = a.own_stream ? 0 : a.B * a.n_kv * nbo * a.S_own;
-  const bool own = (int)blockIdx.x < own_items;
+  const int own_items = a.own_few ? 0 : a.B * a.n_kv * nbo * a.S_own;
+  const bool own = item < own_items;
   int blk, s, j, b;
   if (own) {
-    const int units = a.B * a.n_kv, x = (int)blockIdx.x / units, u = (int)blockIdx.x - x * units;
+    const int units = a.B * a.n_kv, x = item / units, u = item - x * units;
     j = u % a.n_kv;
     b = u / a.n_kv;
     s = x % a.S_own;
     blk = nbo - 1 - x / a.S_own;  // the last rows see the most keys: first
   } else {
-    const int item = (int)blockIdx.x - own_items, units = a.n_kv * a.S_prefix;
+    item -= own_items;
+    const int units = a.n_kv * a.S_prefix;
     blk = item / units;
     const int u = item - blk * units;
     j = u % a.n_kv;
@@ -438,10 +228,10 @@ __global__ __launch_bounds__(256, 2) void rows_tile_kernel(RowsArgs a) {
   float m_run, l_run;  // in units of the scaled score
 
   const uint32_t kbase = score_base<HD>(lane), vbase = v_base<HD>(lane);
-  auto load = [&](int t, uint16_t* ks, uint16_t* vs) {
+  auto load = [&](int t, uint16_t* buf) {
     const int k = (t < np ? t : t - np) * KT, n = (t < np ? kp.n : ko.n) - k;
-    copy_tile<HD, KT, true>((t < np ? Kp : Ko) + (size_t)k * HD, n, ks);
-    copy_tile<HD, KT, false>((t < np ? Vp : Vo) + (size_t)k * HD, n, vs);
+    copy_tile<HD, KT, true>((t < np ? Kp : Ko) + (size_t)k * HD, n, buf);
+    copy_tile<HD, KT, false>((t < np ? Vp : Vo) + (size_t)k * HD, n, buf + KT * HD);
   };
   // A second pass where an infinite or NaN value met a weight of 0 (a row that does not
   // see it): such values count as 0 there and are added afterwards where they are seen.
@@ -454,10 +244,11 @@ again:
   m_run = -INFINITY;
   l_run = 0.0f;
   bool odd = false;
-  auto step = [&](int t, uint16_t* ks, uint16_t* vs, uint16_t* ks_next, uint16_t* vs_next) {
+  auto step = [&](int t, uint16_t* buf, uint16_t* next) {
+    uint16_t *ks = buf, *vs = buf + KT * HD;
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's share of tile t is in LDS
     __syncthreads();                     // every wave's share, and tile t - 1 is no longer read
-    if (t + 1 < nt) load(t + 1, ks_next, vs_next);
+    if (t + 1 < nt) load(t + 1, next);
     if (pass == 1) {
       for (int i = threadIdx.x; i < KT * HD / 2; i += 256) {
         uint32_t* x = reinterpret_cast<uint32_t*>(vs) + i;
@@ -546,10 +337,10 @@ again:
       odd |= __any(nf != 0);
     }
   };
-  if (nt > 0) load(0, k_a, v_a);
+  if (nt > 0) load(0, buf0);
   for (int t = 0; t < nt; t += 2) {
-    step(t, k_a, v_a, k_b, v_b);
-    if (t + 1 < nt) step(t + 1, k_b, v_b, k_a, v_a);
+    step(t, buf0, buf1);
+    if (t + 1 < nt) step(t + 1, buf1, buf0);
   }
   if (pass == 0 && __syncthreads_or(odd)) {
     pass = 1;
@@ -606,6 +397,341 @@ again:
         *reinterpret_cast<float4*>(dst + 32 * db + 8 * q4 + 4 * hl) =
             make_float4(o[db][4 * q4 + 0], o[db][4 * q4 + 1], o[db][4 * q4 + 2], o[db][4 * q4 + 3]);
   }
+}
+
+// ------------------------------------------------------------------ at most 16 rows (bf16)
+
+// Copies 16 rows of HD elements into a wave's LDS slice (rows past n - 1 repeat row n - 1),
+// chunks permuted: score operands as in copy_tile; V by 2 (r % 8) (head_dim 64: 2 (r / 2 %
+// 4)), its reads taking 32 bytes of 8 rows at a time.
+template <int HD>
+__device__ __forceinline__ int few_v_swz(int r) { return HD == 64 ? 2 * ((r >> 1) & 3) : 2 * (r & 7); }
+template <int HD, bool SCORE>
+__device__ __forceinline__ void copy16(const uint16_t* src, int n, uint16_t* dst) {
+  constexpr int CPR = HD / 8, RPI = 64 / CPR, CH = 16 / RPI;
+  const int lane = threadIdx.x & 63, r0 = lane / CPR, ch = lane % CPR;
+  const __amdgpu_buffer_rsrc_t res =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(src), (short)0, 16 * HD * 2, 0x00027000);
+#pragma unroll
+  for (int i = 0; i < CH; ++i) {
+    const int r = r0 + RPI * i;
+    const int col = 16 * (ch ^ (SCORE ? score_swz<HD>(r) : few_v_swz<HD>(r)));
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (__attribute__((address_space(3))) void*)(dst + 512 * i), 16,
+                                             min(r, n - 1) * HD * 2 + col, 0, 0, 0);
+  }
+}
+
+// Waits until at most N of the wave's vector memory operations are in flight (they complete
+// in order), and keeps the LDS reads that follow behind it.
+template <int N>
+__device__ __forceinline__ void wait_copies() {
+  static_assert(N < 16, "low four bits of the count");
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(0x0f70 + N);
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// One workgroup of 4 waves per (unit, split): units 0 .. B n_kv - 1 are the own rows of (b,
+// j) in S_own splits, the rest the prefix of KV head j in S_prefix splits.  A split's 16-key
+// blocks go to the waves in turn, and each wave streams its own through its own slice of
+// LDS, with no barrier: HBM-bound, so what matters is loads in flight (head_dim 256: K and
+// V of one block, K refilled as soon as the scores are taken, V after its product; smaller
+// ones: two blocks).  Scores S^T = K Q^T on MFMA 16x16x32, one row per column; O^T += V^T P^T
+// on 16x16x16 with P^T straight from the score registers, as the sum of two bf16 parts
+// (2^-17 of a weight is lost; the matrix unit idles here anyway).  The waves' states meet in
+// LDS.  With a.sc the scores of own keys are kept for the weights.
+template <int HD>
+__device__ __forceinline__ void rows_few(const RowsArgs& a, int item, uint16_t* buf0, uint16_t* buf1,
+                                         float (*ml)[16][2]) {
+  constexpr int NW = 4, KC = HD / 32, DB = HD / 16;
+  constexpr bool ONE = HD == 256;  // one block at a time: K in buf0, V in buf1
+  constexpr int SLICE = rows_kt(HD) * HD / 2;
+  typedef short s16x4_t __attribute__((ext_vector_type(4)));
+  const int tid = threadIdx.x, lane = tid & 63, w = wave_id(), hq = lane & 15, lg = lane >> 4;
+  const int own_items = a.own_few ? a.B * a.n_kv * a.S_own : 0;
+  const bool own = item < own_items;
+  if (!own) item -= own_items;
+  const int units = own ? a.B * a.n_kv : a.n_kv;
+  const int S = own ? a.S_own : a.S_prefix;
+  const int s = item / units, u = item - s * units;
+  const int j = u % a.n_kv, b = u / a.n_kv;
+  const int slot = own ? a.S_prefix + s : s;
+  const int nr = own ? a.R : a.B * a.R;
+  const int fr0 = own ? b * a.R : 0;
+  Seq sq{0, 0};
+  if (own) sq = seq_of(a, b);
+  if (own && sq.n == 0) return;  // no row of this sequence is asked for
+  const int T = own ? sq.len : a.T_prefix;
+  const int nblk_all = (T + kSaBlock - 1) / kSaBlock;
+  const int k0 = kSaBlock * sa_first_block(s, nblk_all, S);
+  const int nk = min(T, kSaBlock * sa_first_block(s + 1, nblk_all, S)) - k0;  // keys of this split
+  const int nblk = nk > 0 ? (nk + kSaBlock - 1) / kSaBlock : 0;
+  const int nb = nblk > w ? (nblk - 1 - w) / NW + 1 : 0;  // this wave's blocks: w, w + NW, ..
+  const KeyRange kr = own ? own_range(a, b, j, k0, k0 + nk) : prefix_range(a, j, k0, k0 + nk);
+  const uint16_t* Kp = static_cast<const uint16_t*>(own ? a.k : a.pk) + kr.row * HD;
+  const uint16_t* Vp = static_cast<const uint16_t*>(own ? a.v : a.pv) + kr.row * HD;
+  // keys of this split that the lane's row sees, and that every row sees
+  const int lim = hq < nr ? (own ? min(rows_seen(sq, hq / a.g) - k0, nk) : nk) : 0;
+  const int all = own ? min(rows_seen(sq, 0) - k0, nk) : nk;
+  float* sc_row = a.sc != nullptr && own && hq < nr
+                      ? a.sc + (((size_t)b * a.n_kv + j) * a.R + hq) * a.sc_ld + k0 + 4 * lg
+                      : nullptr;
+
+  uint16_t* const sl0 = buf0 + SLICE * w;
+  uint16_t* const sl1 = buf1 + SLICE * w;
+  auto load_k = [&](int i, uint16_t* dst) {
+    const int kb = kSaBlock * (w + NW * i);
+    copy16<HD, true>(Kp + (size_t)kb * HD, nk - kb, dst);
+  };
+  auto load_v = [&](int i, uint16_t* dst) {
+    const int kb = kSaBlock * (w + NW * i);
+    copy16<HD, false>(Vp + (size_t)kb * HD, nk - kb, dst);
+  };
+  // every LDS read of the wave is done: its slice may be written again
+  auto reads_done = [&]() {
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // queries first: the loop's wait for them then leaves the copies in flight
+  bf16x8_t qf[KC];
+  {
+    const uint16_t* qs = static_cast<const uint16_t*>(a.q) + q_off(a, j, fr0 + min(hq, nr - 1), HD) + 8 * lg;
+#pragma unroll
+    for (int c = 0; c < KC; ++c) {
+      u32x4_t v = *reinterpret_cast<const u32x4_t*>(qs + 32 * c);
+      if (hq >= nr) v = u32x4_t{0u, 0u, 0u, 0u};
+      qf[c] = __builtin_bit_cast(bf16x8_t, v);
+    }
+  }
+  if constexpr (ONE) {
+    if (nb > 0) {
+      load_k(0, sl0);
+      load_v(0, sl1);
+    }
+  } else {
+    if (nb > 0) {
+      load_k(0, sl0);
+      load_v(0, sl0 + SLICE / 2);
+    }
+    if (nb > 1) {
+      load_k(1, sl1);
+      load_v(1, sl1 + SLICE / 2);
+    }
+  }
+
+  const uint32_t kbase = hq * HD * 2 + ((lg ^ score_swz<HD>(hq)) << 4);
+  const int vrow = 4 * lg + (hq >> 2);
+  const uint32_t vbase = vrow * HD * 2 + ((((hq & 3) >> 1) ^ few_v_swz<HD>(vrow)) << 4) + 8 * (hq & 1);
+
+  f32x4_t o[DB];
+  float m_run, l_run;
+  // as in rows_tile: a second pass without the infinite and NaN values that met a weight
+  // of 0 (a row that does not see them)
+  int pass = 0;
+again:
+#pragma unroll
+  for (int db = 0; db < DB; ++db) o[db] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+  m_run = -INFINITY;
+  l_run = 0.0f;
+  bool odd = false;
+  // NEXT (head_dim 256): whether another block follows; a condition inside the loop made the
+  // compiler wait for V before K was read
+  auto step = [&](auto next, int i, uint16_t* ks, uint16_t* vs) {
+    constexpr bool NEXT = decltype(next)::value != 0;
+    const int kb = kSaBlock * (w + NW * i);
+    const bool masked = kb + kSaBlock > all;
+    // this block's K (head_dim 256; V was issued after it), or K and V (the next block's
+    // were): copies complete in order
+    if (ONE || i + 1 < nb)
+      wait_copies<ONE ? KC : 2 * KC>();
+    else
+      wait_copies<0>();
+    f32x4_t st = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int c = 0; c < KC; ++c)
+      st = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+          *reinterpret_cast<const bf16x8_t*>(reinterpret_cast<const char*>(ks) + (kbase ^ (c << 6))), qf[c], st, 0, 0,
+          0);
+    if constexpr (ONE) {
+      reads_done();
+      if constexpr (NEXT) load_k(i + 1, ks);
+    }
+    // st[r]: key kb + 4 lg + r, row hq
+    float sv[4], mx = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      sv[r] = st[r] * ScoreScale<HD>::v;
+      if (masked) sv[r] = kb + 4 * lg + r < lim ? sv[r] : -INFINITY;
+      mx = fmaxf(mx, sv[r]);
+    }
+    if (sc_row != nullptr && pass == 0) *reinterpret_cast<float4*>(sc_row + kb) = make_float4(sv[0], sv[1], sv[2], sv[3]);
+    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    const bool grow = mx > m_run + 8.0f;
+    if (__any(grow)) {
+      const float m_new = grow ? mx : m_run;
+      const float alpha = exp2_hw(grow ? m_run - m_new : 0.0f);
+      m_run = m_new;
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) o[db] *= alpha;
+    }
+    const float m_use = m_run == -INFINITY ? 0.0f : m_run;
+    float p[4], lo[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) p[r] = exp2_hw(sv[r] - m_use);
+    l_run += (p[0] + p[1]) + (p[2] + p[3]);
+    const uint2 ph = make_uint2(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]));
+    lo[0] = p[0] - bf_lo(ph.x);
+    lo[1] = p[1] - bf_hi(ph.x);
+    lo[2] = p[2] - bf_lo(ph.y);
+    lo[3] = p[3] - bf_hi(ph.y);
+    const uint2 pl = make_uint2(pack_bf16x2(lo[0], lo[1]), pack_bf16x2(lo[2], lo[3]));
+    const s16x4_t pfh = __builtin_bit_cast(s16x4_t, ph), pfl = __builtin_bit_cast(s16x4_t, pl);
+    if constexpr (ONE) wait_copies<NEXT ? KC : 0>();  // V; the next block's K was issued after it
+    if (masked) {
+      uint32_t nf = 0;
+#pragma unroll 1
+      for (int x = lane; x < 16 * HD / 2; x += 64) {
+        uint32_t* at = reinterpret_cast<uint32_t*>(vs) + x;
+        const uint32_t f = nonfinite2(*at);
+        nf |= f;
+        if (pass == 1 && f != 0) *at &= (f & 0x8000u ? 0u : 0xffffu) | (f & 0x80000000u ? 0u : 0xffff0000u);
+      }
+      odd |= pass == 0 && __any(nf != 0);
+    }
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      const s16x4_t vf = __builtin_bit_cast(
+          s16x4_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4_t*)(
+                       reinterpret_cast<char*>(vs) + (vbase ^ (db << 5)))));
+      o[db] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf, pfh, o[db], 0, 0, 0);
+      o[db] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf, pfl, o[db], 0, 0, 0);
+    }
+    reads_done();
+    if constexpr (ONE) {
+      if constexpr (NEXT) load_v(i + 1, vs);
+    } else {
+      if (i + 2 < nb) {
+        load_k(i + 2, ks);
+        load_v(i + 2, vs);
+      }
+    }
+  };
+  if constexpr (ONE) {
+    for (int i = 0; i + 1 < nb; ++i) step(IC<1>{}, i, sl0, sl1);
+    if (nb > 0) step(IC<0>{}, nb - 1, sl0, sl1);
+  } else {
+    for (int i = 0; i < nb; i += 2) {
+      step(IC<0>{}, i, sl0, sl0 + SLICE / 2);
+      if (i + 1 < nb) step(IC<0>{}, i + 1, sl1, sl1 + SLICE / 2);
+    }
+  }
+  if (pass == 0 && odd) {
+    pass = 1;
+    if constexpr (ONE) {
+      load_k(0, sl0);
+      load_v(0, sl1);
+    } else {
+      load_k(0, sl0);
+      load_v(0, sl0 + SLICE / 2);
+      if (nb > 1) {
+        load_k(1, sl1);
+        load_v(1, sl1 + SLICE / 2);
+      }
+    }
+    goto again;
+  }
+  if (pass == 1) {
+    // the values that pass 1 took as 0 in masked blocks, for the rows that see them
+#pragma unroll 1
+    for (int i = 0; i < nb; ++i) {
+      const int kb = kSaBlock * (w + NW * i);
+      if (kb + kSaBlock <= all) continue;
+#pragma unroll 1
+      for (int t = kb; t < min(kb + kSaBlock, lim); ++t) {
+        const uint16_t* vr = Vp + (size_t)t * HD + 4 * lg;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          const uint2 y = *reinterpret_cast<const uint2*>(vr + 16 * db);
+          const float v[4] = {bf_lo(y.x), bf_hi(y.x), bf_lo(y.y), bf_hi(y.y)};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[db][e] += fabsf(v[e]) < INFINITY ? 0.0f : v[e];
+        }
+      }
+    }
+  }
+  l_run += __shfl_xor(l_run, 16, 64);
+  l_run += __shfl_xor(l_run, 32, 64);
+
+  // The waves' states into LDS (elements below HD / 2 of the 16 rows in buf0, the others
+  // in buf1, 16-byte chunks permuted by the row), then merged in wave order: the slot's
+  // state, or with one slot the output.
+  __syncthreads();
+  constexpr int HH = HD / 2, CM = HH / 4 - 1;
+  float* f0 = reinterpret_cast<float*>(buf0);
+  float* f1 = reinterpret_cast<float*>(buf1);
+  if (lg == 0) {
+    ml[w][hq][0] = m_run;
+    ml[w][hq][1] = l_run;
+  }
+#pragma unroll
+  for (int db = 0; db < DB; ++db) {
+    float* f = db < DB / 2 ? f0 : f1;
+    const int c = (4 * db + lg) & CM;
+    *reinterpret_cast<f32x4_t*>(f + (w * 16 + hq) * HH + 4 * (c ^ (hq & CM))) = o[db];
+  }
+  __syncthreads();
+  const bool direct = a.S_prefix + a.S_own == 1;
+  for (int i = tid; i < nr * (HD / 4); i += 64 * NW) {
+    const int h = i / (HD / 4), c4 = i - h * (HD / 4);
+    const float* f = c4 <= CM ? f0 : f1;
+    float M = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < NW; ++v) M = fmaxf(M, ml[v][h][0]);
+    const float Mu = M == -INFINITY ? 0.0f : M;
+    f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f};
+    float L = 0.0f;
+#pragma unroll
+    for (int v = 0; v < NW; ++v) {
+      const float wt = exp2_hw(ml[v][h][0] - Mu);
+      x += wt * *reinterpret_cast<const f32x4_t*>(f + (v * 16 + h) * HH + 4 * ((c4 & CM) ^ (h & CM)));
+      L = fmaf(wt, ml[v][h][1], L);
+    }
+    const size_t row = slot_row(a, slot, j, fr0 + h);
+    if (direct) {
+      if (row_wanted(a, fr0 + h)) {
+        const float inv = L != 0.0f ? 1.0f / L : 0.0f;
+        uint2 y = make_uint2(0u, 0u);
+        if (L != 0.0f) y = make_uint2(pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv));
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + q_off(a, j, fr0 + h, HD) + 4 * c4) = y;
+      }
+    } else {
+      *reinterpret_cast<f32x4_t*>(a.acc + row * HD + 4 * c4) = x;
+    }
+    if (c4 == 0) {
+      a.ml[row * 2] = Mu;
+      a.ml[row * 2 + 1] = L;
+    }
+  }
+}
+
+// Workgroups 0 .. tile_items - 1 take tiles, the rest few-row splits: the matrix work of the
+// ones runs beside the memory traffic of the others.  The two buffers are two objects,
+// every access naming one: a copy in flight into one is then known not to touch the other
+// (of one array, every LDS read waited for all copies: 8 prompts over 8192 keys 160 us
+// instead of 147).
+template <int HD>
+__global__ __launch_bounds__(256, 2) void rows_bf16_kernel(RowsArgs a, int tile_items) {
+  constexpr int KT = rows_kt(HD);
+  __shared__ __align__(1024) uint16_t buf0[2 * KT * HD], buf1[2 * KT * HD];
+  __shared__ float ml[4][16][2];
+  if ((int)blockIdx.x < tile_items)
+    rows_tile<HD>(a, (int)blockIdx.x, buf0, buf1);
+  else
+    rows_few<HD>(a, (int)blockIdx.x - tile_items, buf0, buf1, ml);
 }
 
 // ------------------------------------------------------------------ fp32
@@ -838,20 +964,26 @@ __global__ __launch_bounds__(256) void rows_finish_kernel(RowsArgs a, int merge_
     float x[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] = 0.0f;
-    // 8 states' loads in flight; an empty state's acc was never written and counts as 0
+    // the states that hold keys, 8 at a time in flight (an empty state has no acc)
     const float* src = a.acc + slot_row(a, 0, j, fr) * HD + E * lane;
     const size_t step = (size_t)a.n_kv * Rt * HD;
-    for (int s0 = 0; s0 < S; s0 += 8) {
-      float y[8][E];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) load_e<E>(src + (size_t)min(s0 + i, S - 1) * step, y[i]);
+    for (int half = 0; half < 2; ++half) {
+      const float wv = half == 0 ? m.w0 : m.w1;
+      unsigned long long left = __ballot(wv != 0.0f);
+      while (left != 0) {
+        float y[8][E], wt[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int s = min(s0 + i, 127);
-        const float wt = __builtin_bit_cast(
-            float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, s < 64 ? m.w0 : m.w1), s & 63));
+        for (int i = 0; i < 8; ++i) {
+          const int s = left != 0 ? __builtin_ctzll(left) : 0;
+          wt[i] = left != 0 ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wv), s)) : 0.0f;
+          if (left != 0) load_e<E>(src + (size_t)(s + 64 * half) * step, y[i]);
+          left &= left - 1;
+        }
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = s0 + i < S && wt != 0.0f ? fmaf(y[i][e], wt, x[e]) : x[e];
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int e = 0; e < E; ++e) x[e] = wt[i] != 0.0f ? fmaf(y[i][e], wt[i], x[e]) : x[e];
       }
     }
     const float L = m.L;
@@ -1046,28 +1178,6 @@ __global__ __launch_bounds__(256) void weight_sum_kernel(RowsArgs a) {
 
 // ------------------------------------------------------------------ launchers
 
-template <int HD, int G>
-static hipError_t stream_t(const RowsArgs& a, int items, hipStream_t st) {
-  if (a.N > 1)
-    hipLaunchKernelGGL((rows_stream_kernel<HD, G, true>), dim3(items), dim3(64 * kSaWaves), 0, st, a);
-  else
-    hipLaunchKernelGGL((rows_stream_kernel<HD, G, false>), dim3(items), dim3(64 * kSaWaves), 0, st, a);
-  return hipGetLastError();
-}
-
-template <int HD>
-static hipError_t stream_rows(const RowsArgs& a, int rows, int items, hipStream_t st) {
-  switch (sa_group(rows)) {
-    case 1: return stream_t<HD, 1>(a, items, st);
-    case 2: return stream_t<HD, 2>(a, items, st);
-    case 3: return stream_t<HD, 3>(a, items, st);
-    case 4: return stream_t<HD, 4>(a, items, st);
-    case 6: return stream_t<HD, 6>(a, items, st);
-    case 8: return stream_t<HD, 8>(a, items, st);
-    default: return stream_t<HD, 16>(a, items, st);
-  }
-}
-
 #define KVD_LAUNCH_TRY(expr)          \
   do {                                \
     hipError_t _e = (expr);           \
@@ -1080,22 +1190,15 @@ static hipError_t launch_rows_t(const RowsArgs& a, hipStream_t st) {
   const int RB = BF ? kRowsTile : kRowsWave;
   const long long nbo = (a.R + RB - 1) / RB, nbp = ((long long)a.B * a.R + RB - 1) / RB;
   const int S_prefix = a.S_prefix;
-  long long stream_items = 0, tile_items = 0;
-  (a.own_stream ? stream_items : tile_items) += (long long)a.B * a.n_kv * a.S_own * (a.own_stream ? 1 : nbo);
-  (a.prefix_stream ? stream_items : tile_items) += (long long)a.n_kv * S_prefix * (a.prefix_stream ? 1 : nbp);
-  if constexpr (BF) {
-    if (stream_items > 0) {
-      const int rows = a.prefix_stream && S_prefix > 0 ? a.B * a.R : a.R;
-      KVD_LAUNCH_TRY(stream_rows<HD>(a, rows, (int)stream_items, st));
-    }
-    if (tile_items > 0) {
-      hipLaunchKernelGGL(rows_tile_kernel<HD>, dim3((unsigned)tile_items), dim3(256), 0, st, a);
-      KVD_LAUNCH_TRY(hipGetLastError());
-    }
-  } else {
+  long long few_items = 0, tile_items = 0;
+  (a.own_few ? few_items : tile_items) += (long long)a.B * a.n_kv * a.S_own * (a.own_few ? 1 : nbo);
+  (a.prefix_few ? few_items : tile_items) += (long long)a.n_kv * S_prefix * (a.prefix_few ? 1 : nbp);
+  if constexpr (BF)
+    hipLaunchKernelGGL(rows_bf16_kernel<HD>, dim3((unsigned)(tile_items + few_items)), dim3(256), 0, st, a,
+                       (int)tile_items);
+  else
     hipLaunchKernelGGL(rows_f32_kernel<HD>, dim3((unsigned)tile_items), dim3(64), 0, st, a);
-    KVD_LAUNCH_TRY(hipGetLastError());
-  }
+  KVD_LAUNCH_TRY(hipGetLastError());
   const int S = S_prefix + a.S_own;
   const bool sums = a.weight != nullptr && a.T_own > 0;
   const long long rows = (long long)a.B * a.R * a.n_kv;

@@ -155,3 +155,20 @@ def test_captured_and_replayed():
             torch.cuda.synchronize()
             assert all(torch.equal(a, c) for a, c in zip(mine, want))
             assert lens.tolist() == [keep, min(keep, T - i)]
+
+
+def test_arrays_at_4_byte_alignment():
+    k, v, w, pos = cache("bf16", 2, 3, 64, 77, 21)
+    flat = torch.empty(2 * w.numel() + 9, dtype=torch.int32, device="cuda")
+    for off in (1, 2, 3):
+        w2 = flat[off:off + w.numel()].view(torch.float32).view(w.shape)
+        p2 = flat[off + w.numel():off + 2 * w.numel()].view(pos.shape)
+        for T, keep in ((77, 76), (70, 33)):
+            w2.copy_(w)
+            p2.copy_(pos)
+            s = shape("bf16", 6, 3, 64)
+            mine = [k.clone(), v.clone()]
+            ws = torch.empty(kvd.kvd_evict_workspace_bytes(s, 2, T), dtype=torch.uint8, device="cuda")
+            kvd.kvd_evict(s, *mine, T, keep, w2, ws, pos=p2, last_pos=i32([76, 76]), sink=2, recent=7)
+            want = evict("bf16", k, v, w, pos, T, keep, None, [76, 76], 2, 7)
+            assert all(torch.equal(a, b) for a, b in zip((*mine, w2, p2), want))

@@ -261,3 +261,16 @@ def test_offsets_beyond_32_bits():
         a = call(s, {**y, "k": k, "v": v}, 0, T, None, None, w, 0.0, 0, t_off)
         c = call(s, {**y, "k": x["k"], "v": x["v"]}, 0, T, None, None, w2, 0.0)
         assert torch.equal(a, c) and torch.equal(w[:, :, t_off:], w2)
+
+
+@pytest.mark.parametrize("N", [1, 30])
+def test_weights_at_4_byte_alignment(N):
+    for dtype in ("bf16", "f32"):
+        s = shape(dtype, 6, 2, 64)
+        x = make(dtype, 6, 2, 64, 2, N, 50, 45, 33)
+        flat = torch.zeros(x["weight"].numel() + 3, device="cuda")
+        w = flat[3:].view(x["weight"].shape)
+        w.copy_(x["weight"])
+        a = call(s, x, 50, 45, None, None, w, 0.5)
+        b = call(s, x, 50, 45, None, None, x["weight"], 0.5)
+        assert torch.equal(a, b) and torch.equal(w, x["weight"])

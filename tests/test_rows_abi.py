@@ -10,7 +10,7 @@ import oracle as O
 
 kvd = pytest.importorskip("paper_2603_19664_amd.kvd")
 lib = kvd.lib
-FAKE, MISALIGNED = 0x10000, 0x10008
+FAKE, MISALIGNED, ODD = 0x10000, 0x10008, 0x10002
 BIG = 1 << 40
 
 
@@ -62,7 +62,7 @@ def evict(s=None, kv=view(), B=2, T=16, keep=8, weight=FAKE, pos=None, last=None
     (kvd.KVD_ERR_NULL, dict(own=view(v=0))),
     (kvd.KVD_ERR_ALIGN, dict(q=MISALIGNED)),
     (kvd.KVD_ERR_ALIGN, dict(out=MISALIGNED)),
-    (kvd.KVD_ERR_ALIGN, dict(weight=MISALIGNED)),
+    (kvd.KVD_ERR_ALIGN, dict(weight=ODD)),
     (kvd.KVD_ERR_ALIGN, dict(p=view(k=MISALIGNED))),
     (kvd.KVD_ERR_SHAPE, dict(p=view(t_cap=15))),
     (kvd.KVD_ERR_SHAPE, dict(own=view(t_cap=20, t_off=5))),
@@ -110,8 +110,8 @@ def test_weighted_refusals(status, kw):
     (kvd.KVD_ERR_NULL, dict(sink=1)),
     (kvd.KVD_ERR_NULL, dict(recent=1)),
     (kvd.KVD_ERR_NULL, dict(recent=1, pos=FAKE)),
-    (kvd.KVD_ERR_ALIGN, dict(pos=MISALIGNED)),
-    (kvd.KVD_ERR_ALIGN, dict(weight=MISALIGNED)),
+    (kvd.KVD_ERR_ALIGN, dict(pos=ODD)),
+    (kvd.KVD_ERR_ALIGN, dict(weight=ODD)),
     (kvd.KVD_ERR_WORKSPACE, dict(ws=None)),
     (kvd.KVD_ERR_WORKSPACE, dict(n=100)),
     (kvd.KVD_ERR_ALIGN, dict(ws=FAKE + 128)),
