@@ -888,19 +888,23 @@ struct RowsPlan {
 };
 
 // Slots of a key range that `units` items share, each of at least `least` keys and at most
-// `most`: the count with the shortest rounds of kRowsTargetWgs workgroups, a slot's fixed
-// cost (first loads, state written and merged) taken as kRowsSlotKeys keys of a nominal
-// 4096.  Grows with keys only (the candidates grow, their order does not change).
-int32_t row_slots(long long units, long long keys, int32_t least, int32_t most) {
-  const long long top = std::max(1ll, std::min<long long>((keys + least - 1) / least, most));
-  int32_t best = 1;
-  double best_cost = 0;
-  for (int32_t S = 1; S <= top; ++S) {
-    const double rounds = (double)((units * S + kvd::kRowsTargetWgs - 1) / kvd::kRowsTargetWgs);
-    const double cost = rounds * (4096.0 / S + kvd::kRowsSlotKeys);
-    if (S == 1 || cost < best_cost) best = S, best_cost = cost;
-  }
-  return best;
+// kRowsMostSlots: enough for kRowsTargetWgs workgroups, and beyond that the count S that
+// balances what the last workgroups of a launch leave idle, about half a slot (keys / S /
+// 2), against a slot's fixed cost of kRowsSlotKeys keys (first loads, state written and
+// merged) for every workgroup's units S / kRowsTargetWgs of them.  A causal range (every row
+// its own length) holds half of the keys.  Grows with keys.
+int32_t row_slots(long long units, long long keys, int32_t least, bool causal) {
+  const double work = (double)units * kvd::kRowsSlotKeys * (causal ? 0.5 : 1.0);
+  const long long balance = (long long)std::sqrt(0.5 * kvd::kRowsTargetWgs * (double)keys / work);
+  const long long fill = (kvd::kRowsTargetWgs + units - 1) / units;
+  return (int32_t)std::max(1ll, std::min({std::max(balance, fill), (keys + least - 1) / least,
+                                          (long long)kvd::kRowsMostSlots}));
+}
+// Slots of T own rows of which the last N are the new tokens: causal while those are more
+// than half of them.  Never fewer for more rows.
+int32_t causal_slots(long long units, int32_t T, int32_t least, int32_t N) {
+  const int32_t c = row_slots(units, std::min<long long>(T, 2ll * N), least, N > 1);
+  return 2ll * N > T ? c : std::max(c, row_slots(units, T, least, false));
 }
 int32_t slot_keys(long long keys, int32_t slots) {
   return (int32_t)((((keys + slots - 1) / slots) + 63) / 64 * 64);
@@ -911,31 +915,30 @@ bool rows_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T_prefix, 
                RowsPlan* p) {
   const bool bf = s->dtype == KVD_BF16;
   const int32_t g = s->n_q_heads / s->n_kv_heads, RB = bf ? kvd::kRowsTile : kvd::kRowsWave;
+  const int32_t least = bf ? kvd::kRowsLeastKeys : kvd::kRowsLeastKeysF32;
   *p = RowsPlan{};
   const long long R = (long long)N * g, Rt = R * B, units = (long long)B * s->n_kv_heads;
   const long long keys = (long long)T_prefix + T_own;
-  if (Rt * s->n_kv_heads > INT32_MAX || keys > INT32_MAX - 1024 || units > INT32_MAX) return false;
+  if (Rt * s->n_kv_heads > INT32_MAX || Rt >= 1ll << 28 || keys > INT32_MAX - 1024 || units > INT32_MAX) return false;
   p->R = (int32_t)R;
   p->joint = T_prefix > 0 && T_own > 0 && R >= RB / 2;
   const long long nbo = (R + RB - 1) / RB, nbp = (Rt + RB - 1) / RB;
   if (p->joint) {
-    p->S_own = row_slots(units * nbo, keys, kvd::kRowsLeastKeys, kvd::kRowsMostSlots);
+    p->S_own = row_slots(units * nbo, keys, least, false);
     p->C_own = slot_keys(keys, p->S_own);
     p->items = units * nbo * p->S_own;
   } else {
     if (T_prefix > 0) {
       p->prefix_few = bf && Rt <= kvd::kRowsFew;
       const long long u = p->prefix_few ? s->n_kv_heads : s->n_kv_heads * nbp;
-      p->S_prefix = row_slots(u, T_prefix, p->prefix_few ? kvd::kSaBlock : kvd::kRowsLeastKeys,
-                              p->prefix_few ? kvd::kSaMaxSplits : kvd::kRowsMostSlots);
+      p->S_prefix = row_slots(u, T_prefix, least, false);
       p->C_prefix = slot_keys(T_prefix, p->S_prefix);
       p->items += u * p->S_prefix;
     }
     if (T_own > 0) {
       p->own_few = bf && R <= kvd::kRowsFew;
       const long long u = p->own_few ? units : units * nbo;
-      p->S_own = row_slots(u, T_own, p->own_few ? kvd::kSaBlock : kvd::kRowsLeastKeys,
-                           p->own_few ? kvd::kSaMaxSplits : kvd::kRowsMostSlots);
+      p->S_own = causal_slots(u, T_own, least, N);
       p->C_own = slot_keys(T_own, p->S_own);
       p->items += u * p->S_own;
     }
@@ -956,12 +959,12 @@ bool rows_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T_prefix, 
       p->items = std::max(p->items, (long long)rows + units * ((T_own + 255) / 256));
     } else {
       // tiles of keys, their rows in S_w parts of at least 256 until the chip is full
-      const long long tiles = units * ((T_own + (bf ? 127 : 15)) / (bf ? 128 : 16));
-      p->S_w = row_slots(tiles, R, 256, 64);
+      const long long keys_w = bf ? 128 : 16, tiles = units * ((T_own + keys_w - 1) / keys_w);
+      const long long most = std::min(64ll, (R + 255) / 256), want = kvd::kRowsTargetWgs;
+      p->S_w = (int32_t)std::max(1ll, std::min((want + tiles - 1) / tiles, most));
       p->lse = take(4 * rows);
-      // S_w T_own grows with T_own up to a rounding: room for the largest of either
-      p->wpart = take(4 * (size_t)units * std::max((long long)p->S_w * T_own,
-                                                   p->S_w > 1 || R > 256 ? kvd::kRowsTargetWgs * 128ll / units + T_own : 0));
+      // S_w T_own, or its bound over smaller T_own (it does not grow steadily)
+      p->wpart = take(4 * (size_t)units * std::min(most * T_own, want * keys_w / units + T_own + keys_w));
       p->items = std::max(p->items, tiles * p->S_w);
     }
   }
@@ -1033,6 +1036,7 @@ kvd_status rows_call(const kvd_attn_shape* shape, const void* q, int32_t N, cons
   a.n_q = shape->n_q_heads;
   a.n_kv = shape->n_kv_heads;
   a.g = shape->n_q_heads / shape->n_kv_heads;
+  a.g_inv = a.g > 1 ? (uint32_t)(((1ull << 32) + a.g - 1) / a.g) : 0;
   a.R = p.R;
   a.S_prefix = p.S_prefix;
   a.C_prefix = p.C_prefix;

@@ -225,6 +225,7 @@ struct RowsArgs {
   int B, N, n_q, n_kv, g, R;
   int S_prefix, C_prefix, S_own, C_own, S_w, sc_ld;
   int joint, prefix_few, own_few;
+  uint32_t g_inv;  // ceil(2^32 / g), g > 1
 };
 hipError_t launch_rows(const RowsArgs& a, int dtype_bf16, int hd, hipStream_t st);
 

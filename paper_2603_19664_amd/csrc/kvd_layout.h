@@ -394,8 +394,9 @@ constexpr int kRowsTile = 128;    // rows per workgroup of the tile kernel
 constexpr int kRowsWave = 16;     // rows per wave of the fp32 kernel
 constexpr int kRowsFew = 16;      // rows rows_few takes (one MFMA column block)
 constexpr int kRowsTargetWgs = 512;
-constexpr int kRowsLeastKeys = 128;  // keys per slot of the tile and fp32 kernels, at least
-constexpr int kRowsSlotKeys = 256;   // a slot's fixed cost in keys
+constexpr int kRowsLeastKeys = 128;     // keys per slot, at least (bf16)
+constexpr int kRowsLeastKeysF32 = 128;
+constexpr int kRowsSlotKeys = 512;   // a slot's fixed cost in keys
 constexpr int kRowsMostSlots = 64;
 
 // Value-absorbed fused attention (AbsorbArgs; head_dim 256).  Score tiles: K rows

@@ -6,7 +6,7 @@
 //                       rows per key range (single tokens), whose waves stream 16-key
 //                       blocks each on its own; rows_tile, 128 rows per workgroup that
 //                       share key tiles in LDS.  Both products on MFMA.
-//   rows_f32_kernel     fp32: 16 rows per wave, both products on MFMA 16x16x4 f32.
+//   rows_f32_kernel     fp32: 16 rows per workgroup, both products on MFMA 16x16x4 f32.
 //   rows_finish_kernel  merges the key ranges' softmax states into out, and adds up
 //                       the streamed scores' weights.
 //   weight_tile_kernel, weight_f32_kernel
@@ -41,11 +41,16 @@ __device__ __forceinline__ Seq seq_of(const RowsArgs& a, int b) {
 // Own rows that token i of n sees: those up to its own.
 __device__ __forceinline__ int rows_seen(const Seq& s, int i) { return i < s.n ? max(s.len - s.n + i + 1, 0) : 0; }
 
+// Token of a row (r / g): the high half of r ceil(2^32 / g), exact below 2^28 rows (g <= 16);
+// a division costs some 30 instructions, and copies of query rows take one per row.
+__device__ __forceinline__ int token_of(const RowsArgs& a, int r) {
+  return a.g == 1 ? r : (int)__umulhi((uint32_t)r, a.g_inv);
+}
 // Whether flat row fr belongs to a new token (the rows behind a sequence's n are left alone).
 __device__ __forceinline__ bool row_wanted(const RowsArgs& a, int fr) {
   if (a.n_new == nullptr) return true;
   const int b = fr / a.R;
-  return (fr - b * a.R) / a.g < seq_of(a, b).n;
+  return token_of(a, fr - b * a.R) < seq_of(a, b).n;
 }
 
 __device__ __forceinline__ size_t slot_row(const RowsArgs& a, int s, int j, int fr) {
@@ -53,8 +58,8 @@ __device__ __forceinline__ size_t slot_row(const RowsArgs& a, int s, int j, int 
 }
 // Element offset of flat row fr of KV head j in q and out.
 __device__ __forceinline__ size_t q_off(const RowsArgs& a, int j, int fr, int hd) {
-  const unsigned tok = (unsigned)fr / (unsigned)a.g;
-  return ((size_t)tok * a.n_q + (size_t)j * a.g + (fr - (int)tok * a.g)) * hd;
+  const int tok = token_of(a, fr);
+  return ((size_t)tok * a.n_q + (size_t)j * a.g + (fr - tok * a.g)) * hd;
 }
 
 // A range of keys [k0, k1) of KV head j: of the prefix, or of sequence b's own rows.
@@ -85,13 +90,21 @@ __device__ __forceinline__ int score_swz(int r) { return HD == 64 ? (r >> 1) & 7
 template <int HD>
 __device__ __forceinline__ int v_swz(int r) { return HD == 64 ? 4 * ((r >> 1) & 1) : 4 * (r & 3); }
 
+// A value that the compiler must compute again where it is used: offsets derived from it
+// are not kept in registers across a loop (the row tiles of head_dim 256 have none to spare:
+// their scores ran on one register quad for K, read, wait, multiply).
+__device__ __forceinline__ uint32_t fresh(uint32_t x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // Copies KT rows of HD elements from global memory straight into the LDS tile dst (rows
 // past n - 1 repeat row n - 1).  Thread tid copies chunk tid % CPR of rows r0 + RPI i, r0 =
 // tid / CPR: a full tile takes its rows' offsets from the thread once, 4096 i as a scalar.
 template <int HD, int KT, bool SCORE>
 __device__ __forceinline__ void copy_tile(const uint16_t* src, int n, uint16_t* dst) {
   constexpr int CPR = HD / 8, RPI = 256 / CPR, CH = KT / RPI;
-  const int tid = threadIdx.x, w = wave_id();
+  const int tid = (int)fresh(threadIdx.x), w = wave_id();
   const int r0 = tid / CPR, ch = tid % CPR;
   const __amdgpu_buffer_rsrc_t res =
       __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(src), (short)0, KT * HD * 2, 0x00027000);
@@ -159,7 +172,7 @@ __device__ __forceinline__ float poison_of(float codes) {
 // rounding; the sum is taken before the rounding).
 template <int HD>
 __device__ __forceinline__ void rows_tile(const RowsArgs& a, int item, uint16_t* buf0, uint16_t* buf1) {
-  constexpr int KT = rows_kt(HD), KH = KT / 32, KS = HD / 16, DB = HD / 32;
+  constexpr int KT = rows_kt(HD), KH = KT / 32, KS = HD / 16, DB = HD / 32, kLead = 4;
   const int lane = threadIdx.x & 63, w = wave_id(), hl = lane >> 5;
   // the item: own (or joint) row blocks first, then the prefix's
   const int nbo = (a.R + kRowsTile - 1) / kRowsTile;
@@ -195,7 +208,7 @@ __device__ __forceinline__ void rows_tile(const RowsArgs& a, int item, uint16_t*
     p1 = min(p0 + a.C_prefix, a.T_prefix);
   } else {
     const int last = min(r_blk + kRowsTile, sq.n * a.g) - 1;
-    const int seen = rows_seen(sq, last / a.g);  // the block's longest row
+    const int seen = rows_seen(sq, token_of(a, last));  // the block's longest row
     const int base = a.joint ? a.T_prefix : 0;
     const long long k0 = (long long)s * a.C_own, k1 = k0 + a.C_own;
     p0 = (int)min(k0, (long long)base);
@@ -215,9 +228,9 @@ __device__ __forceinline__ void rows_tile(const RowsArgs& a, int item, uint16_t*
   const bool wave_on = r_blk + 32 * w < (own ? sq.n * a.g : nr);
   const int fr = fr0 + min(rl, nr - 1);
   // keys of the item's own range that the row sees; every prefix key is seen
-  const int lim = own && rl < nr ? min(rows_seen(sq, rl / a.g) - o0, ko.n) : 0;
+  const int lim = own && rl < nr ? min(rows_seen(sq, token_of(a, rl)) - o0, ko.n) : 0;
   // own keys that every row of the wave's block sees
-  const int all = own ? min(rows_seen(sq, min(r_blk + 32 * w, nr - 1) / a.g) - o0, ko.n) : 0;
+  const int all = own ? min(rows_seen(sq, token_of(a, min(r_blk + 32 * w, nr - 1))) - o0, ko.n) : 0;
   bf16x8_t qf[KS];
   {
     const uint16_t* qs = static_cast<const uint16_t*>(a.q) + q_off(a, j, fr, HD) + 8 * hl;
@@ -227,7 +240,6 @@ __device__ __forceinline__ void rows_tile(const RowsArgs& a, int item, uint16_t*
   f32x16_t o[DB];
   float m_run, l_run;  // in units of the scaled score
 
-  const uint32_t kbase = score_base<HD>(lane), vbase = v_base<HD>(lane);
   auto load = [&](int t, uint16_t* buf) {
     const int k = (t < np ? t : t - np) * KT, n = (t < np ? kp.n : ko.n) - k;
     copy_tile<HD, KT, true>((t < np ? Kp : Ko) + (size_t)k * HD, n, buf);
@@ -264,6 +276,7 @@ again:
     const bool masked = k0 + KT > (is_own ? all : kp.n);
 
     f32x16_t st[KH];
+    const uint32_t kbase = fresh(score_base<HD>(lane));
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int kh = 0; kh < KH; ++kh)
@@ -277,6 +290,14 @@ again:
         st[kh] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[kk], st[kh], 0, 0, 0);
       }
     }
+    // reads kLead operands ahead of the products
+    __builtin_amdgcn_sched_group_barrier(0x100, kLead, 0);
+#pragma unroll
+    for (int i = 0; i < KS * KH - kLead; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, kLead, 0);
     __builtin_amdgcn_s_setprio(0);
     if (masked) {
       asm volatile("");  // a branch: as selects they ran for every tile (a third of its VALU work)
@@ -322,6 +343,7 @@ again:
       pf[tt] = __builtin_bit_cast(bf16x8_t, make_uint4(pw[0], pw[1], pw[2], pw[3]));
     }
     l_run += sum;  // this lane's keys; lane ^ 32 holds the others
+    const uint32_t vbase = fresh(v_base<HD>(lane));
 #pragma unroll
     for (int tt = 0; tt < 2 * KH; ++tt)
 #pragma unroll
@@ -472,7 +494,7 @@ __device__ __forceinline__ void rows_few(const RowsArgs& a, int item, uint16_t* 
   const uint16_t* Kp = static_cast<const uint16_t*>(own ? a.k : a.pk) + kr.row * HD;
   const uint16_t* Vp = static_cast<const uint16_t*>(own ? a.v : a.pv) + kr.row * HD;
   // keys of this split that the lane's row sees, and that every row sees
-  const int lim = hq < nr ? (own ? min(rows_seen(sq, hq / a.g) - k0, nk) : nk) : 0;
+  const int lim = hq < nr ? (own ? min(rows_seen(sq, token_of(a, hq)) - k0, nk) : nk) : 0;
   const int all = own ? min(rows_seen(sq, 0) - k0, nk) : nk;
   float* sc_row = a.sc != nullptr && own && hq < nr
                       ? a.sc + (((size_t)b * a.n_kv + j) * a.R + hq) * a.sc_ld + k0 + 4 * lg
@@ -736,18 +758,22 @@ __global__ __launch_bounds__(256, 2) void rows_bf16_kernel(RowsArgs a, int tile_
 
 // ------------------------------------------------------------------ fp32
 
-// One wave per (16-row block, key range), 16 keys at a step, on v_mfma_f32_16x16x4_f32.
+// One workgroup of 4 waves per (16-row block, key range); the range's 16-key blocks go to
+// the waves in turn, on v_mfma_f32_16x16x4_f32.
 // Scores S^T = K Q^T: lane (row lane % 16, group lg = lane / 16) holds elements 16 c + 4
 // lg .. + 3 of a key (A) and of its query row (B); MFMA e of chunk c takes element e.
 // P V: O^T = V^T P^T, step t takes the keys 4 lg + t, whose weights the lanes hold; a
 // lane's 16 bytes of V row 4 lg + t (dims 64 u + 4 (lane % 16) ..) are the A operands of
-// four MFMAs, MFMA e giving dims 64 u + 4 i + e.  No LDS.  Masked keys: score -inf;
-// a non-finite value that some row does not see is taken out of the product, and its code
-// (code_of), summed over the keys a row does see, puts it back.
+// four MFMAs, MFMA e giving dims 64 u + 4 i + e.  Both operands come straight from memory;
+// LDS only merges the waves.  Masked keys: score -inf; a non-finite value that some row does
+// not see is taken out of the product, and its code (code_of), summed over the keys a row
+// does see, puts it back.
 template <int HD>
-__global__ __launch_bounds__(64) void rows_f32_kernel(RowsArgs a) {
+__global__ __launch_bounds__(256) void rows_f32_kernel(RowsArgs a) {
   constexpr int KC = HD / 16, VU = HD / 64;
-  const int lane = threadIdx.x, rq = lane & 15, lg = lane >> 4;
+  __shared__ __align__(16) float part[3][16][HD + 4];
+  __shared__ float ml[4][16][2];
+  const int lane = threadIdx.x & 63, w = wave_id(), rq = lane & 15, lg = lane >> 4;
   const int nbo = (a.R + kRowsWave - 1) / kRowsWave;
   const int own_items = a.B * a.n_kv * nbo * a.S_own;
   const bool own = (int)blockIdx.x < own_items;
@@ -779,7 +805,7 @@ __global__ __launch_bounds__(64) void rows_f32_kernel(RowsArgs a) {
     p1 = min(p0 + a.C_prefix, a.T_prefix);
   } else {
     const int last = min(r_blk + kRowsWave, sq.n * a.g) - 1;
-    const int seen = rows_seen(sq, last / a.g);
+    const int seen = rows_seen(sq, token_of(a, last));
     const int base = a.joint ? a.T_prefix : 0;
     const long long k0 = (long long)s * a.C_own, k1 = k0 + a.C_own;
     p0 = (int)min(k0, (long long)base);
@@ -791,7 +817,7 @@ __global__ __launch_bounds__(64) void rows_f32_kernel(RowsArgs a) {
   const int np = (kp.n + 15) / 16, nt = np + (ko.n + 15) / 16;
   const int rl = r_blk + rq;
   const int fr = fr0 + min(rl, nr - 1);
-  const int lim = own && rl < nr ? min(rows_seen(sq, rl / a.g) - o0, ko.n) : 0;
+  const int lim = own && rl < nr ? min(rows_seen(sq, token_of(a, rl)) - o0, ko.n) : 0;
 
   f32x4_t q[KC];
   {
@@ -806,7 +832,7 @@ __global__ __launch_bounds__(64) void rows_f32_kernel(RowsArgs a) {
     for (int e = 0; e < 4; ++e) o[u][e] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
   float m_run = -INFINITY, l_run = 0.0f;
 
-  for (int t = 0; t < nt; ++t) {
+  for (int t = w; t < nt; t += 4) {
     const bool is_own = t >= np;
     const KeyRange& kr = is_own ? ko : kp;
     const float* K = static_cast<const float*>(is_own ? a.k : a.pk) + kr.row * HD;
@@ -894,14 +920,55 @@ __global__ __launch_bounds__(64) void rows_f32_kernel(RowsArgs a) {
   }
   l_run += __shfl_xor(l_run, 16, 64);
   l_run += __shfl_xor(l_run, 32, 64);
-  if (rl >= nr || !row_wanted(a, fr)) return;
+  // the waves' states, merged by the first in wave order.  o[u][e][r]: dim 64 u + 16 lg + 4
+  // r + e
+  if (lg == 0) {
+    ml[w][rq][0] = m_run;
+    ml[w][rq][1] = l_run;
+  }
+  if (w > 0) {
+#pragma unroll
+    for (int u = 0; u < VU; ++u)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        *reinterpret_cast<float4*>(&part[w - 1][rq][64 * u + 16 * lg + 4 * r]) =
+            make_float4(o[u][0][r], o[u][1][r], o[u][2][r], o[u][3][r]);
+  }
+  __syncthreads();
+  if (w > 0 || rl >= nr || !row_wanted(a, fr)) return;
+  float M = m_run;
+#pragma unroll
+  for (int v = 1; v < 4; ++v) M = fmaxf(M, ml[v][rq][0]);
+  const float Mu = M == -INFINITY ? 0.0f : M;
+  {
+    const float wt = exp2_hw(m_run - Mu);
+    l_run *= wt;
+#pragma unroll
+    for (int u = 0; u < VU; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[u][e] *= wt;
+  }
+#pragma unroll
+  for (int v = 1; v < 4; ++v) {
+    const float wt = exp2_hw(ml[v][rq][0] - Mu);
+    l_run = fmaf(wt, ml[v][rq][1], l_run);
+#pragma unroll
+    for (int u = 0; u < VU; ++u)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float4 y = *reinterpret_cast<const float4*>(&part[v - 1][rq][64 * u + 16 * lg + 4 * r]);
+        o[u][0][r] = fmaf(wt, y.x, o[u][0][r]);
+        o[u][1][r] = fmaf(wt, y.y, o[u][1][r]);
+        o[u][2][r] = fmaf(wt, y.z, o[u][2][r]);
+        o[u][3][r] = fmaf(wt, y.w, o[u][3][r]);
+      }
+  }
   const bool direct = a.S_prefix + a.S_own == 1;
   const size_t row = slot_row(a, slot, j, fr);
   if (lg == 0) {
-    a.ml[2 * row] = m_run == -INFINITY ? 0.0f : m_run;
+    a.ml[2 * row] = Mu;
     a.ml[2 * row + 1] = l_run;
   }
-  // o[u][e][r]: dim 64 u + 16 lg + 4 r + e
   if (direct || l_run != 0.0f) {
     float* dst = direct ? static_cast<float*>(a.out) + q_off(a, j, fr, HD) : a.acc + row * HD;
 #pragma unroll
@@ -939,38 +1006,41 @@ __device__ __forceinline__ Merge merge_states(const RowsArgs& a, int S, int j, i
   return m;
 }
 
-constexpr int kFinishRows = 4;     // merged rows per workgroup (one per wave)
 constexpr int kFinishKeys = 256;   // keys per workgroup of the streamed weights
+// Waves that share a row's states: a wave keeps 8 in flight, so that many states are many
+// round trips (512 rows of 66 states: 12.0 us with one wave per row).
+constexpr int finish_waves(int S) { return S > 8 ? 4 : 1; }
 
-// Workgroups 0 .. merge_wgs - 1 merge 4 rows each (out, and their max + log2(sum) where
-// the weights of tiles need them); the rest add up the weights of 256 own keys of one
+// Workgroups 0 .. merge_wgs - 1 merge 4 / WPR rows each (out, and their max + log2(sum)
+// where the weights of tiles need them); the rest add up the weights of 256 own keys of one
 // (b, j) from the kept scores: weight = decay weight + sum_rows 2^(score - max) / sum.
-template <typename T, int HD>
+template <typename T, int HD, int WPR>
 __global__ __launch_bounds__(256) void rows_finish_kernel(RowsArgs a, int merge_wgs) {
   constexpr int E = HD / 64;
   const int lane = threadIdx.x & 63, w = wave_id();
   const int S = a.S_prefix + a.S_own;
   if ((int)blockIdx.x < merge_wgs) {
-    const long long idx = (long long)blockIdx.x * kFinishRows + w;
+    const long long idx = (long long)blockIdx.x * (4 / WPR) + w / WPR;
     const int Rt = a.B * a.R;
-    if (idx >= (long long)Rt * a.n_kv) return;
-    const int j = (int)(idx / Rt), fr = (int)(idx - (long long)j * Rt);
-    const int tok = fr / a.g, b = tok / a.N;
-    if (tok - b * a.N >= seq_of(a, b).n) return;
+    const bool in = idx < (long long)Rt * a.n_kv;
+    const int j = in ? (int)(idx / Rt) : 0, fr = in ? (int)(idx - (long long)j * Rt) : 0;
+    const bool on = in && row_wanted(a, fr);
+    if (WPR == 1 && !on) return;
     const Merge m = merge_states(a, S, j, fr, lane);
-    if (a.lse != nullptr && lane == 0)
+    if (a.lse != nullptr && on && lane == 0 && w % WPR == 0)
       a.lse[(size_t)j * Rt + fr] = m.L != 0.0f ? m.M + __builtin_amdgcn_logf(m.L) : INFINITY;
     if (S == 1) return;  // written by the attention kernel itself
     float x[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] = 0.0f;
-    // the states that hold keys, 8 at a time in flight (an empty state has no acc)
+    // the states that hold keys (every WPR-th of them), 8 at a time in flight; an empty
+    // state has no acc
     const float* src = a.acc + slot_row(a, 0, j, fr) * HD + E * lane;
     const size_t step = (size_t)a.n_kv * Rt * HD;
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       const float wv = half == 0 ? m.w0 : m.w1;
-      unsigned long long left = __ballot(wv != 0.0f);
+      unsigned long long left = __ballot(wv != 0.0f && lane % WPR == w % WPR);
       while (left != 0) {
         float y[8][E], wt[8];
 #pragma unroll
@@ -986,10 +1056,20 @@ __global__ __launch_bounds__(256) void rows_finish_kernel(RowsArgs a, int merge_
           for (int e = 0; e < E; ++e) x[e] = wt[i] != 0.0f ? fmaf(y[i][e], wt[i], x[e]) : x[e];
       }
     }
-    const float L = m.L;
+    if constexpr (WPR > 1) {  // one row per workgroup: its waves' sums in wave order
+      __shared__ float part[WPR][HD];
+#pragma unroll
+      for (int e = 0; e < E; ++e) part[w][E * lane + e] = x[e];
+      __syncthreads();
+      if (w > 0 || !on) return;
+#pragma unroll
+      for (int v = 1; v < WPR; ++v)
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] += part[v][E * lane + e];
+    }
     T* dst = static_cast<T*>(a.out) + q_off(a, j, fr, HD) + E * lane;
 #pragma unroll
-    for (int e = 0; e < E; ++e) dst[e] = from_f<T>(L != 0.0f ? x[e] / L : 0.0f);
+    for (int e = 0; e < E; ++e) dst[e] = from_f<T>(m.L != 0.0f ? x[e] / m.L : 0.0f);
     return;
   }
   __shared__ float lse[kMaxGroup];
@@ -1078,31 +1158,53 @@ __global__ __launch_bounds__(256, 2) void weight_tile_kernel(RowsArgs a) {
           (__attribute__((address_space(3))) void*)(dst + 8 * (64 * w + 256 * i)), 16, 0, 0);
     }
   };
+  // max + log2(sum) of the lane's two rows of a tile, loaded a tile ahead and before that
+  // tile's copies (a load is waited for with everything issued before it); rows past the
+  // part get +inf, weight 0
+  const float* lse_row = a.lse + (size_t)j * a.B * a.R + fr0;
+  float lse_next[2];
+  auto load_lse = [&](int t) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int r = rs.r0 + t * kWtRows + 32 * h + (lane & 31);
+      lse_next[h] = lse_row[min(r, rs.r1 - 1)];
+      if (r >= rs.r1) lse_next[h] = INFINITY;
+    }
+  };
   auto step = [&](int t, const uint16_t* qs, uint16_t* next) {
     __builtin_amdgcn_s_waitcnt(0x0f70);
     __syncthreads();
-    if (t + 1 < nt) load(t + 1, next);
+    const float lse[2] = {lse_next[0], lse_next[1]};
+    if (t + 1 < nt) {
+      load_lse(t + 1);
+      load(t + 1, next);
+    }
+    // whether every row of the tile sees every key of the workgroup
+    const int first = rs.r0 + t * kWtRows;
+    const bool masked = rows_seen(sq, token_of(a, first)) < k0 + kWtKeys;
 #pragma unroll
     for (int h = 0; h < kWtRows / 32; ++h) {
-      const int row = 32 * h + (lane & 31), r = rs.r0 + t * kWtRows + row;
       f32x16_t st;
 #pragma unroll
       for (int i = 0; i < 16; ++i) st[i] = 0.0f;
-      const float lse = r < rs.r1 ? a.lse[(size_t)j * a.B * a.R + fr0 + r] : INFINITY;
-      const int lim = r < rs.r1 ? rows_seen(sq, r / a.g) - k0 - 32 * w : 0;  // keys of the wave that the row sees
 #pragma unroll
-      for (int i = 0; i < KS; ++i) {
-        const bf16x8_t qf = score_operand(qs, qbase, i, 64 * HD * h);
-        st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], qf, st, 0, 0, 0);
+      for (int i = 0; i < KS; ++i)
+        st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], score_operand(qs, qbase, i, 64 * HD * h), st, 0, 0, 0);
+      float p[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) p[i] = exp2_hw(fmaf(st[i], ScoreScale<HD>::v, -lse[h]));
+      if (masked) {
+        asm volatile("");
+        const int r = first + 32 * h + (lane & 31);
+        const int lim = r < rs.r1 ? rows_seen(sq, token_of(a, r)) - k0 - 32 * w : 0;  // keys of the wave that the row sees
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p[i] = 8 * (i >> 2) + 4 * hl + (i & 3) < lim ? p[i] : 0.0f;
       }
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int key = 8 * (i >> 2) + 4 * hl + (i & 3);
-        const float p = exp2_hw(fmaf(st[i], ScoreScale<HD>::v, -lse));
-        sum[i] += key < lim ? p : 0.0f;
-      }
+      for (int i = 0; i < 16; ++i) sum[i] += p[i];
     }
   };
+  if (nt > 0) load_lse(0);
   if (nt > 0) load(0, q_a);
   for (int t = 0; t < nt; t += 2) {
     step(t, q_a, q_b);
@@ -1149,7 +1251,7 @@ __global__ __launch_bounds__(64) void weight_f32_kernel(RowsArgs a) {
       }
     }
     const float lse = r < rs.r1 ? a.lse[(size_t)j * a.B * a.R + fr] : INFINITY;
-    const int lim = r < rs.r1 ? rows_seen(sq, r / a.g) - k0 : 0;
+    const int lim = r < rs.r1 ? rows_seen(sq, token_of(a, r)) - k0 : 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const float p = exp2_hw((s0[i] + s1[i]) * ScoreScale<HD>::v - lse);
@@ -1197,15 +1299,19 @@ static hipError_t launch_rows_t(const RowsArgs& a, hipStream_t st) {
     hipLaunchKernelGGL(rows_bf16_kernel<HD>, dim3((unsigned)(tile_items + few_items)), dim3(256), 0, st, a,
                        (int)tile_items);
   else
-    hipLaunchKernelGGL(rows_f32_kernel<HD>, dim3((unsigned)tile_items), dim3(64), 0, st, a);
+    hipLaunchKernelGGL(rows_f32_kernel<HD>, dim3((unsigned)tile_items), dim3(256), 0, st, a);
   KVD_LAUNCH_TRY(hipGetLastError());
   const int S = S_prefix + a.S_own;
   const bool sums = a.weight != nullptr && a.T_own > 0;
   const long long rows = (long long)a.B * a.R * a.n_kv;
-  const int merge_wgs = S > 1 || a.lse != nullptr ? (int)((rows + kFinishRows - 1) / kFinishRows) : 0;
+  const int per = 4 / finish_waves(S);  // merged rows per workgroup
+  const int merge_wgs = S > 1 || a.lse != nullptr ? (int)((rows + per - 1) / per) : 0;
   const int weight_wgs = sums && a.sc != nullptr ? a.B * a.n_kv * ((a.T_own + kFinishKeys - 1) / kFinishKeys) : 0;
   if (merge_wgs + weight_wgs > 0) {
-    hipLaunchKernelGGL((rows_finish_kernel<T, HD>), dim3(merge_wgs + weight_wgs), dim3(256), 0, st, a, merge_wgs);
+    if (finish_waves(S) == 4)
+      hipLaunchKernelGGL((rows_finish_kernel<T, HD, 4>), dim3(merge_wgs + weight_wgs), dim3(256), 0, st, a, merge_wgs);
+    else
+      hipLaunchKernelGGL((rows_finish_kernel<T, HD, 1>), dim3(merge_wgs + weight_wgs), dim3(256), 0, st, a, merge_wgs);
     KVD_LAUNCH_TRY(hipGetLastError());
   }
   if (sums && a.sc == nullptr) {
