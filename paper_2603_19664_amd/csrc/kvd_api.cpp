@@ -880,7 +880,8 @@ namespace {
 // bf16 rows stream their keys while one MFMA column block (16) holds them, else share
 // 128-row tiles; fp32 to waves of 16 rows.  A sequence whose own rows fill half
 // a block takes prefix and own keys in one pass (joint): the prefix is then shared by
-// its own rows, and neither half leaves a partial state.
+// its own rows, and neither half leaves a partial state.  So do calls of few rows and at most
+// kRowsSmall keys, which then take one launch.
 struct RowsPlan {
   int32_t R, joint, prefix_few, own_few, S_prefix, C_prefix, S_own, C_own, S_w, sc_ld;
   size_t ml, acc, lse, sc, wpart, end;  // byte offsets in the workspace
@@ -921,10 +922,12 @@ bool rows_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T_prefix, 
   const long long keys = (long long)T_prefix + T_own;
   if (Rt * s->n_kv_heads > INT32_MAX || Rt >= 1ll << 28 || keys > INT32_MAX - 1024 || units > INT32_MAX) return false;
   p->R = (int32_t)R;
-  p->joint = T_prefix > 0 && T_own > 0 && R >= RB / 2;
+  const bool small = keys <= kvd::kRowsSmall;
+  p->joint = T_prefix > 0 && T_own > 0 && (R >= RB / 2 || (small && (!bf || R <= kvd::kRowsFew)));
   const long long nbo = (R + RB - 1) / RB, nbp = (Rt + RB - 1) / RB;
   if (p->joint) {
-    p->S_own = row_slots(units * nbo, keys, least, false);
+    p->own_few = bf && R <= kvd::kRowsFew;
+    p->S_own = small ? 1 : row_slots(units * nbo, keys, least, false);
     p->C_own = slot_keys(keys, p->S_own);
     p->items = units * nbo * p->S_own;
   } else {

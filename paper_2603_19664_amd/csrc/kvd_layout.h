@@ -398,6 +398,7 @@ constexpr int kRowsLeastKeys = 128;     // keys per slot, at least (bf16)
 constexpr int kRowsLeastKeysF32 = 128;
 constexpr int kRowsSlotKeys = 512;   // a slot's fixed cost in keys
 constexpr int kRowsMostSlots = 64;
+constexpr int kRowsSmall = 256;  // keys that one workgroup takes at once
 
 // Value-absorbed fused attention (AbsorbArgs; head_dim 256).  Score tiles: K rows
 // x tokens per workgroup.

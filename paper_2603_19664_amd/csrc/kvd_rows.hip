@@ -183,7 +183,7 @@ __device__ __forceinline__ void rows_tile(const RowsArgs& a, int item, uint16_t*
     const int units = a.B * a.n_kv, x = item / units, u = item - x * units;
     j = u % a.n_kv;
     b = u / a.n_kv;
-    s = x % a.S_own;
+    s = (x + x / a.S_own) % a.S_own;  // from another slot in every block: XCDs (item % 8) share early and late keys
     blk = nbo - 1 - x / a.S_own;  // the last rows see the most keys: first
   } else {
     item -= own_items;
@@ -395,6 +395,8 @@ again:
   if (hl == 0) {
     a.ml[2 * row] = m_out;
     a.ml[2 * row + 1] = l_run;
+    if (direct && a.lse != nullptr)
+      a.lse[(size_t)j * a.B * a.R + fr] = l_run != 0.0f ? m_out + __builtin_amdgcn_logf(l_run) : INFINITY;
   }
   if (direct) {
     const float inv = l_run != 0.0f ? 1.0f / l_run : 0.0f;
@@ -455,7 +457,8 @@ __device__ __forceinline__ void wait_copies() {
 }
 
 // One workgroup of 4 waves per (unit, split): units 0 .. B n_kv - 1 are the own rows of (b,
-// j) in S_own splits, the rest the prefix of KV head j in S_prefix splits.  A split's 16-key
+// j) in S_own splits (of a joint call all keys, prefix and own, at once), the rest the prefix
+// of KV head j in S_prefix splits.  A split's 16-key
 // blocks go to the waves in turn, and each wave streams its own through its own slice of
 // LDS, with no barrier: HBM-bound, so what matters is loads in flight (head_dim 256: K and
 // V of one block, K refilled as soon as the scores are taken, V after its product; smaller
@@ -484,18 +487,23 @@ __device__ __forceinline__ void rows_few(const RowsArgs& a, int item, uint16_t* 
   Seq sq{0, 0};
   if (own) sq = seq_of(a, b);
   if (own && sq.n == 0) return;  // no row of this sequence is asked for
+  // the split's keys: of the prefix (a prefix unit's split; all of a joint call's), then of
+  // the sequence's own rows
   const int T = own ? sq.len : a.T_prefix;
   const int nblk_all = (T + kSaBlock - 1) / kSaBlock;
   const int k0 = kSaBlock * sa_first_block(s, nblk_all, S);
-  const int nk = min(T, kSaBlock * sa_first_block(s + 1, nblk_all, S)) - k0;  // keys of this split
-  const int nblk = nk > 0 ? (nk + kSaBlock - 1) / kSaBlock : 0;
+  const int nk = max(min(T, kSaBlock * sa_first_block(s + 1, nblk_all, S)) - k0, 0);
+  const KeyRange kp = own ? prefix_range(a, j, 0, a.joint ? a.T_prefix : 0) : prefix_range(a, j, k0, k0 + nk);
+  const KeyRange ko = own ? own_range(a, b, j, k0, k0 + nk) : KeyRange{0, 0};
+  const int pblk = (kp.n + kSaBlock - 1) / kSaBlock, nblk = pblk + (ko.n + kSaBlock - 1) / kSaBlock;
   const int nb = nblk > w ? (nblk - 1 - w) / NW + 1 : 0;  // this wave's blocks: w, w + NW, ..
-  const KeyRange kr = own ? own_range(a, b, j, k0, k0 + nk) : prefix_range(a, j, k0, k0 + nk);
-  const uint16_t* Kp = static_cast<const uint16_t*>(own ? a.k : a.pk) + kr.row * HD;
-  const uint16_t* Vp = static_cast<const uint16_t*>(own ? a.v : a.pv) + kr.row * HD;
-  // keys of this split that the lane's row sees, and that every row sees
-  const int lim = hq < nr ? (own ? min(rows_seen(sq, token_of(a, hq)) - k0, nk) : nk) : 0;
-  const int all = own ? min(rows_seen(sq, 0) - k0, nk) : nk;
+  const uint16_t* Kp = static_cast<const uint16_t*>(a.pk) + kp.row * HD;
+  const uint16_t* Vp = static_cast<const uint16_t*>(a.pv) + kp.row * HD;
+  const uint16_t* Ko = static_cast<const uint16_t*>(a.k) + ko.row * HD;
+  const uint16_t* Vo = static_cast<const uint16_t*>(a.v) + ko.row * HD;
+  // own keys of this split that the lane's row sees, and that every row sees
+  const int lim = hq < nr && own ? min(rows_seen(sq, token_of(a, hq)) - k0, ko.n) : 0;
+  const int all = own ? min(rows_seen(sq, 0) - k0, ko.n) : 0;
   float* sc_row = a.sc != nullptr && own && hq < nr
                       ? a.sc + (((size_t)b * a.n_kv + j) * a.R + hq) * a.sc_ld + k0 + 4 * lg
                       : nullptr;
@@ -503,12 +511,14 @@ __device__ __forceinline__ void rows_few(const RowsArgs& a, int item, uint16_t* 
   uint16_t* const sl0 = buf0 + SLICE * w;
   uint16_t* const sl1 = buf1 + SLICE * w;
   auto load_k = [&](int i, uint16_t* dst) {
-    const int kb = kSaBlock * (w + NW * i);
-    copy16<HD, true>(Kp + (size_t)kb * HD, nk - kb, dst);
+    const int x = w + NW * i;
+    const int kb = kSaBlock * (x < pblk ? x : x - pblk), n = x < pblk ? kp.n : ko.n;
+    copy16<HD, true>((x < pblk ? Kp : Ko) + (size_t)kb * HD, n - kb, dst);
   };
   auto load_v = [&](int i, uint16_t* dst) {
-    const int kb = kSaBlock * (w + NW * i);
-    copy16<HD, false>(Vp + (size_t)kb * HD, nk - kb, dst);
+    const int x = w + NW * i;
+    const int kb = kSaBlock * (x < pblk ? x : x - pblk), n = x < pblk ? kp.n : ko.n;
+    copy16<HD, false>((x < pblk ? Vp : Vo) + (size_t)kb * HD, n - kb, dst);
   };
   // every LDS read of the wave is done: its slice may be written again
   auto reads_done = [&]() {
@@ -562,8 +572,10 @@ again:
   // compiler wait for V before K was read
   auto step = [&](auto next, int i, uint16_t* ks, uint16_t* vs) {
     constexpr bool NEXT = decltype(next)::value != 0;
-    const int kb = kSaBlock * (w + NW * i);
-    const bool masked = kb + kSaBlock > all;
+    const bool is_own = w + NW * i >= pblk;
+    const int kb = kSaBlock * (w + NW * i - (is_own ? pblk : 0));
+    const int row_lim = is_own ? lim : kp.n;
+    const bool masked = kb + kSaBlock > (is_own ? all : kp.n);
     // this block's K (head_dim 256; V was issued after it), or K and V (the next block's
     // were): copies complete in order
     if (ONE || i + 1 < nb)
@@ -585,10 +597,11 @@ again:
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       sv[r] = st[r] * ScoreScale<HD>::v;
-      if (masked) sv[r] = kb + 4 * lg + r < lim ? sv[r] : -INFINITY;
+      if (masked) sv[r] = kb + 4 * lg + r < row_lim ? sv[r] : -INFINITY;
       mx = fmaxf(mx, sv[r]);
     }
-    if (sc_row != nullptr && pass == 0) *reinterpret_cast<float4*>(sc_row + kb) = make_float4(sv[0], sv[1], sv[2], sv[3]);
+    if (sc_row != nullptr && is_own && pass == 0)
+      *reinterpret_cast<float4*>(sc_row + kb) = make_float4(sv[0], sv[1], sv[2], sv[3]);
     mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
     const bool grow = mx > m_run + 8.0f;
@@ -670,11 +683,12 @@ again:
     // the values that pass 1 took as 0 in masked blocks, for the rows that see them
 #pragma unroll 1
     for (int i = 0; i < nb; ++i) {
-      const int kb = kSaBlock * (w + NW * i);
-      if (kb + kSaBlock <= all) continue;
+      const bool is_own = w + NW * i >= pblk;
+      const int kb = kSaBlock * (w + NW * i - (is_own ? pblk : 0));
+      if (kb + kSaBlock <= (is_own ? all : kp.n)) continue;
 #pragma unroll 1
-      for (int t = kb; t < min(kb + kSaBlock, lim); ++t) {
-        const uint16_t* vr = Vp + (size_t)t * HD + 4 * lg;
+      for (int t = kb; t < min(kb + kSaBlock, is_own ? lim : kp.n); ++t) {
+        const uint16_t* vr = (is_own ? Vo : Vp) + (size_t)t * HD + 4 * lg;
 #pragma unroll
         for (int db = 0; db < DB; ++db) {
           const uint2 y = *reinterpret_cast<const uint2*>(vr + 16 * db);
@@ -782,7 +796,7 @@ __global__ __launch_bounds__(256) void rows_f32_kernel(RowsArgs a) {
     const int units = a.B * a.n_kv, x = (int)blockIdx.x / units, u = (int)blockIdx.x - x * units;
     j = u % a.n_kv;
     b = u / a.n_kv;
-    s = x % a.S_own;
+    s = (x + x / a.S_own) % a.S_own;  // from another slot in every block: XCDs (item % 8) share early and late keys
     blk = nbo - 1 - x / a.S_own;
   } else {
     const int item = (int)blockIdx.x - own_items, units = a.n_kv * a.S_prefix;
@@ -968,6 +982,8 @@ __global__ __launch_bounds__(256) void rows_f32_kernel(RowsArgs a) {
   if (lg == 0) {
     a.ml[2 * row] = Mu;
     a.ml[2 * row + 1] = l_run;
+    if (direct && a.lse != nullptr)
+      a.lse[(size_t)j * a.B * a.R + fr] = l_run != 0.0f ? Mu + __builtin_amdgcn_logf(l_run) : INFINITY;
   }
   if (direct || l_run != 0.0f) {
     float* dst = direct ? static_cast<float*>(a.out) + q_off(a, j, fr, HD) : a.acc + row * HD;
@@ -1029,7 +1045,6 @@ __global__ __launch_bounds__(256) void rows_finish_kernel(RowsArgs a, int merge_
     const Merge m = merge_states(a, S, j, fr, lane);
     if (a.lse != nullptr && on && lane == 0 && w % WPR == 0)
       a.lse[(size_t)j * Rt + fr] = m.L != 0.0f ? m.M + __builtin_amdgcn_logf(m.L) : INFINITY;
-    if (S == 1) return;  // written by the attention kernel itself
     float x[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] = 0.0f;
@@ -1305,7 +1320,7 @@ static hipError_t launch_rows_t(const RowsArgs& a, hipStream_t st) {
   const bool sums = a.weight != nullptr && a.T_own > 0;
   const long long rows = (long long)a.B * a.R * a.n_kv;
   const int per = 4 / finish_waves(S);  // merged rows per workgroup
-  const int merge_wgs = S > 1 || a.lse != nullptr ? (int)((rows + per - 1) / per) : 0;
+  const int merge_wgs = S > 1 ? (int)((rows + per - 1) / per) : 0;
   const int weight_wgs = sums && a.sc != nullptr ? a.B * a.n_kv * ((a.T_own + kFinishKeys - 1) / kFinishKeys) : 0;
   if (merge_wgs + weight_wgs > 0) {
     if (finish_waves(S) == 4)

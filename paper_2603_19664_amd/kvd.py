@@ -505,33 +505,35 @@ def _dims(t, name, want):
 
 
 def _dev_ptr(t, name, dtype, dev):
-    """t's pointer, once its device, dtype and layout are checked (None for None)."""
+    """t's pointer, once its device (an index), dtype and layout are checked (None for None)."""
     if t is None:
         return None
-    if t.device != dev:
-        if t.device.type != "cuda":
-            raise ValueError(f"{name} must be a torch tensor on the GPU")
-        raise ValueError(f"{name} is on {t.device}, q or k on {dev}")
+    if t.get_device() == dev and t.dtype is dtype and t.is_contiguous():
+        return t.data_ptr()
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} must be a torch tensor on the GPU")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, q or k on cuda:{dev}")
     if t.dtype is not dtype:
         raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return t.data_ptr()
+    raise ValueError(f"{name} must be contiguous")
 
 
 def _device_of(t, name):
     if t.device.type != "cuda":
         raise ValueError(f"{name} must be a torch tensor on the GPU")
-    return t.device
+    return t.get_device()
 
 
 def _run_on(dev, fn, *args):
-    """fn(*args, stream) on device dev and its current stream."""
-    i = dev.index
-    if torch.cuda.current_device() == i:
-        return _check(fn(*args, torch._C._cuda_getCurrentRawStream(i)))
-    with torch.cuda.device(i):
-        _check(fn(*args, torch._C._cuda_getCurrentRawStream(i)))
+    """fn(*args, stream) on device `dev` (an index) and its current stream."""
+    if torch._C._cuda_getDevice() == dev:
+        st = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
+    else:
+        with torch.cuda.device(dev):
+            st = fn(*args, torch._C._cuda_getCurrentRawStream(dev))
+    if st != KVD_OK:
+        raise KvdError(st, last_error())
 
 
 def _own_dims(k, v, name, B, shape, T, t_off):
