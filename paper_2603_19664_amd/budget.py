@@ -31,6 +31,11 @@ Memory per layer and sequence: (T - B) evicted residuals plus B cached K/V
 entries (Eq. total_mem per layer), plus what Algorithm 1 holds beside them and
 the equation leaves out: the current token's K_t / V_t (the ring's extra slot)
 and the residuals of the B cached tokens, kept for their eviction.
+
+WeightedCache bounds the cache by attention weight instead of age: it keeps the rows
+that received the most (the paper's comparison systems that score cached tokens by
+accumulated attention, Sec. 4), drops the others for good and recomputes nothing.  The
+batch may share a prefix, whose keys and values are stored once and never evicted.
 """
 from __future__ import annotations
 
@@ -136,3 +141,104 @@ class BoundedCache:
                                      self.ws, self.ring_k, self.ring_v, st.tail_rows(), st.head)  # RECOMPUTE+ATTN
         st.advance()                                                                             # EVICT_OLDEST
         return self.q
+
+
+class WeightedCache:
+    """One layer's stored K/V for `batch` sequences decoded in lockstep, held at `budget` rows per (sequence, KV
+    head) by accumulated attention weight.
+
+    Rows past the budget collect in `room` further slots (the tokens of one call at most); then kvd_evict keeps the
+    `budget` heaviest: the first `sink` positions and the newest `recent` ones always, the others by the weight
+    that kvd_prefix_attn has added up, `decay` times the earlier weight at every call (1: over the whole past, 0: the
+    last call's alone).  Slots are reused, so row order says nothing about age; pos holds every row's position.
+
+    prefix: (K, V) of [n_kv, T_prefix, head_dim], shared by the batch: its tokens sit at positions pos0 ..
+    pos0 + T_prefix - 1 of every sequence, the sequences' own from pos0 + T_prefix on.
+    """
+
+    def __init__(self, shape, batch: int, budget: int, room: int = 1, prefix=None, sink: int = 0, recent: int = 0,
+                 decay: float = 1.0, pos0: int = 0, device="cuda"):
+        import torch
+
+        from . import kvd
+        if budget < 1 or room < 1:
+            raise ValueError("budget and room must be >= 1")
+        if sink < 0 or recent < 0 or sink + recent > budget:
+            raise ValueError(f"sink={sink} and recent={recent} rows do not fit a budget of {budget}")
+        self.kvd, self.torch = kvd, torch
+        self.shape, self.B, self.budget, self.room = shape, batch, budget, room
+        self.sink, self.recent, self.decay, self.pos0 = sink, recent, decay, pos0
+        self.prefix_k, self.prefix_v = prefix if prefix is not None else (None, None)
+        self.T_prefix = 0 if prefix is None else self.prefix_k.shape[1]
+        dt, dev, cap = shape.torch_dtype, device, budget + room
+        self.k = torch.zeros((batch, shape.n_kv_heads, cap, shape.head_dim), dtype=dt, device=dev)
+        self.v = torch.zeros_like(self.k)
+        self.weight = torch.zeros((batch, shape.n_kv_heads, cap), dtype=torch.float32, device=dev)
+        self.pos = torch.zeros((batch, shape.n_kv_heads, cap), dtype=torch.int32, device=dev)
+        self.last_pos = torch.zeros((batch,), dtype=torch.int32, device=dev)
+        self.n = 0   # rows held
+        self.T = 0   # tokens seen
+        sizes = [kvd.kvd_evict_workspace_bytes(shape, batch, cap)] if batch else []
+        sizes += [kvd.kvd_prefix_workspace_bytes(shape, batch, n, self.T_prefix, cap, True)
+                  for n in sorted({1, room}) if batch]
+        self.ws = torch.empty(max(sizes, default=256), dtype=torch.uint8, device=dev)
+        self._ws_tokens = {1, room}
+
+    def _positions(self, N):
+        """Positions of the N tokens being added, [B, N] int32."""
+        t = self.torch.arange(self.T, self.T + N, dtype=self.torch.int32, device=self.k.device)
+        return (t + (self.pos0 + self.T_prefix)).expand(self.B, N).contiguous()
+
+    def _attend(self, q, N, out):
+        kvd = self.kvd
+        if N not in self._ws_tokens:
+            need = kvd.kvd_prefix_workspace_bytes(self.shape, self.B, N, self.T_prefix, self.budget + self.room, True)
+            if need > self.ws.numel():
+                self.ws = self.torch.empty(need, dtype=self.torch.uint8, device=self.k.device)
+            self._ws_tokens.add(N)
+        self.pos[:, :, self.n:self.n + N] = self.torch.arange(self.T, self.T + N, device=self.k.device)
+        self.last_pos.fill_(self.T + N - 1)
+        self.n += N
+        self.T += N
+        kvd.kvd_prefix_attn(self.shape, q, self.prefix_k, self.prefix_v, self.T_prefix, self.k, self.v, self.n, out,
+                            self.ws, weight=self.weight, decay=self.decay)
+
+    def evict(self):
+        """Back to the budget, if there is more."""
+        if self.n > self.budget:
+            self.kvd.kvd_evict(self.shape, self.k, self.v, self.n, self.budget, self.weight, self.ws, pos=self.pos,
+                               last_pos=self.last_pos, sink=self.sink, recent=self.recent)
+            self.n = self.budget
+
+    def step(self, h_new, gamma, w_q, w_k, w_v, out):
+        """Decode one token per sequence: h_new [batch, d] is its residual h^(l); out [batch, n_q, hd].  Returns q."""
+        s = self.shape
+        if self.n + 1 > self.budget + self.room:
+            self.evict()
+        q = self.torch.empty((self.B, s.n_q_heads, s.head_dim), dtype=s.torch_dtype, device=self.k.device)
+        self.kvd.kvd_project_qkv(s, h_new, gamma, w_q, w_k, w_v, self._positions(1).view(self.B), q, self.k, self.v,
+                                 self.n)
+        self._attend(q, 1, out)
+        if self.n == self.budget + self.room:
+            self.evict()
+        return q
+
+    def prompt(self, h, gamma, w_q, w_k, w_v, out):
+        """Take in the tokens of h [batch, T, d], at most `room` at a time, each chunk attended (causally) to what
+        the cache holds and evicted down to the budget; out [batch, T, n_q, hd].  Returns q."""
+        s, torch, kvd = self.shape, self.torch, self.kvd
+        B, T = h.shape[0], h.shape[1]
+        q = torch.empty((B, T, s.n_q_heads, s.head_dim), dtype=s.torch_dtype, device=self.k.device)
+        for t in range(0, T, self.room):
+            self.evict()
+            N = min(self.room, T - t)
+            x, pos = h[:, t:t + N].contiguous(), self._positions(N)
+            qc = torch.empty((B, N, s.n_q_heads, s.head_dim), dtype=s.torch_dtype, device=self.k.device)
+            kvd.kvd_project_q(s, x.view(B * N, s.d_model), gamma, w_q, pos.view(B * N),
+                              qc.view(B * N, s.n_q_heads, s.head_dim))
+            kvd.kvd_recompute_kv(s, x, gamma, w_k, w_v, pos[:, 0].contiguous(), N, self.k, self.v, self.n)
+            oc = torch.empty_like(qc)
+            self._attend(qc, N, oc)
+            q[:, t:t + N], out[:, t:t + N] = qc, oc
+        self.evict()
+        return q
