@@ -881,7 +881,7 @@ namespace {
 // 128-row tiles; fp32 to waves of 16 rows.  A sequence whose own rows fill half
 // a block takes prefix and own keys in one pass (joint): the prefix is then shared by
 // its own rows, and neither half leaves a partial state.  So do calls of few rows and at most
-// kRowsSmall keys, which then take one launch.
+// kRowsSmall keys; a range of that many keys is one slot, and the call one launch.
 struct RowsPlan {
   int32_t R, joint, prefix_few, own_few, S_prefix, C_prefix, S_own, C_own, S_w, sc_ld;
   size_t ml, acc, lse, sc, wpart, end;  // byte offsets in the workspace
@@ -934,14 +934,14 @@ bool rows_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T_prefix, 
     if (T_prefix > 0) {
       p->prefix_few = bf && Rt <= kvd::kRowsFew;
       const long long u = p->prefix_few ? s->n_kv_heads : s->n_kv_heads * nbp;
-      p->S_prefix = row_slots(u, T_prefix, least, false);
+      p->S_prefix = small && T_own == 0 ? 1 : row_slots(u, T_prefix, least, false);
       p->C_prefix = slot_keys(T_prefix, p->S_prefix);
       p->items += u * p->S_prefix;
     }
     if (T_own > 0) {
       p->own_few = bf && R <= kvd::kRowsFew;
       const long long u = p->own_few ? units : units * nbo;
-      p->S_own = causal_slots(u, T_own, least, N);
+      p->S_own = small && T_prefix == 0 ? 1 : causal_slots(u, T_own, least, N);
       p->C_own = slot_keys(T_own, p->S_own);
       p->items += u * p->S_own;
     }
@@ -956,7 +956,7 @@ bool rows_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T_prefix, 
   p->ml = take(8 * S * rows);
   p->acc = take(S > 1 ? 4 * S * rows * s->head_dim : 0);
   if (weights && T_own > 0) {
-    if (p->own_few) {
+    if (R <= kvd::kRowsFew) {  // the scores are kept
       p->sc_ld = (T_own + 15) / 16 * 16;
       p->sc = take(4 * (size_t)units * R * p->sc_ld);
       p->items = std::max(p->items, (long long)rows + units * ((T_own + 255) / 256));
@@ -1025,7 +1025,7 @@ kvd_status rows_call(const kvd_attn_shape* shape, const void* q, int32_t N, cons
   a.ml = reinterpret_cast<float*>(base + p.ml);
   a.acc = reinterpret_cast<float*>(base + p.acc);
   if (weight != nullptr) {
-    if (p.own_few) {
+    if (p.R <= kvd::kRowsFew) {
       a.sc = reinterpret_cast<float*>(base + p.sc);
     } else {
       a.lse = reinterpret_cast<float*>(base + p.lse);

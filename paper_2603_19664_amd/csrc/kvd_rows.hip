@@ -779,7 +779,8 @@ __global__ __launch_bounds__(256, 2) void rows_bf16_kernel(RowsArgs a, int tile_
 // P V: O^T = V^T P^T, step t takes the keys 4 lg + t, whose weights the lanes hold; a
 // lane's 16 bytes of V row 4 lg + t (dims 64 u + 4 (lane % 16) ..) are the A operands of
 // four MFMAs, MFMA e giving dims 64 u + 4 i + e.  Both operands come straight from memory;
-// LDS only merges the waves.  Masked keys: score -inf; a non-finite value that some row does
+// LDS only merges the waves.  With a.sc (at most 16 rows) the scores of own keys are kept
+// for the weights.  Masked keys: score -inf; a non-finite value that some row does
 // not see is taken out of the product, and its code (code_of), summed over the keys a row
 // does see, puts it back.
 template <int HD>
@@ -880,6 +881,12 @@ __global__ __launch_bounds__(256) void rows_f32_kernel(RowsArgs a) {
       unseen |= !in;
       sv[r] = in ? (s0[r] + s1[r]) * ScoreScale<HD>::v : -INFINITY;
       mx = fmaxf(mx, sv[r]);
+    }
+    if (a.sc != nullptr && is_own && rl < nr) {
+      float* sc = a.sc + (((size_t)b * a.n_kv + j) * a.R + rl) * a.sc_ld + o0 + k0 + 4 * lg;
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (k0 + 4 * lg + r < ko.n) sc[r] = sv[r];
     }
     mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
