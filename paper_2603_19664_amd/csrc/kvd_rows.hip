@@ -349,20 +349,18 @@ again:
 #pragma unroll
       for (int db = 0; db < DB; ++db)
         o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand<HD>(vs, vbase, 16 * tt, db), pf[tt], o[db], 0, 0, 0);
-    if (masked && pass == 0) {
-      uint32_t nf = 0;
-#pragma unroll 1
-      for (int i = lane; i < KT * HD / 8; i += 64) {
-        const uint4 x = *reinterpret_cast<const uint4*>(vs + 8 * i);
-        nf |= nonfinite2(x.x) | nonfinite2(x.y) | nonfinite2(x.z) | nonfinite2(x.w);
-      }
-      odd |= __any(nf != 0);
-    }
   };
   if (nt > 0) load(0, buf0);
   for (int t = 0; t < nt; t += 2) {
     step(t, buf0, buf1);
     if (t + 1 < nt) step(t + 1, buf1, buf0);
+  }
+  // O holds no infinity or NaN unless V did
+  if (pass == 0) {
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) odd |= !(fabsf(o[db][i]) < INFINITY);
   }
   if (pass == 0 && __syncthreads_or(odd)) {
     pass = 1;
@@ -626,16 +624,13 @@ again:
     const uint2 pl = make_uint2(pack_bf16x2(lo[0], lo[1]), pack_bf16x2(lo[2], lo[3]));
     const s16x4_t pfh = __builtin_bit_cast(s16x4_t, ph), pfl = __builtin_bit_cast(s16x4_t, pl);
     if constexpr (ONE) wait_copies<NEXT ? KC : 0>();  // V; the next block's K was issued after it
-    if (masked) {
-      uint32_t nf = 0;
+    if (masked && pass == 1) {
 #pragma unroll 1
       for (int x = lane; x < 16 * HD / 2; x += 64) {
         uint32_t* at = reinterpret_cast<uint32_t*>(vs) + x;
         const uint32_t f = nonfinite2(*at);
-        nf |= f;
-        if (pass == 1 && f != 0) *at &= (f & 0x8000u ? 0u : 0xffffu) | (f & 0x80000000u ? 0u : 0xffff0000u);
+        if (f != 0) *at &= (f & 0x8000u ? 0u : 0xffffu) | (f & 0x80000000u ? 0u : 0xffff0000u);
       }
-      odd |= pass == 0 && __any(nf != 0);
     }
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
@@ -664,7 +659,13 @@ again:
       if (i + 1 < nb) step(IC<0>{}, i + 1, sl1, sl1 + SLICE / 2);
     }
   }
-  if (pass == 0 && odd) {
+  if (pass == 0) {
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) odd |= !(fabsf(o[db][e]) < INFINITY);
+  }
+  if (pass == 0 && __any(odd)) {
     pass = 1;
     if constexpr (ONE) {
       load_k(0, sl0);
