@@ -4,9 +4,8 @@
 //   evict_one_kernel     keep = T - 1, a decode step's call: the lightest row of each
 //                        cache, and the move of its last one, in one launch.
 //   evict_select_kernel  otherwise, one workgroup per (b, j): the rows' ranks, the rank of
-//                        the last row kept, and who moves where; weights and positions
-//                        are moved here.
-//   evict_move_kernel    then the K and V rows.
+//                        the last row kept, and who moves where.
+//   evict_move_kernel    then the moves themselves.
 //
 // Kept rows in slots >= n' move into the freed slots < n', both in slot order: sources
 // and destinations are disjoint sets, so the copies need no order, and no fewer rows
@@ -60,58 +59,77 @@ constexpr int kEvictBins = 2 * kNtEvict;
 // The rank of the last row kept: each pass spreads the ranks that can still be it, [lo,
 // hi], over 2048 equal bins (a first pass over the ranks that occur, so that weights of
 // like size do not share a bin, whose counter they would take turns at; protected and
-// NaN rows are counted apart) and goes on with the bin that holds it.  At most three
-// passes.  Then rows are taken thread by thread in slot order: c consecutive slots each, c
+// NaN rows are counted apart) and goes on with the bin that holds it, at most three times;
+// a bin of up to 64 rows (the first one as a rule) is settled by one wave that compares
+// them.  Then rows are taken thread by thread in slot order: c consecutive slots each, c
 // odd (LDS banks), one prefix sum for the rows that tie with the last rank and one for
-// freed slots and movers.  KEYS: ranks that fit in LDS; 0: they stay in the workspace.
-// 8 x 2 caches of 8192 .. 16385 rows to 2048: 88 us with 8-bit digits of the whole rank and
-// serial bin walks.
-template <int KEYS>
+// freed slots and movers.  Latency-bound: a thread keeps the ranks of its PER rows (t, t +
+// 1024, ..) in registers, all its loads in flight at once, and LDS turns them into slot
+// order.  PER = 0: any length, ranks in the workspace.  16 caches of 8192 .. 16385 rows to
+// 2048: 88 us with 8-bit digits of the whole rank and serial bin walks, 28 us with ranks
+// read from LDS in every pass and four loads in flight, 26 us with three passes always,
+// 23 us so.
+template <int PER>
 __global__ __launch_bounds__(kNtEvict) void evict_select_kernel(EvictArgs a) {
-  __shared__ uint32_t lkeys[KEYS > 0 ? KEYS : 1];
+  __shared__ uint32_t lkeys[PER > 0 ? PER * kNtEvict : 1];
   __shared__ uint32_t hist[kEvictBins];
   __shared__ uint32_t buf[kNtEvict / 64];
-  __shared__ uint32_t s_lo, s_hi, s_top, s_bin, s_need;
+  __shared__ uint32_t list[64];
+  __shared__ uint32_t s_lo, s_hi, s_top, s_bin, s_need, s_count, s_fill;
   const int tid = threadIdx.x, lane = tid & 63;
   const int bj = blockIdx.x, b = bj / a.n_kv;
+  float* wt = a.weight + (size_t)bj * a.t_cap + a.t_off;
+  int32_t* ps = a.pos != nullptr ? a.pos + (size_t)bj * a.t_cap + a.t_off : nullptr;
+  uint32_t* keys = PER > 0 ? lkeys : a.keys + (size_t)bj * a.T;
+  // the weights and positions of all T rows, before the length is known
+  constexpr int N = PER > 0 ? PER : 1;
+  float x[N];
+  int p[N];
+  if constexpr (PER > 0) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = wt[min(tid + i * kNtEvict, a.T - 1)];
+    if (ps != nullptr) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) p[i] = ps[min(tid + i * kNtEvict, a.T - 1)];
+    }
+  }
   const int n = a.len != nullptr ? min(max(a.len[b], 0), a.T) : a.T;
+  const int newest = a.last_pos != nullptr ? a.last_pos[b] : 0;
   const int left = min(n, a.keep);
   if (n == left) {
     if (tid == 0) a.n_moves[bj] = 0;
     return;
   }
-  float* wt = a.weight + (size_t)bj * a.t_cap + a.t_off;
-  int32_t* ps = a.pos != nullptr ? a.pos + (size_t)bj * a.t_cap + a.t_off : nullptr;
-  uint32_t* keys = KEYS > 0 ? lkeys : a.keys + (size_t)bj * a.T;
-  const int newest = a.last_pos != nullptr ? a.last_pos[b] : 0;
   if (tid == 0) {
     s_lo = 0xffffffffu;
     s_hi = 0u;
     s_top = 0u;
   }
+  for (int i = tid; i < kEvictBins; i += kNtEvict) hist[i] = 0u;
   __syncthreads();
   uint32_t lo = 0xffffffffu, hi = 0u, top = 0u;
-  for (int t0 = tid; t0 < n; t0 += 4 * kNtEvict) {
-    float x[4];
-    int p[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int t = min(t0 + i * kNtEvict, n - 1);
-      x[i] = wt[t];
-      p[i] = ps != nullptr ? ps[t] : 0;
+  uint32_t k[N];
+  auto take = [&](uint32_t r) {
+    if (r == 0xffffffffu) {
+      ++top;
+    } else if (r != 0u) {
+      lo = min(lo, r);
+      hi = max(hi, r);
     }
+  };
+  if constexpr (PER > 0) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int t = t0 + i * kNtEvict;
-      if (t >= n) continue;
-      const uint32_t k = rank_of(a, x[i], p[i], newest);
-      keys[t] = k;
-      if (k == 0xffffffffu) {
-        ++top;
-      } else if (k != 0u) {
-        lo = min(lo, k);
-        hi = max(hi, k);
-      }
+    for (int i = 0; i < N; ++i) {
+      const int t = tid + i * kNtEvict;
+      k[i] = t < n ? rank_of(a, x[i], ps != nullptr ? p[i] : 0, newest) : 0u;  // past the rows: as NaN, never counted
+      lkeys[t] = k[i];
+      take(k[i]);
+    }
+  } else {
+    for (int t = tid; t < n; t += kNtEvict) {
+      const uint32_t r = rank_of(a, wt[t], ps != nullptr ? ps[t] : 0, newest);
+      keys[t] = r;
+      take(r);
     }
   }
 #pragma unroll
@@ -143,16 +161,25 @@ __global__ __launch_bounds__(kNtEvict) void evict_select_kernel(EvictArgs a) {
     // bin width 2^shift: the least that covers [lo, hi] with 2048 bins
     const uint32_t range = hi - lo;
     const int shift = range < (uint32_t)kEvictBins ? 0 : 21 - __clz(range);
-    for (int i = tid; i < kEvictBins; i += kNtEvict) hist[i] = 0u;
-    if (tid == 0) s_bin = 0xffffffffu;
-    __syncthreads();
-    for (int t = tid; t < n; t += kNtEvict) {
-      const uint32_t k = keys[t];
-      if (k >= lo && k <= hi) atomicAdd(&hist[(k - lo) >> shift], 1u);
+    if (tid == 0) {
+      s_bin = 0xffffffffu;
+      s_fill = 0u;
+    }
+    if constexpr (PER > 0) {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (k[i] >= lo && k[i] <= hi) atomicAdd(&hist[(k[i] - lo) >> shift], 1u);
+    } else {
+      for (int t = tid; t < n; t += kNtEvict) {
+        const uint32_t r = keys[t];
+        if (r >= lo && r <= hi) atomicAdd(&hist[(r - lo) >> shift], 1u);
+      }
     }
     __syncthreads();
-    // thread i takes the i-th pair of bins from the top
+    // thread i takes the i-th pair of bins from the top, and leaves them at zero
     const uint32_t h1 = hist[kEvictBins - 1 - 2 * tid], h0 = hist[kEvictBins - 2 - 2 * tid];
+    hist[kEvictBins - 1 - 2 * tid] = 0u;
+    hist[kEvictBins - 2 - 2 * tid] = 0u;
     uint32_t total;
     const uint32_t upto = block_scan(h0 + h1, buf, total);
     const uint32_t before = upto - h0 - h1;
@@ -160,6 +187,7 @@ __global__ __launch_bounds__(kNtEvict) void evict_select_kernel(EvictArgs a) {
       const bool first = need <= before + h1;
       s_bin = kEvictBins - 1 - 2 * tid - (first ? 0 : 1);
       s_need = need - before - (first ? 0u : h1);
+      s_count = first ? h1 : h0;
     }
     __syncthreads();
     if (s_bin == 0xffffffffu) {  // every number stays, and some NaN
@@ -172,6 +200,35 @@ __global__ __launch_bounds__(kNtEvict) void evict_select_kernel(EvictArgs a) {
       if (shift == 0) {
         last = lo;
         found = true;
+      } else if (s_count <= 64u) {  // the bin's rows, compared by the first wave
+        const auto gather = [&](uint32_t r) {
+          if (r >= lo && r <= hi) list[atomicAdd(&s_fill, 1u)] = r;
+        };
+        if constexpr (PER > 0) {
+#pragma unroll
+          for (int i = 0; i < N; ++i) gather(k[i]);
+        } else {
+          for (int t = tid; t < n; t += kNtEvict) gather(keys[t]);
+        }
+        __syncthreads();
+        if (tid < 64) {
+          const int count = (int)s_count;
+          const uint32_t mine = list[min(lane, count - 1)];
+          uint32_t above = 0, same = 0;
+          for (int i = 0; i < count; ++i) {
+            const uint32_t r = list[i];
+            above += r > mine ? 1u : 0u;
+            same += r == mine ? 1u : 0u;
+          }
+          if (lane < count && above < need && need <= above + same) {
+            s_bin = mine;
+            s_need = need - above;
+          }
+        }
+        __syncthreads();
+        last = s_bin;
+        need = s_need;
+        found = true;
       }
     }
     __syncthreads();
@@ -180,36 +237,47 @@ __global__ __launch_bounds__(kNtEvict) void evict_select_kernel(EvictArgs a) {
   const int c = ((n + kNtEvict - 1) / kNtEvict) | 1;
   const int t0 = (int)min((long long)tid * c, (long long)n), t1 = min(t0 + c, n);
   uint32_t eq = 0, total;
+#pragma unroll 8
   for (int t = t0; t < t1; ++t) eq += keys[t] == last ? 1u : 0u;
   const uint32_t eq0 = block_scan(eq, buf, total) - eq;
-  uint32_t holes = 0, movers = 0, e = eq0;
+  uint32_t e = eq0;
+  auto kept = [&](uint32_t r) { return r > last || (r == last && e++ < ties); };
+  uint32_t holes = 0, movers = 0;
+#pragma unroll 8
   for (int t = t0; t < t1; ++t) {
-    const uint32_t k = keys[t];
-    const bool kept = k > last || (k == last && e++ < ties);
-    holes += !kept && t < left ? 1u : 0u;
-    movers += kept && t >= left ? 1u : 0u;
+    const bool stays = kept(keys[t]);
+    holes += !stays && t < left ? 1u : 0u;
+    movers += stays && t >= left ? 1u : 0u;
   }
-  uint32_t n_holes, n_movers;
-  uint32_t h = block_scan(holes, buf, n_holes) - holes;
+  uint32_t n_movers;
+  uint32_t h = block_scan(holes, buf, total) - holes;
   uint32_t m = block_scan(movers, buf, n_movers) - movers;
   int2* mv = a.moves + (size_t)bj * a.max_moves;
   e = eq0;
+#pragma unroll 8
   for (int t = t0; t < t1; ++t) {
-    const uint32_t k = keys[t];
-    const bool kept = k > last || (k == last && e++ < ties);
-    if (!kept && t < left) mv[h++].x = t;
-    if (kept && t >= left) mv[m++].y = t;
+    const bool stays = kept(keys[t]);
+    if (t < left) {
+      if (!stays) mv[h++].x = t;
+    } else if (stays) {
+      mv[m++].y = t;
+    } else if (keys[t] == last) {
+      wt[t] = 0.0f;
+    }
   }
-  __threadfence_block();
-  __syncthreads();
+  // weights of the freed slots from `left` on: ranks below the last one here, ties that do
+  // not stay above, a mover's when it has moved
+  if constexpr (PER > 0) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int t = tid + i * kNtEvict;
+      if (t >= left && t < n && k[i] < last) wt[t] = 0.0f;
+    }
+  } else {
+    for (int t = left + tid; t < n; t += kNtEvict)
+      if (keys[t] < last) wt[t] = 0.0f;
+  }
   if (tid == 0) a.n_moves[bj] = (int)n_movers;
-  for (int i = tid; i < (int)n_movers; i += kNtEvict) {
-    const int2 d = mv[i];
-    wt[d.x] = wt[d.y];
-    if (ps != nullptr) ps[d.x] = ps[d.y];
-  }
-  __syncthreads();
-  for (int t = left + tid; t < n; t += kNtEvict) wt[t] = 0.0f;
 }
 
 // keep = T - 1: a cache of T rows loses its lightest one (of equal ones the highest slot),
@@ -287,7 +355,8 @@ __global__ __launch_bounds__(kNtEvict) void evict_one_kernel(EvictArgs a, int he
   if (a.len != nullptr && threadIdx.x == 0) a.len[b] = a.keep;
 }
 
-// `parts` workgroups per (b, j) copy its moves, 16 bytes per lane.  Also the lengths.
+// `parts` workgroups per (b, j) copy its moves, 16 bytes of K and V per lane, weights and
+// positions beside a row's first.  Also the lengths.
 __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, int parts) {
   const int bj = (int)(blockIdx.x / (unsigned)parts), part = (int)blockIdx.x - bj * parts, b = bj / a.n_kv;
   const int n = a.n_moves[bj];
@@ -301,8 +370,14 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, int parts)
     const int m = (int)(i / cpr), c = (int)(i - (long long)m * cpr);
     const int2 d = mv[m];
     const size_t dst = (size_t)d.x * cpr + c, src = (size_t)d.y * cpr + c;
-    k[dst] = k[src];
-    v[dst] = v[src];
+    const uint4 x = k[src], y = v[src];
+    k[dst] = x;
+    v[dst] = y;
+    if (c == 0) {
+      a.weight[row0 + d.x] = a.weight[row0 + d.y];
+      a.weight[row0 + d.y] = 0.0f;
+      if (a.pos != nullptr) a.pos[row0 + d.x] = a.pos[row0 + d.y];
+    }
   }
   if (a.len != nullptr && bj == b * a.n_kv && part == 0 && threadIdx.x == 0)
     a.len[b] = min(min(max(a.len[b], 0), a.T), a.keep);
@@ -315,12 +390,15 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t st) {
     hipLaunchKernelGGL(evict_one_kernel, dim3(bjs / heads), dim3(kNtEvict), 0, st, a, heads);
     return hipGetLastError();
   }
-  if (a.T <= 8192)
-    hipLaunchKernelGGL(evict_select_kernel<8192>, dim3(bjs), dim3(kNtEvict), 0, st, a);
-  else if (a.T <= 32768)
-    hipLaunchKernelGGL(evict_select_kernel<32768>, dim3(bjs), dim3(kNtEvict), 0, st, a);
+  const auto select = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(bjs), dim3(kNtEvict), 0, st, a); };
+  if (a.T <= 4 * kNtEvict)
+    select(evict_select_kernel<4>);
+  else if (a.T <= 17 * kNtEvict)
+    select(evict_select_kernel<17>);
+  else if (a.T <= 32 * kNtEvict)
+    select(evict_select_kernel<32>);
   else
-    hipLaunchKernelGGL(evict_select_kernel<0>, dim3(bjs), dim3(kNtEvict), 0, st, a);
+    select(evict_select_kernel<0>);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const long long work = (long long)a.max_moves * (a.row_bytes / 16);
