@@ -413,10 +413,13 @@ size_t kvd_block_workspace_bytes(const kvd_attn_shape* shape, int32_t d_ff, int3
  *   ws       kvd_prefix_workspace_bytes(shape, B, N, T_prefix, T_own, weight != NULL)
  *            bytes, 256-byte aligned, overwritten; it need not be cleared, and calls
  *            ordered on one stream may share it.
- * Results repeat bit for bit (no atomics).  The shape's d_model, rms_eps, rope_theta
- * and w_layout are not used.  Any N; bf16 calls with N * n_q_heads / n_kv_heads <= 16
- * rows per key keep the softmax weights in fp32, larger ones round each to bf16 before
- * the value product.  B == 0 or N == 0 is a no-op.                              */
+ * Results repeat bit for bit (no atomics), and out does not depend on whether weight
+ * is given.  The shape's d_model, rms_eps, rope_theta and w_layout are not used.
+ * bf16: where a key range has at most 16 rows (N * n_q_heads / n_kv_heads of an own
+ * range or a small call, B times as many of a prefix) the softmax weights enter the value
+ * product as the sum of two bf16 parts, elsewhere rounded to one bf16.  Sums of p V are
+ * taken before the division by sum p, so |V| near the largest float overflows.
+ * B == 0 or N == 0 is a no-op.                                                  */
 kvd_status kvd_prefix_attn(const kvd_attn_shape* shape, const void* q, int32_t N,
                            const kvd_kv_view* prefix, int32_t T_prefix, const kvd_kv_view* own,
                            const int32_t* own_len, const int32_t* n_new, int32_t B, int32_t T_own,

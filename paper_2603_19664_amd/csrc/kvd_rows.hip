@@ -1015,10 +1015,12 @@ __global__ __launch_bounds__(256) void rows_f32_kernel(RowsArgs a) {
 struct Merge {
   float M, L, w0, w1;
 };
-__device__ __forceinline__ Merge merge_states(const RowsArgs& a, int S, int j, int fr, int lane) {
-  float2 x = make_float2(-INFINITY, 0.0f), y = x;
+__device__ __forceinline__ void load_states(const RowsArgs& a, int S, int j, int fr, int lane, float2& x, float2& y) {
+  x = y = make_float2(-INFINITY, 0.0f);
   if (lane < S) x = *reinterpret_cast<const float2*>(a.ml + 2 * slot_row(a, lane, j, fr));
   if (lane + 64 < S) y = *reinterpret_cast<const float2*>(a.ml + 2 * slot_row(a, lane + 64, j, fr));
+}
+__device__ __forceinline__ Merge merge_states(float2 x, float2 y) {
   if (x.y == 0.0f) x.x = -INFINITY;
   if (y.y == 0.0f) y.x = -INFINITY;
   Merge m;
@@ -1050,7 +1052,9 @@ __global__ __launch_bounds__(256) void rows_finish_kernel(RowsArgs a, int merge_
     const int j = in ? (int)(idx / Rt) : 0, fr = in ? (int)(idx - (long long)j * Rt) : 0;
     const bool on = in && row_wanted(a, fr);
     if (WPR == 1 && !on) return;
-    const Merge m = merge_states(a, S, j, fr, lane);
+    float2 s0, s1;
+    load_states(a, S, j, fr, lane, s0, s1);
+    const Merge m = merge_states(s0, s1);
     if (a.lse != nullptr && on && lane == 0 && w % WPR == 0)
       a.lse[(size_t)j * Rt + fr] = m.L != 0.0f ? m.M + __builtin_amdgcn_logf(m.L) : INFINITY;
     float x[E];
@@ -1100,21 +1104,38 @@ __global__ __launch_bounds__(256) void rows_finish_kernel(RowsArgs a, int merge_
   const int c = item / units, u = item - c * units;
   const int j = u % a.n_kv, b = u / a.n_kv;
   const Seq sq = seq_of(a, b);
-  for (int r = w; r < sq.n * a.g; r += 4) {
-    const Merge m = merge_states(a, S, j, b * a.R + r, lane);
-    if (lane == 0) lse[r] = m.L != 0.0f ? m.M + __builtin_amdgcn_logf(m.L) : INFINITY;
-  }
-  __syncthreads();
-  const int t = c * kFinishKeys + threadIdx.x;
-  if (t >= sq.len) return;
-  const float* sc = a.sc + ((size_t)b * a.n_kv + j) * a.R * a.sc_ld + t;
-  float sum = 0.0f;
-  for (int r = 0; r < sq.n * a.g; ++r) {
-    const float x = sc[(size_t)r * a.sc_ld];
-    sum += x == -INFINITY ? 0.0f : exp2_hw(x - lse[r]);
-  }
+  const int nr = sq.n * a.g, t = c * kFinishKeys + threadIdx.x;
+  // the earlier weight and the first four rows' scores while the rows' sums are merged
+  const bool in = t < sq.len;
   float* wp = a.weight + ((size_t)b * a.n_kv + j) * a.t_cap + a.t_off + t;
-  *wp = a.decay != 0.0f ? fmaf(a.decay, *wp, sum) : sum;
+  const float* sc = a.sc + ((size_t)b * a.n_kv + j) * a.R * a.sc_ld + t;
+  const float old = in && a.decay != 0.0f ? a.decay * *wp : 0.0f;
+  float x[4];
+  auto scores = [&](int r0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = in && r0 + i < nr ? sc[(size_t)(r0 + i) * a.sc_ld] : -INFINITY;
+  };
+  scores(0);
+  float2 s0[4], s1[4];  // of rows w, w + 4, ..
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (w + 4 * i < nr) load_states(a, S, j, b * a.R + w + 4 * i, lane, s0[i], s1[i]);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (w + 4 * i < nr) {
+      const Merge m = merge_states(s0[i], s1[i]);
+      if (lane == 0) lse[w + 4 * i] = m.L != 0.0f ? m.M + __builtin_amdgcn_logf(m.L) : INFINITY;
+    }
+  __syncthreads();
+  float sum = 0.0f;
+  for (int r = 0; r < nr; r += 4) {
+    float p[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = x[i] == -INFINITY ? 0.0f : exp2_hw(x[i] - lse[min(r + i, nr - 1)]);
+    if (r + 4 < nr) scores(r + 4);
+    sum += (p[0] + p[1]) + (p[2] + p[3]);
+  }
+  if (in) *wp = old + sum;
 }
 
 // ------------------------------------------------------------------ weights of a key tile

@@ -498,10 +498,11 @@ def kvd_evict_workspace_bytes(shape: Shape, B: int, T: int) -> int:
 
 def _dims(t, name, want):
     """ValueError unless tensor t has exactly the extents `want`."""
+    if getattr(t, "shape", None) == want and isinstance(t, torch.Tensor):
+        return
     if not isinstance(t, torch.Tensor):
         raise ValueError(f"{name} must be a torch tensor")
-    if t.shape != want:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(want)}")
+    raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(want)}")
 
 
 def _dev_ptr(t, name, dtype, dev):
