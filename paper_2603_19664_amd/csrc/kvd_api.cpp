@@ -885,7 +885,7 @@ namespace {
 struct RowsPlan {
   int32_t R, joint, prefix_few, own_few, S_prefix, C_prefix, S_own, C_own, S_w, sc_ld;
   size_t ml, acc, lse, sc, wpart, end;  // byte offsets in the workspace
-  long long items;                      // workgroups of the largest launch
+  long long items;                      // workgroups of the largest attention or weight launch
 };
 
 // Slots of a key range that `units` items share, each of at least `least` keys and at most
@@ -911,7 +911,7 @@ int32_t slot_keys(long long keys, int32_t slots) {
   return (int32_t)((((keys + slots - 1) / slots) + 63) / 64 * 64);
 }
 
-// False when a size passes the kernels' 32-bit indexes.
+// False when a size passes the kernels' 32-bit indexes or a launch's number of threads.
 bool rows_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T_prefix, int32_t T_own, bool weights,
                RowsPlan* p) {
   const bool bf = s->dtype == KVD_BF16;
@@ -920,7 +920,7 @@ bool rows_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T_prefix, 
   *p = RowsPlan{};
   const long long R = (long long)N * g, Rt = R * B, units = (long long)B * s->n_kv_heads;
   const long long keys = (long long)T_prefix + T_own;
-  if (Rt * s->n_kv_heads > INT32_MAX || Rt >= 1ll << 28 || keys > INT32_MAX - 1024 || units > INT32_MAX) return false;
+  if (Rt * s->n_kv_heads > INT32_MAX || Rt >= 1ll << 28 || keys > INT32_MAX - 8192 || units > INT32_MAX) return false;
   p->R = (int32_t)R;
   const bool small = keys <= kvd::kRowsSmall;
   p->joint = T_prefix > 0 && T_own > 0 && (R >= RB / 2 || (small && (!bf || R <= kvd::kRowsFew)));
@@ -947,6 +947,8 @@ bool rows_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T_prefix, 
     }
   }
   const size_t rows = (size_t)Rt * s->n_kv_heads, S = (size_t)p->S_prefix + p->S_own;
+  const int per_wg = 4 / kvd::rows_finish_waves((int)S);
+  long long merge = S > 1 ? ((long long)rows + per_wg - 1) / per_wg : 0;
   size_t at = 0;
   const auto take = [&at](size_t bytes) {
     const size_t o = at;
@@ -959,7 +961,7 @@ bool rows_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T_prefix, 
     if (R <= kvd::kRowsFew) {  // the scores are kept
       p->sc_ld = (T_own + 15) / 16 * 16;
       p->sc = take(4 * (size_t)units * R * p->sc_ld);
-      p->items = std::max(p->items, (long long)rows + units * ((T_own + 255) / 256));
+      merge += units * ((T_own + 255) / 256);
     } else {
       // tiles of keys, their rows in S_w parts of at least 256 until the chip is full
       const long long keys_w = bf ? 128 : 16, tiles = units * ((T_own + keys_w - 1) / keys_w);
@@ -971,9 +973,8 @@ bool rows_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T_prefix, 
       p->items = std::max(p->items, tiles * p->S_w);
     }
   }
-  p->items = std::max(p->items, (long long)rows);
   p->end = std::max<size_t>(at, 256);
-  return p->items <= INT32_MAX / 2;
+  return std::max(p->items, merge) <= kvd::most_wgs(256);
 }
 
 kvd_status rows_call(const kvd_attn_shape* shape, const void* q, int32_t N, const kvd_kv_view* prefix,
@@ -1059,7 +1060,7 @@ struct EvictPlan {
 };
 bool evict_plan(const kvd_attn_shape* s, int32_t B, int32_t T, EvictPlan* p) {
   const size_t units = (size_t)B * s->n_kv_heads;
-  if (units > INT32_MAX / 2) return false;
+  if (units > (size_t)kvd::most_wgs(1024)) return false;
   p->moves = kvd::align_up(4 * units * T, 256);
   p->count = p->moves + kvd::align_up(8 * units * (T / 2 + 1), 256);  // at most min(T - keep, keep) moves
   p->end = p->count + kvd::align_up(4 * units, 256);
@@ -1093,7 +1094,9 @@ size_t kvd_prefix_workspace_bytes(const kvd_attn_shape* shape, int32_t B, int32_
     fail(KVD_ERR_SHAPE, "B=%d N=%d T_prefix=%d T_own=%d weights=%d", B, N, T_prefix, T_own, weights);
     return 0;
   }
-  return rows_plan(shape, B, N, T_prefix, T_own, weights != 0, &p) ? p.end : 0;
+  if (rows_plan(shape, B, N, T_prefix, T_own, weights != 0, &p)) return p.end;
+  fail(KVD_ERR_SHAPE, "B=%d N=%d T_prefix=%d T_own=%d is too large for one call", B, N, T_prefix, T_own);
+  return 0;
 }
 
 kvd_status kvd_evict(const kvd_attn_shape* shape, const kvd_kv_view* kv, int32_t* kv_len, int32_t B, int32_t T,
@@ -1147,7 +1150,9 @@ size_t kvd_evict_workspace_bytes(const kvd_attn_shape* shape, int32_t B, int32_t
     fail(KVD_ERR_SHAPE, "B=%d T=%d must be >= 1", B, T);
     return 0;
   }
-  return evict_plan(shape, B, T, &p) ? p.end : 0;
+  if (evict_plan(shape, B, T, &p)) return p.end;
+  fail(KVD_ERR_SHAPE, "B=%d is too large for one call", B);
+  return 0;
 }
 
 namespace {

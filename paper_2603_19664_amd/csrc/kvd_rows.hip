@@ -355,8 +355,9 @@ again:
     step(t, buf0, buf1);
     if (t + 1 < nt) step(t + 1, buf1, buf0);
   }
-  // O holds no infinity or NaN unless V did
-  if (pass == 0) {
+  // O holds no infinity or NaN unless V or the scores did; rows nobody asked for may
+  const bool wanted = rl < nr && row_wanted(a, fr);
+  if (pass == 0 && wanted) {
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -386,7 +387,7 @@ again:
         }
     }
   }
-  if (rl >= nr || !row_wanted(a, fr)) return;
+  if (!wanted) return;
   const float m_out = m_run == -INFINITY ? 0.0f : m_run;
   const bool direct = a.S_prefix + a.S_own == 1;
   const size_t row = slot_row(a, slot, j, fr);
@@ -659,7 +660,7 @@ again:
       if (i + 1 < nb) step(IC<0>{}, i + 1, sl1, sl1 + SLICE / 2);
     }
   }
-  if (pass == 0) {
+  if (pass == 0 && hq < nr && row_wanted(a, fr0 + hq)) {
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -1033,9 +1034,6 @@ __device__ __forceinline__ Merge merge_states(float2 x, float2 y) {
 }
 
 constexpr int kFinishKeys = 256;   // keys per workgroup of the streamed weights
-// Waves that share a row's states: a wave keeps 8 in flight, so that many states are many
-// round trips (512 rows of 66 states: 12.0 us with one wave per row).
-constexpr int finish_waves(int S) { return S > 8 ? 4 : 1; }
 
 // Workgroups 0 .. merge_wgs - 1 merge 4 / WPR rows each (out, and their max + log2(sum)
 // where the weights of tiles need them); the rest add up the weights of 256 own keys of one
@@ -1348,11 +1346,11 @@ static hipError_t launch_rows_t(const RowsArgs& a, hipStream_t st) {
   const int S = S_prefix + a.S_own;
   const bool sums = a.weight != nullptr && a.T_own > 0;
   const long long rows = (long long)a.B * a.R * a.n_kv;
-  const int per = 4 / finish_waves(S);  // merged rows per workgroup
+  const int per = 4 / rows_finish_waves(S);  // merged rows per workgroup
   const int merge_wgs = S > 1 ? (int)((rows + per - 1) / per) : 0;
   const int weight_wgs = sums && a.sc != nullptr ? a.B * a.n_kv * ((a.T_own + kFinishKeys - 1) / kFinishKeys) : 0;
   if (merge_wgs + weight_wgs > 0) {
-    if (finish_waves(S) == 4)
+    if (rows_finish_waves(S) == 4)
       hipLaunchKernelGGL((rows_finish_kernel<T, HD, 4>), dim3(merge_wgs + weight_wgs), dim3(256), 0, st, a, merge_wgs);
     else
       hipLaunchKernelGGL((rows_finish_kernel<T, HD, 1>), dim3(merge_wgs + weight_wgs), dim3(256), 0, st, a, merge_wgs);

@@ -146,6 +146,22 @@ def test_what_is_not_seen_has_no_part(dtype, N, T_prefix):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("N,T_prefix,T", [(3, 40, 90), (3, 700, 900), (40, 40, 90), (90, 0, 700), (90, 600, 300)])
+def test_queries_of_no_token_have_no_part(dtype, N, T_prefix, T):
+    # a padded batch: the queries behind a sequence's new tokens are NaN, in blocks with others and in ones of their own
+    B, news = 4, [N, 1, 0, N - 1]
+    lens = [T, T - 5, 7, 2]
+    s = shape(dtype, 6, 2, 64)
+    x = make(dtype, 6, 2, 64, B, N, T_prefix, T, 7)
+    w, w0 = x["weight"].clone(), x["weight"].clone()
+    a = call(s, x, T_prefix, T, lens, news, w0, 0.5)
+    for b, n in enumerate(news):
+        x["q"][b, n:] = float("nan")
+    c = call(s, x, T_prefix, T, lens, news, w, 0.5)
+    assert torch.isfinite(c).all() and torch.equal(a, c) and torch.equal(w, w0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_infinite_values_at_a_range_end(dtype):
     # a seen infinity in the last, ragged block is an infinity, not 0 * inf
     for T_prefix, T, N in ((0, 37, 1), (37, 5, 1), (37, 70, 40), (333, 0, 60)):

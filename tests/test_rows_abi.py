@@ -72,6 +72,8 @@ def evict(s=None, kv=view(), B=2, T=16, keep=8, weight=FAKE, pos=None, last=None
     (kvd.KVD_ERR_ALIGN, dict(ws=FAKE + 16)),
     (kvd.KVD_ERR_SHAPE, dict(N=1 << 28, B=2)),
     (kvd.KVD_ERR_SHAPE, dict(B=65535, N=65535)),
+    # 65535 x 62 x 32 rows to merge, 4 per workgroup of 256 threads: 2^32 threads and more
+    (kvd.KVD_ERR_SHAPE, dict(s=shape(n_q_heads=64, n_kv_heads=32), B=65535, N=31)),
 ])
 def test_prefix_refusals(status, kw):
     assert prefix(**kw) == status
@@ -115,6 +117,8 @@ def test_weighted_refusals(status, kw):
     (kvd.KVD_ERR_WORKSPACE, dict(ws=None)),
     (kvd.KVD_ERR_WORKSPACE, dict(n=100)),
     (kvd.KVD_ERR_ALIGN, dict(ws=FAKE + 128)),
+    # a workgroup of 1024 threads per (sequence, KV head): 2^32 threads
+    (kvd.KVD_ERR_SHAPE, dict(s=shape(n_q_heads=256, n_kv_heads=256), B=1 << 14)),
 ])
 def test_evict_refusals(status, kw):
     assert evict(**kw) == status
@@ -159,6 +163,7 @@ def test_workspace_of_invalid_arguments():
     assert f(ref(s), 1, 1, 5, 0, 1) == 0
     assert f(ref(s), 1, 1, -1, 5, 0) == 0
     assert f(ref(s), 65535, 65535, 1, 1, 0) == 0
+    assert "too large" in kvd.last_error()
     assert lib.kvd_evict_workspace_bytes(ref(s), 1, 0) == 0
     assert lib.kvd_evict_workspace_bytes(ref(s), 0, 1) == 0
     sizes = [lib.kvd_evict_workspace_bytes(ref(s), 4, t) for t in range(1, 5000, 11)]
