@@ -888,27 +888,46 @@ struct RowsPlan {
   long long items;                      // workgroups of the largest attention or weight launch
 };
 
-// Slots of a key range that `units` items share, each of at least `least` keys and at most
-// kRowsMostSlots: enough for kRowsTargetWgs workgroups, and beyond that the count S that
-// balances what the last workgroups of a launch leave idle, about half a slot (keys / S /
-// 2), against a slot's fixed cost of kRowsSlotKeys keys (first loads, state written and
-// merged) for every workgroup's units S / kRowsTargetWgs of them.  A causal range (every row
-// its own length) holds half of the keys.  Grows with keys.
-int32_t row_slots(long long units, long long keys, int32_t least, bool causal) {
+// Slots of a key range that `units` items of `rows` rows in all share, each of at least
+// `least` keys and at most kRowsMostSlots; grows with keys.
+// Enough for `wgs` workgroups, but fewer than sqrt(keys kRowsStateRows / rows): a slot
+// leaves every row a state that is written and read, as dear as 1 / kRowsStateRows of a key in
+// a workgroup's range of keys / S.  (64 tokens, 8 heads of 256 over a prefix of 16384: 85
+// us with 64 slots, 74 with 43; 12 heads of 128: 41 and 34; prompts of 400 tokens over 1500
+// keys: 52 us with 6, 49 with 3.)  Beside own rows, whose reads fill the idle workgroups'
+// time, the states count half as much again.
+// Beyond `wgs`, the count S that balances what the last workgroups of a launch leave
+// idle, about half a slot (keys / S / 2), against a slot's fixed cost of kRowsSlotKeys keys
+// (first loads, state written and merged) for every workgroup's units S / kRowsTargetWgs of
+// them.  A causal range (every row its own length) holds half of the keys.
+int32_t row_slots(long long units, long long rows, long long keys, int32_t least, bool causal,
+                  bool beside = false, long long wgs = kvd::kRowsTargetWgs) {
   const double work = (double)units * kvd::kRowsSlotKeys * (causal ? 0.5 : 1.0);
   const long long balance = (long long)std::sqrt(0.5 * kvd::kRowsTargetWgs * (double)keys / work);
-  const long long fill = (kvd::kRowsTargetWgs + units - 1) / units;
+  const double cost = (double)rows * (beside ? 1.5 : 1.0) / kvd::kRowsStateRows;
+  const long long fill = std::min((wgs + units - 1) / units, (long long)std::sqrt((double)keys / cost));
   return (int32_t)std::max(1ll, std::min({std::max(balance, fill), (keys + least - 1) / least,
                                           (long long)kvd::kRowsMostSlots}));
 }
 // Slots of T own rows of which the last N are the new tokens: causal while those are more
 // than half of them.  Never fewer for more rows.
-int32_t causal_slots(long long units, int32_t T, int32_t least, int32_t N) {
-  const int32_t c = row_slots(units, std::min<long long>(T, 2ll * N), least, N > 1);
-  return 2ll * N > T ? c : std::max(c, row_slots(units, T, least, false));
+int32_t causal_slots(long long units, long long rows, int32_t T, int32_t least, int32_t N, bool beside,
+                     long long wgs) {
+  const int32_t c = row_slots(units, rows, std::min<long long>(T, 2ll * N), least, N > 1, beside, wgs);
+  return 2ll * N > T ? c : std::max(c, row_slots(units, rows, T, least, false, beside, wgs));
 }
-int32_t slot_keys(long long keys, int32_t slots) {
-  return (int32_t)((((keys + slots - 1) / slots) + 63) / 64 * 64);
+// Keys per slot (a multiple of 64, at least `least`) and slots, as near to S as those allow.
+void cut_keys(long long keys, int32_t least, int32_t* S, int32_t* C) {
+  const long long up = std::max<long long>((((keys + *S - 1) / *S) + 63) / 64 * 64, 64);
+  const long long down = std::max<long long>(up - 64, least);
+  const long long su = (keys + up - 1) / up, sd = (keys + down - 1) / down;
+  const bool more = down < up && sd <= kvd::kRowsMostSlots && sd - *S <= *S - su;
+  *S = (int32_t)(more ? sd : su);
+  *C = (int32_t)(more ? down : up);
+}
+// What cut_keys makes of S at most: a slot of C >= 128 keys is off by 32 at most.
+int32_t most_slots(int32_t S) {
+  return S > 1 ? std::min(S + (S + 3) / 4 + 1, kvd::kRowsMostSlots) : S;
 }
 
 // False when a size passes the kernels' 32-bit indexes or a launch's number of threads.
@@ -922,41 +941,53 @@ bool rows_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T_prefix, 
   const long long keys = (long long)T_prefix + T_own;
   if (Rt * s->n_kv_heads > INT32_MAX || Rt >= 1ll << 28 || keys > INT32_MAX - 8192 || units > INT32_MAX) return false;
   p->R = (int32_t)R;
+  int32_t S = 0;  // slots for which the workspace has room: falls with no length
   const bool small = keys <= kvd::kRowsSmall;
   p->joint = T_prefix > 0 && T_own > 0 && (R >= RB / 2 || (small && (!bf || R <= kvd::kRowsFew)));
   const long long nbo = (R + RB - 1) / RB, nbp = (Rt + RB - 1) / RB;
+  const long long rows = Rt * s->n_kv_heads;
   if (p->joint) {
     p->own_few = bf && R <= kvd::kRowsFew;
-    p->S_own = small ? 1 : row_slots(units * nbo, keys, least, false);
-    p->C_own = slot_keys(keys, p->S_own);
+    p->S_own = small ? 1 : row_slots(units * nbo, rows, keys, least, false);
+    S = most_slots(p->S_own);
+    cut_keys(keys, least, &p->S_own, &p->C_own);
     p->items = units * nbo * p->S_own;
   } else {
     if (T_prefix > 0) {
       p->prefix_few = bf && Rt <= kvd::kRowsFew;
       const long long u = p->prefix_few ? s->n_kv_heads : s->n_kv_heads * nbp;
-      p->S_prefix = small && T_own == 0 ? 1 : row_slots(u, T_prefix, least, false);
-      p->C_prefix = slot_keys(T_prefix, p->S_prefix);
+      p->S_prefix = small && T_own == 0 ? 1 : row_slots(u, rows, T_prefix, least, false, T_own > 0);
+      S = most_slots(p->S_prefix);
+      if (!p->prefix_few) cut_keys(T_prefix, least, &p->S_prefix, &p->C_prefix);
       p->items += u * p->S_prefix;
     }
     if (T_own > 0) {
       p->own_few = bf && R <= kvd::kRowsFew;
       const long long u = p->own_few ? units : units * nbo;
-      p->S_own = small && T_prefix == 0 ? 1 : causal_slots(u, T_own, least, N);
-      p->C_own = slot_keys(T_own, p->S_own);
+      if (small && T_prefix == 0) {
+        p->S_own = 1;
+        S += 1;
+      } else {
+        // beside a prefix, the workgroups that it leaves (more would be a second round)
+        const long long wgs = kvd::kRowsTargetWgs;
+        const bool beside = p->items > 0;
+        p->S_own = causal_slots(u, rows, T_own, least, N, beside, beside ? std::max(wgs - p->items, u) / u * u : wgs);
+        S += most_slots(causal_slots(u, rows, T_own, least, N, beside, wgs));
+      }
+      if (!p->own_few) cut_keys(T_own, least, &p->S_own, &p->C_own);
       p->items += u * p->S_own;
     }
   }
-  const size_t rows = (size_t)Rt * s->n_kv_heads, S = (size_t)p->S_prefix + p->S_own;
-  const int per_wg = 4 / kvd::rows_finish_waves((int)S);
-  long long merge = S > 1 ? ((long long)rows + per_wg - 1) / per_wg : 0;
+  const int per_wg = 4 / kvd::rows_finish_waves(S);
+  long long merge = S > 1 ? (rows + per_wg - 1) / per_wg : 0;
   size_t at = 0;
   const auto take = [&at](size_t bytes) {
     const size_t o = at;
     at += kvd::align_up(bytes, 256);
     return o;
   };
-  p->ml = take(8 * S * rows);
-  p->acc = take(S > 1 ? 4 * S * rows * s->head_dim : 0);
+  p->ml = take(8 * (size_t)S * rows);
+  p->acc = take(S > 1 ? 4 * (size_t)S * rows * s->head_dim : 0);
   if (weights && T_own > 0) {
     if (R <= kvd::kRowsFew) {  // the scores are kept
       p->sc_ld = (T_own + 15) / 16 * 16;

@@ -397,6 +397,7 @@ constexpr int kRowsTargetWgs = 512;
 constexpr int kRowsLeastKeys = 128;     // keys per slot, at least (bf16)
 constexpr int kRowsLeastKeysF32 = 128;
 constexpr int kRowsSlotKeys = 512;   // a slot's fixed cost in keys
+constexpr int kRowsStateRows = 96;   // rows whose states cost what a key costs a workgroup
 constexpr int kRowsMostSlots = 64;
 constexpr int kRowsSmall = 256;  // keys that one workgroup takes at once
 // Waves that share a row's S states when they are merged: a wave keeps 8 in flight, so that
