@@ -1165,7 +1165,7 @@ constexpr int kWtKeys = 128, kWtRows = 64;
 // adds 2^(score - lse) into 16 sums, one per key; lanes are added at the end.
 template <int HD>
 __global__ __launch_bounds__(256, 2) void weight_tile_kernel(RowsArgs a) {
-  constexpr int KS = HD / 16, CPR = HD / 8, CH = kWtRows * CPR / 256;
+  constexpr int KS = HD / 16, CPR = HD / 8, CH = kWtRows * CPR / 256, kLead = 4;
   __shared__ __align__(1024) uint16_t q_a[kWtRows * HD], q_b[kWtRows * HD];  // two objects: see rows_tile_kernel
   const int tid = threadIdx.x, lane = tid & 63, w = wave_id(), hl = lane >> 5;
   const int units = a.B * a.n_kv, x = (int)blockIdx.x / units, u = (int)blockIdx.x - x * units;
@@ -1224,14 +1224,29 @@ __global__ __launch_bounds__(256, 2) void weight_tile_kernel(RowsArgs a) {
     // whether every row of the tile sees every key of the workgroup
     const int first = rs.r0 + t * kWtRows;
     const bool masked = rows_seen(sq, token_of(a, first)) < k0 + kWtKeys;
+    f32x16_t sts[2];
 #pragma unroll
-    for (int h = 0; h < kWtRows / 32; ++h) {
-      f32x16_t st;
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) st[i] = 0.0f;
+      for (int i = 0; i < 16; ++i) sts[h][i] = 0.0f;
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-      for (int i = 0; i < KS; ++i)
-        st = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], score_operand(qs, qbase, i, 64 * HD * h), st, 0, 0, 0);
+    for (int i = 0; i < KS; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        sts[h] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], score_operand(qs, qbase, i, 64 * HD * h), sts[h], 0, 0, 0);
+    // reads kLead operands ahead of the products
+    __builtin_amdgcn_sched_group_barrier(0x100, kLead, 0);
+#pragma unroll
+    for (int i = 0; i < 2 * KS - kLead; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, kLead, 0);
+    __builtin_amdgcn_s_setprio(0);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const f32x16_t st = sts[h];
       float p[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) p[i] = exp2_hw(fmaf(st[i], ScoreScale<HD>::v, -lse[h]));
