@@ -883,7 +883,7 @@ namespace {
 // its own rows, and neither half leaves a partial state.  So do calls of few rows and at most
 // kRowsSmall keys; a range of that many keys is one slot, and the call one launch.
 struct RowsPlan {
-  int32_t R, joint, prefix_few, own_few, S_prefix, C_prefix, S_own, C_own, S_w, sc_ld;
+  int32_t R, joint, prefix_few, own_few, S_prefix, C_prefix, S_own, C_own, S_w, P_w, sc_ld;
   size_t ml, acc, lse, sc, wpart, end;  // byte offsets in the workspace
   long long items;                      // workgroups of the largest attention or weight launch
 };
@@ -994,13 +994,17 @@ bool rows_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T_prefix, 
       p->sc = take(4 * (size_t)units * R * p->sc_ld);
       merge += units * ((T_own + 255) / 256);
     } else {
-      // tiles of keys, their rows in S_w parts of at least 256 until the chip is full
+      // tiles of keys, the rows that see one in parts of P_w (at least 256), so that all parts
+      // together are just one round of workgroups.  Of N new tokens among T keys, 1 - N / 2 T
+      // of the rows see a key on average, and a tile's last part is half full.
       const long long keys_w = bf ? 128 : 16, tiles = units * ((T_own + keys_w - 1) / keys_w);
       const long long most = std::min(64ll, (R + 255) / 256), want = kvd::kRowsTargetWgs;
-      p->S_w = (int32_t)std::max(1ll, std::min((want + tiles - 1) / tiles, most));
+      const double seen = 1.0 - 0.5 * std::min(N, T_own) / T_own, parts = (double)want / tiles - 0.5;
+      p->S_w = (int32_t)std::max(1ll, std::min((long long)(parts / seen), most));
+      p->P_w = (int32_t)(((R + p->S_w - 1) / p->S_w + 63) / 64 * 64);
       p->lse = take(4 * rows);
-      // S_w T_own, or its bound over smaller T_own (it does not grow steadily)
-      p->wpart = take(4 * (size_t)units * std::min(most * T_own, want * keys_w / units + T_own + keys_w));
+      // S_w T_own, or its bound over smaller T_own (it does not grow steadily): seen >= 1 / 2
+      p->wpart = take(4 * (size_t)units * std::min(most * T_own, 2 * want * keys_w / units + T_own + keys_w));
       p->items = std::max(p->items, tiles * p->S_w);
     }
   }
@@ -1078,6 +1082,7 @@ kvd_status rows_call(const kvd_attn_shape* shape, const void* q, int32_t N, cons
   a.S_own = p.S_own;
   a.C_own = p.C_own;
   a.S_w = p.S_w;
+  a.P_w = p.P_w;
   a.sc_ld = p.sc_ld;
   a.joint = p.joint;
   a.prefix_few = p.prefix_few;

@@ -223,7 +223,7 @@ struct RowsArgs {
   float decay;
   int p_cap, p_off, T_prefix, t_cap, t_off, T_own;
   int B, N, n_q, n_kv, g, R;
-  int S_prefix, C_prefix, S_own, C_own, S_w, sc_ld;
+  int S_prefix, C_prefix, S_own, C_own, S_w, P_w, sc_ld;  // weights of tiles: up to S_w parts of P_w rows
   int joint, prefix_few, own_few;
   uint32_t g_inv;  // ceil(2^32 / g), g > 1
 };

@@ -1138,14 +1138,16 @@ __global__ __launch_bounds__(256) void rows_finish_kernel(RowsArgs a, int merge_
 
 // ------------------------------------------------------------------ weights of a key tile
 
-// Rows [r0, r1) of part c of C of the rows that see key k0 of sequence sq.
+// Rows [r0, r1) of part c, P_w rows each, of the rows that see key k0 of sequence sq: early
+// keys have more parts than late ones, all of one size (a 3001-token prompt: 35 us; with the
+// same number for each key, the first tiles' the longest, 37).
 struct RowSpan {
   int r0, r1;
 };
-__device__ __forceinline__ RowSpan rows_of_part(const Seq& sq, int g, int k0, int c, int C) {
+__device__ __forceinline__ RowSpan rows_of_part(const RowsArgs& a, const Seq& sq, int k0, int c) {
   const int i0 = min(max(k0 - (sq.len - sq.n), 0), sq.n);  // the first token that sees key k0
-  const long long first = (long long)i0 * g, n = (long long)(sq.n - i0) * g;
-  return RowSpan{(int)(first + n * c / C), (int)(first + n * (c + 1) / C)};
+  const long long r0 = (long long)i0 * a.g + (long long)c * a.P_w, end = (long long)sq.n * a.g;
+  return RowSpan{(int)min(r0, end), (int)min(r0 + a.P_w, end)};
 }
 __device__ __forceinline__ void put_weight(const RowsArgs& a, int c, int b, int j, int t, float sum) {
   const size_t bj = (size_t)b * a.n_kv + j;
@@ -1159,9 +1161,24 @@ __device__ __forceinline__ void put_weight(const RowsArgs& a, int c, int b, int 
 
 constexpr int kWtKeys = 128, kWtRows = 64;
 
+// Byte offset of the thread's i-th chunk of a tile of `rows` query rows from the first one's
+// token, whose row `at` it is (at most 65 tokens: 32 bits), and its copy into LDS.
+template <int HD>
+__device__ __forceinline__ uint32_t chunk_offset(const RowsArgs& a, int i, int at, int rows) {
+  constexpr int CPR = HD / 8;
+  const int r = threadIdx.x / CPR + 256 / CPR * i, x = at + min(r, rows - 1), tok = token_of(a, x);
+  return ((uint32_t)x + (uint32_t)tok * (uint32_t)(a.n_q - a.g)) * (HD * 2) +
+         16u * ((threadIdx.x % CPR) ^ score_swz<HD>(r));
+}
+__device__ __forceinline__ void copy_chunk(const uint16_t* src, uint32_t off, uint16_t* dst) {
+  const __amdgpu_buffer_rsrc_t res =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(src), (short)0, -1, 0x00027000);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (__attribute__((address_space(3))) void*)dst, 16, off, 0, 0, 0);
+}
+
 // bf16: one workgroup of 4 waves per (128 keys of (b, j), part of the rows).  A wave
-// keeps its 32 keys as MFMA A operands; the rows pass through LDS 64 at a time (tile
-// layout of copy_tile's score operands), two buffers.  A lane holds the scores of one row and
+// keeps its 32 keys as MFMA A operands; the rows pass through LDS 64 at a time
+// (layout of copy_tile's score operands), two buffers.  A lane holds the scores of one row and
 // adds 2^(score - lse) into 16 sums, one per key; lanes are added at the end.
 template <int HD>
 __global__ __launch_bounds__(256, 2) void weight_tile_kernel(RowsArgs a) {
@@ -1174,31 +1191,42 @@ __global__ __launch_bounds__(256, 2) void weight_tile_kernel(RowsArgs a) {
   const Seq sq = seq_of(a, b);
   const int k0 = tile * kWtKeys;
   if (k0 >= sq.len) return;
-  const RowSpan rs = rows_of_part(sq, a.g, k0, c, a.S_w);
+  const RowSpan rs = rows_of_part(a, sq, k0, c);
+  if (c > 0 && rs.r0 >= rs.r1) return;  // the first part writes in any case
   const KeyRange kr = own_range(a, b, j, 0, sq.len);
+  const uint32_t qbase = score_base<HD>(lane);
+  // The keys through the rows' buffers, whole lines at a time (straight into the registers a
+  // load takes 32 bytes of 32 rows: 32.0 us instead of 31.1).
   bf16x8_t kf[KS];
   {
-    const uint16_t* ks = static_cast<const uint16_t*>(a.k) +
-                         (kr.row + min(k0 + 32 * w + (lane & 31), sq.len - 1)) * HD + 8 * hl;
+    const uint16_t* ks = static_cast<const uint16_t*>(a.k) + kr.row * HD;
+    const int k1 = min(k0 + 64, sq.len - 1);
+    copy_tile<HD, 64, true>(ks + (size_t)k0 * HD, sq.len - k0, q_a);
+    copy_tile<HD, 64, true>(ks + (size_t)k1 * HD, sq.len - k1, q_b);
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < KS; ++i) kf[i] = *reinterpret_cast<const bf16x8_t*>(ks + 16 * i);
+    for (int i = 0; i < KS; ++i) kf[i] = score_operand(w < 2 ? q_a : q_b, qbase, i, 64 * HD * (w & 1));
+    __syncthreads();
   }
   float sum[16];
 #pragma unroll
   for (int r = 0; r < 16; ++r) sum[r] = 0.0f;
   const int fr0 = b * a.R;
-  const uint32_t qbase = score_base<HD>(lane);
   const int nt = rs.r1 > rs.r0 ? (rs.r1 - rs.r0 + kWtRows - 1) / kWtRows : 0;
-  auto load = [&](int t, uint16_t* dst) {
+  // A group size that divides 64: every tile starts with a token, and a thread's rows have
+  // the same offsets from it (64-bit offsets of every row: 35 us instead of 32).
+  const bool same = kWtRows % a.g == 0;
+  uint32_t off[CH];
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      const int cc = tid + 256 * i, row = cc / CPR, ch = cc - row * CPR;
-      const int fr = fr0 + min(rs.r0 + t * kWtRows + row, rs.r1 - 1);
-      __builtin_amdgcn_global_load_lds(
-          (const __attribute__((address_space(1))) void*)(static_cast<const uint16_t*>(a.q) + q_off(a, j, fr, HD) +
-                                                           8 * (ch ^ score_swz<HD>(row))),
-          (__attribute__((address_space(3))) void*)(dst + 8 * (64 * w + 256 * i)), 16, 0, 0);
-    }
+  for (int i = 0; i < CH; ++i) off[i] = chunk_offset<HD>(a, i, 0, kWtRows);
+  auto load = [&](int t, uint16_t* dst) {
+    const int first = rs.r0 + t * kWtRows, left = rs.r1 - first, at = first - token_of(a, first) * a.g;
+    const uint16_t* src = static_cast<const uint16_t*>(a.q) + q_off(a, j, fr0 + first - at, HD);
+    const bool full = same && left >= kWtRows;
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+      copy_chunk(src, full ? off[i] : chunk_offset<HD>(a, i, at, left), dst + 512 * w + 2048 * i);
   };
   // max + log2(sum) of the lane's two rows of a tile, loaded a tile ahead and before that
   // tile's copies (a load is waited for with everything issued before it); rows past the
@@ -1287,7 +1315,8 @@ __global__ __launch_bounds__(64) void weight_f32_kernel(RowsArgs a) {
   const Seq sq = seq_of(a, b);
   const int k0 = tile * 16;
   if (k0 >= sq.len) return;
-  const RowSpan rs = rows_of_part(sq, a.g, k0, c, a.S_w);
+  const RowSpan rs = rows_of_part(a, sq, k0, c);
+  if (c > 0 && rs.r0 >= rs.r1) return;  // the first part writes in any case
   const KeyRange kr = own_range(a, b, j, 0, sq.len);
   f32x4_t kf[KC];
   const float* ks = static_cast<const float*>(a.k) + (kr.row + min(k0 + rq, sq.len - 1)) * HD + 4 * lg;
@@ -1324,13 +1353,17 @@ __global__ __launch_bounds__(64) void weight_f32_kernel(RowsArgs a) {
   }
 }
 
-// weight = decay weight + the S_w parts' sums, in part order.
-__global__ __launch_bounds__(256) void weight_sum_kernel(RowsArgs a) {
+// weight = decay weight + the sums of the parts that key t's tile has, in part order.
+__global__ __launch_bounds__(256) void weight_sum_kernel(RowsArgs a, int tile_keys) {
   const int chunks = (a.T_own + 255) / 256;
   const int bj = (int)blockIdx.x / chunks, t = ((int)blockIdx.x - bj * chunks) * 256 + threadIdx.x;
-  if (t >= seq_of(a, bj / a.n_kv).len) return;
+  const Seq sq = seq_of(a, bj / a.n_kv);
+  if (t >= sq.len) return;
+  const RowSpan rs = rows_of_part(a, sq, t / tile_keys * tile_keys, 0);
+  const int parts = max((sq.n * a.g - rs.r0 + a.P_w - 1) / a.P_w, 1);
   float sum = 0.0f;
-  for (int c = 0; c < a.S_w; ++c) sum += a.wpart[((size_t)c * a.B * a.n_kv + bj) * a.T_own + t];
+#pragma unroll 4
+  for (int c = 0; c < parts; ++c) sum += a.wpart[((size_t)c * a.B * a.n_kv + bj) * a.T_own + t];
   float* wp = a.weight + (size_t)bj * a.t_cap + a.t_off + t;
   *wp = a.decay != 0.0f ? fmaf(a.decay, *wp, sum) : sum;
 }
@@ -1381,7 +1414,7 @@ static hipError_t launch_rows_t(const RowsArgs& a, hipStream_t st) {
     KVD_LAUNCH_TRY(hipGetLastError());
     if (a.S_w > 1) {
       hipLaunchKernelGGL(weight_sum_kernel, dim3((unsigned)(a.B * a.n_kv * ((a.T_own + 255) / 256))), dim3(256), 0, st,
-                         a);
+                         a, keys);
       KVD_LAUNCH_TRY(hipGetLastError());
     }
   }
