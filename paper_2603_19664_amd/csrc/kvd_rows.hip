@@ -358,10 +358,12 @@ again:
   // O holds no infinity or NaN unless V or the scores did; rows nobody asked for may
   const bool wanted = rl < nr && row_wanted(a, fr);
   if (pass == 0 && wanted) {
+    float x = 0.0f;  // 0 o: 4 bytes of code each; a small call waits for its instructions, 60 ns for 64 bytes
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) odd |= !(fabsf(o[db][i]) < INFINITY);
+      for (int i = 0; i < 16; ++i) x = fmaf(o[db][i], 0.0f, x);
+    odd = x != 0.0f;
   }
   if (pass == 0 && __syncthreads_or(odd)) {
     pass = 1;
@@ -404,11 +406,9 @@ again:
     for (int db = 0; db < DB; ++db)
 #pragma unroll
       for (int q4 = 0; q4 < 4; ++q4) {
-        uint2 v = make_uint2(0u, 0u);
-        if (l_run != 0.0f) {
-          v.x = pack_bf16x2(o[db][4 * q4 + 0] * inv, o[db][4 * q4 + 1] * inv);
-          v.y = pack_bf16x2(o[db][4 * q4 + 2] * inv, o[db][4 * q4 + 3] * inv);
-        }
+        // with no key o is 0
+        const uint2 v = make_uint2(pack_bf16x2(o[db][4 * q4 + 0] * inv, o[db][4 * q4 + 1] * inv),
+                                   pack_bf16x2(o[db][4 * q4 + 2] * inv, o[db][4 * q4 + 3] * inv));
         *reinterpret_cast<uint2*>(dst + 32 * db + 8 * q4 + 4 * hl) = v;
       }
   } else if (l_run != 0.0f) {
@@ -661,10 +661,12 @@ again:
     }
   }
   if (pass == 0 && hq < nr && row_wanted(a, fr0 + hq)) {
+    float x = 0.0f;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) odd |= !(fabsf(o[db][e]) < INFINITY);
+      for (int e = 0; e < 4; ++e) x = fmaf(o[db][e], 0.0f, x);
+    odd = x != 0.0f;
   }
   if (pass == 0 && __any(odd)) {
     pass = 1;
@@ -1179,7 +1181,7 @@ __device__ __forceinline__ void copy_chunk(const uint16_t* src, uint32_t off, ui
 // bf16: one workgroup of 4 waves per (128 keys of (b, j), part of the rows).  A wave
 // keeps its 32 keys as MFMA A operands; the rows pass through LDS 64 at a time
 // (layout of copy_tile's score operands), two buffers.  A lane holds the scores of one row and
-// adds 2^(score - lse) into 16 sums, one per key; lanes are added at the end.
+// adds 2^(score - lse) into 16 sums, one per key.
 template <int HD>
 __global__ __launch_bounds__(256, 2) void weight_tile_kernel(RowsArgs a) {
   constexpr int KS = HD / 16, CPR = HD / 8, CH = kWtRows * CPR / 256, kLead = 4;
@@ -1295,13 +1297,20 @@ __global__ __launch_bounds__(256, 2) void weight_tile_kernel(RowsArgs a) {
     step(t, q_a, q_b);
     if (t + 1 < nt) step(t + 1, q_b, q_a);
   }
+  // over the 32 lanes: each exchange adds half of the keys and hands the other half over
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
+  for (int o = 1, n = 8; o < 16; o <<= 1, n >>= 1) {
+    const bool up = (lane & o) != 0;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) sum[i] += __shfl_xor(sum[i], o, 64);
-    const int t = k0 + 32 * w + 8 * (i >> 2) + 4 * hl + (i & 3);
-    if ((lane & 31) == 0 && t < sq.len) put_weight(a, c, b, j, t, sum[i]);
+    for (int i = 0; i < n; ++i) {
+      const float give = up ? sum[i] : sum[i + n];
+      sum[i] = (up ? sum[i + n] : sum[i]) + __shfl_xor(give, o, 64);
+    }
   }
+  const float total = sum[0] + __shfl_xor(sum[0], 16, 64);
+  const int i = (lane & 1) * 8 + (lane & 2) * 2 + ((lane & 4) >> 1) + ((lane & 8) >> 3);  // the lane's key
+  const int t = k0 + 32 * w + 8 * (i >> 2) + 4 * hl + (i & 3);
+  if ((lane & 16) == 0 && t < sq.len) put_weight(a, c, b, j, t, total);
 }
 
 // fp32: one wave per (16 keys of (b, j), part of the rows), 16 rows at a step.
