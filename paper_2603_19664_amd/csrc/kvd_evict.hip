@@ -62,13 +62,13 @@ constexpr int kEvictBins = 2 * kNtEvict;
 // NaN rows are counted apart) and goes on with the bin that holds it, at most three times;
 // a bin of up to 64 rows (the first one as a rule) is settled by one wave that compares
 // them.  Then rows are taken thread by thread in slot order: c consecutive slots each, c
-// odd (LDS banks), one prefix sum for the rows that tie with the last rank and one for
-// freed slots and movers.  Latency-bound: a thread keeps the ranks of its PER rows (t, t +
+// odd (LDS banks), one prefix sum for freed slots and movers, and before it one for the rows
+// that tie with the last rank unless all of those stay.  Latency-bound: a thread keeps the ranks of its PER rows (t, t +
 // 1024, ..) in registers, all its loads in flight at once, and LDS turns them into slot
 // order.  PER = 0: any length, ranks in the workspace.  16 caches of 8192 .. 16385 rows to
 // 2048: 88 us with 8-bit digits of the whole rank and serial bin walks, 28 us with ranks
 // read from LDS in every pass and four loads in flight, 26 us with three passes always,
-// 23 us so.
+// 21 us so.
 template <int PER>
 __global__ __launch_bounds__(kNtEvict) void evict_select_kernel(EvictArgs a) {
   __shared__ uint32_t lkeys[PER > 0 ? PER * kNtEvict : 1];
@@ -149,9 +149,10 @@ __global__ __launch_bounds__(kNtEvict) void evict_select_kernel(EvictArgs a) {
   hi = s_hi;
   uint32_t need = (uint32_t)left;  // rows still to be kept among those of rank <= hi
   uint32_t last = 0u;              // rank of the last row kept
-  bool found = false;
+  bool found = false, whole = false;  // whole: every row of that rank stays
   if (need <= s_top) {
     last = 0xffffffffu;
+    whole = need == s_top;
     found = true;
   } else {
     need -= s_top;
@@ -199,6 +200,7 @@ __global__ __launch_bounds__(kNtEvict) void evict_select_kernel(EvictArgs a) {
       hi = lo + ((1u << shift) - 1u);
       if (shift == 0) {
         last = lo;
+        whole = need == s_count;
         found = true;
       } else if (s_count <= 64u) {  // the bin's rows, compared by the first wave
         const auto gather = [&](uint32_t r) {
@@ -223,11 +225,13 @@ __global__ __launch_bounds__(kNtEvict) void evict_select_kernel(EvictArgs a) {
           if (lane < count && above < need && need <= above + same) {
             s_bin = mine;
             s_need = need - above;
+            s_count = same;
           }
         }
         __syncthreads();
         last = s_bin;
         need = s_need;
+        whole = need == s_count;
         found = true;
       }
     }
@@ -236,31 +240,29 @@ __global__ __launch_bounds__(kNtEvict) void evict_select_kernel(EvictArgs a) {
   const uint32_t ties = need;  // rows of rank `last` that stay: the lowest slots
   const int c = ((n + kNtEvict - 1) / kNtEvict) | 1;
   const int t0 = (int)min((long long)tid * c, (long long)n), t1 = min(t0 + c, n);
-  uint32_t eq = 0, total;
+  uint32_t eq0 = 0, total;
+  if (!whole) {
+    uint32_t eq = 0;
 #pragma unroll 8
-  for (int t = t0; t < t1; ++t) eq += keys[t] == last ? 1u : 0u;
-  const uint32_t eq0 = block_scan(eq, buf, total) - eq;
-  uint32_t e = eq0;
-  auto kept = [&](uint32_t r) { return r > last || (r == last && e++ < ties); };
-  uint32_t holes = 0, movers = 0;
-#pragma unroll 8
-  for (int t = t0; t < t1; ++t) {
-    const bool stays = kept(keys[t]);
-    holes += !stays && t < left ? 1u : 0u;
-    movers += stays && t >= left ? 1u : 0u;
+    for (int t = t0; t < t1; ++t) eq += keys[t] == last ? 1u : 0u;
+    eq0 = block_scan(eq, buf, total) - eq;
   }
-  uint32_t n_movers;
-  uint32_t h = block_scan(holes, buf, total) - holes;
-  uint32_t m = block_scan(movers, buf, n_movers) - movers;
+  uint32_t e = eq0;
+  auto kept = [&](uint32_t r) { return r > last || (r == last && (whole || e++ < ties)); };
+  // freed slots below `left` and, as many, movers behind it, in one sum
+  uint32_t count = 0;
+#pragma unroll 8
+  for (int t = t0; t < t1; ++t) count += kept(keys[t]) == (t >= left) ? 1u : 0u;
+  uint32_t at = block_scan(count, buf, total) - count;
   int2* mv = a.moves + (size_t)bj * a.max_moves;
   e = eq0;
 #pragma unroll 8
   for (int t = t0; t < t1; ++t) {
     const bool stays = kept(keys[t]);
     if (t < left) {
-      if (!stays) mv[h++].x = t;
+      if (!stays) mv[at++].x = t;
     } else if (stays) {
-      mv[m++].y = t;
+      mv[at++ - total / 2].y = t;
     } else if (keys[t] == last) {
       wt[t] = 0.0f;
     }
@@ -277,7 +279,7 @@ __global__ __launch_bounds__(kNtEvict) void evict_select_kernel(EvictArgs a) {
     for (int t = left + tid; t < n; t += kNtEvict)
       if (keys[t] < last) wt[t] = 0.0f;
   }
-  if (tid == 0) a.n_moves[bj] = (int)n_movers;
+  if (tid == 0) a.n_moves[bj] = (int)(total / 2);
 }
 
 // keep = T - 1: a cache of T rows loses its lightest one (of equal ones the highest slot),
