@@ -1313,11 +1313,14 @@ __global__ __launch_bounds__(256, 2) void weight_tile_kernel(RowsArgs a) {
   if ((lane & 16) == 0 && t < sq.len) put_weight(a, c, b, j, t, total);
 }
 
-// fp32: one wave per (16 keys of (b, j), part of the rows), 16 rows at a step.
+// fp32: one workgroup of 4 waves per (16 keys of (b, j), part of the rows), 16 rows at a step
+// and wave in turn (a wave's steps are round trips: 3 x 512 tokens of 9 heads 38 us with one
+// wave per workgroup, 19 with four), the waves' sums in wave order.
 template <int HD>
-__global__ __launch_bounds__(64) void weight_f32_kernel(RowsArgs a) {
+__global__ __launch_bounds__(256) void weight_f32_kernel(RowsArgs a) {
   constexpr int KC = HD / 16;
-  const int lane = threadIdx.x, rq = lane & 15, lg = lane >> 4;
+  __shared__ float part[4][16];
+  const int lane = threadIdx.x & 63, wv = wave_id(), rq = lane & 15, lg = lane >> 4;
   const int units = a.B * a.n_kv, x = (int)blockIdx.x / units, u = (int)blockIdx.x - x * units;
   const int j = u % a.n_kv, b = u / a.n_kv;
   const int c = x % a.S_w, tile = x / a.S_w;
@@ -1332,7 +1335,7 @@ __global__ __launch_bounds__(64) void weight_f32_kernel(RowsArgs a) {
 #pragma unroll
   for (int i = 0; i < KC; ++i) kf[i] = *reinterpret_cast<const f32x4_t*>(ks + 16 * i);
   float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int r0 = rs.r0; r0 < rs.r1; r0 += 16) {
+  for (int r0 = rs.r0 + 16 * wv; r0 < rs.r1; r0 += 64) {
     const int r = r0 + rq, fr = b * a.R + min(r, rs.r1 - 1);
     const float* qs = static_cast<const float*>(a.q) + q_off(a, j, fr, HD) + 4 * lg;
     f32x4_t s0 = {0.0f, 0.0f, 0.0f, 0.0f}, s1 = s0;
@@ -1357,9 +1360,11 @@ __global__ __launch_bounds__(64) void weight_f32_kernel(RowsArgs a) {
   for (int i = 0; i < 4; ++i) {
 #pragma unroll
     for (int o = 1; o < 16; o <<= 1) sum[i] += __shfl_xor(sum[i], o, 64);
-    const int t = k0 + 4 * lg + i;
-    if (rq == 0 && t < sq.len) put_weight(a, c, b, j, t, sum[i]);
+    if (rq == 0) part[wv][4 * lg + i] = sum[i];
   }
+  __syncthreads();
+  const int k = threadIdx.x;
+  if (k < 16 && k0 + k < sq.len) put_weight(a, c, b, j, k0 + k, (part[0][k] + part[1][k]) + (part[2][k] + part[3][k]));
 }
 
 // weight = decay weight + the sums of the parts that key t's tile has, in part order.
@@ -1419,7 +1424,7 @@ static hipError_t launch_rows_t(const RowsArgs& a, hipStream_t st) {
     if constexpr (BF)
       hipLaunchKernelGGL(weight_tile_kernel<HD>, dim3(items), dim3(256), 0, st, a);
     else
-      hipLaunchKernelGGL(weight_f32_kernel<HD>, dim3(items), dim3(64), 0, st, a);
+      hipLaunchKernelGGL(weight_f32_kernel<HD>, dim3(items), dim3(256), 0, st, a);
     KVD_LAUNCH_TRY(hipGetLastError());
     if (a.S_w > 1) {
       hipLaunchKernelGGL(weight_sum_kernel, dim3((unsigned)(a.B * a.n_kv * ((a.T_own + 255) / 256))), dim3(256), 0, st,
