@@ -412,7 +412,8 @@ size_t kvd_block_workspace_bytes(const kvd_attn_shape* shape, int32_t d_ff, int3
  *            Needs T_own >= 1.
  *   ws       kvd_prefix_workspace_bytes(shape, B, N, T_prefix, T_own, weight != NULL)
  *            bytes, 256-byte aligned, overwritten; it need not be cleared, and calls
- *            ordered on one stream may share it.
+ *            ordered on one stream may share it (not with calls that find their counters
+ *            cleared in theirs, kvd_workspace_bytes).
  * Results repeat bit for bit (no atomics), and out does not depend on whether weight
  * is given.  The shape's d_model, rms_eps, rope_theta and w_layout are not used.
  * bf16: where a key range has at most 16 rows (N * n_q_heads / n_kv_heads of an own
