@@ -13,6 +13,7 @@
 #include <string>
 
 #include "kvd_launch.h"
+#include "kvd_rows_layout.h"
 
 namespace {
 
@@ -878,18 +879,22 @@ namespace {
 // Launch geometry and workspace of a kvd_prefix_attn / kvd_weighted_attn call.
 //
 // bf16 rows stream their keys while one MFMA column block (16) holds them, else share
-// 128-row tiles; fp32 to waves of 16 rows.  A sequence whose own rows fill half
-// a block takes prefix and own keys in one pass (joint): the prefix is then shared by
-// its own rows, and neither half leaves a partial state.  So do calls of few rows and at most
-// kRowsSmall keys; a range of that many keys is one slot, and the call one launch.
+// 128-row tiles; fp32 to waves of 16 rows.  A sequence whose own rows fill their blocks to
+// 9 / 10, or two and more of them, takes prefix and own keys in one pass (joint): neither half
+// leaves a partial state of its own.  Others leave the prefix to blocks of all sequences' rows,
+// none of them empty (8 x 144 rows, prefix 3000: 28 us joint, 23 so; 6 x 120: 33.5 and 35).
+// Calls of few rows and at most kRowsSmall keys are joint too, and a range of that many keys is
+// one slot: one launch (8 tokens over 240 keys 8.7 us, 10.7 in two).
 struct RowsPlan {
   int32_t R, joint, prefix_few, own_few, S_prefix, C_prefix, S_own, C_own, S_w, P_w, sc_ld;
   size_t ml, acc, lse, sc, wpart, end;  // byte offsets in the workspace
   long long items;                      // workgroups of the largest attention or weight launch
 };
 
-// Slots of a key range that `units` items of `rows` rows in all share, each of at least
-// `least` keys and at most kRowsMostSlots; grows with keys.
+// Slots of a key range that `units` items of `rows` rows in all share, at most
+// kRowsMostSlots of at least kRowsLeastKeys keys each; grows with keys.  Few rows and fp32 take
+// half as many keys, a 16-key block per wave, up to 32 slots, which the merge still has in
+// flight at once (1000 keys 11.9 -> 11.1 us; 5000 keys in 64 slots 16.0 us, in 40 13.7).
 // Enough for `wgs` workgroups, but fewer than sqrt(keys kRowsStateRows / rows): a slot
 // leaves every row a state that is written and read, as dear as 1 / kRowsStateRows of a key in
 // a workgroup's range of keys / S.  (64 tokens, 8 heads of 256 over a prefix of 16384: 85
@@ -900,34 +905,35 @@ struct RowsPlan {
 // idle, about half a slot (keys / S / 2), against a slot's fixed cost of kRowsSlotKeys keys
 // (first loads, state written and merged) for every workgroup's units S / kRowsTargetWgs of
 // them.  A causal range (every row its own length) holds half of the keys.
-int32_t row_slots(long long units, long long rows, long long keys, int32_t least, bool causal,
+int32_t row_slots(long long units, long long rows, long long keys, bool few, bool causal,
                   bool beside = false, long long wgs = kvd::kRowsTargetWgs) {
   const double work = (double)units * kvd::kRowsSlotKeys * (causal ? 0.5 : 1.0);
   const long long balance = (long long)std::sqrt(0.5 * kvd::kRowsTargetWgs * (double)keys / work);
+  const long long least = kvd::kRowsLeastKeys, wide = (keys + least - 1) / least;
+  const long long most = few ? std::max(wide, std::min((keys + least / 2 - 1) / (least / 2), 32ll)) : wide;
   const double cost = (double)rows * (beside ? 1.5 : 1.0) / kvd::kRowsStateRows;
   const long long fill = std::min((wgs + units - 1) / units, (long long)std::sqrt((double)keys / cost));
-  return (int32_t)std::max(1ll, std::min({std::max(balance, fill), (keys + least - 1) / least,
-                                          (long long)kvd::kRowsMostSlots}));
+  return (int32_t)std::max(1ll, std::min({std::max(balance, fill), most, (long long)kvd::kRowsMostSlots}));
 }
 // Slots of T own rows of which the last N are the new tokens: causal while those are more
 // than half of them.  Never fewer for more rows.
-int32_t causal_slots(long long units, long long rows, int32_t T, int32_t least, int32_t N, bool beside,
+int32_t causal_slots(long long units, long long rows, int32_t T, bool few, int32_t N, bool beside,
                      long long wgs) {
-  const int32_t c = row_slots(units, rows, std::min<long long>(T, 2ll * N), least, N > 1, beside, wgs);
-  return 2ll * N > T ? c : std::max(c, row_slots(units, rows, T, least, false, beside, wgs));
+  const int32_t c = row_slots(units, rows, std::min<long long>(T, 2ll * N), few, N > 1, beside, wgs);
+  return 2ll * N > T ? c : std::max(c, row_slots(units, rows, T, few, false, beside, wgs));
 }
-// Keys per slot (a multiple of 64, at least `least`) and slots, as near to S as those allow.
-void cut_keys(long long keys, int32_t least, int32_t* S, int32_t* C) {
+// Keys per slot (a multiple of 64) and slots, as near to S as those allow.
+void cut_keys(long long keys, bool few, int32_t* S, int32_t* C) {
   const long long up = std::max<long long>((((keys + *S - 1) / *S) + 63) / 64 * 64, 64);
-  const long long down = std::max<long long>(up - 64, least);
+  const long long down = std::max<long long>(up - 64, few ? 64 : kvd::kRowsLeastKeys);
   const long long su = (keys + up - 1) / up, sd = (keys + down - 1) / down;
   const bool more = down < up && sd <= kvd::kRowsMostSlots && sd - *S <= *S - su;
   *S = (int32_t)(more ? sd : su);
   *C = (int32_t)(more ? down : up);
 }
-// What cut_keys makes of S at most: a slot of C >= 128 keys is off by 32 at most.
+// What cut_keys makes of S at most: a slot of C >= 64 keys is off by 32 at most.
 int32_t most_slots(int32_t S) {
-  return S > 1 ? std::min(S + (S + 3) / 4 + 1, kvd::kRowsMostSlots) : S;
+  return S > 1 ? std::min(S + (S + 1) / 2 + 1, kvd::kRowsMostSlots) : S;
 }
 
 // False when a size passes the kernels' 32-bit indexes or a launch's number of threads.
@@ -935,7 +941,6 @@ bool rows_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T_prefix, 
                RowsPlan* p) {
   const bool bf = s->dtype == KVD_BF16;
   const int32_t g = s->n_q_heads / s->n_kv_heads, RB = bf ? kvd::kRowsTile : kvd::kRowsWave;
-  const int32_t least = bf ? kvd::kRowsLeastKeys : kvd::kRowsLeastKeysF32;
   *p = RowsPlan{};
   const long long R = (long long)N * g, Rt = R * B, units = (long long)B * s->n_kv_heads;
   const long long keys = (long long)T_prefix + T_own;
@@ -943,26 +948,30 @@ bool rows_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T_prefix, 
   p->R = (int32_t)R;
   int32_t S = 0;  // slots for which the workspace has room: falls with no length
   const bool small = keys <= kvd::kRowsSmall;
-  p->joint = T_prefix > 0 && T_own > 0 && (R >= RB / 2 || (small && (!bf || R <= kvd::kRowsFew)));
   const long long nbo = (R + RB - 1) / RB, nbp = (Rt + RB - 1) / RB;
+  p->joint = T_prefix > 0 && T_own > 0 &&
+             (R >= 2 * RB || 10 * R >= 9 * nbo * RB || (small && (!bf || R <= kvd::kRowsFew)));
   const long long rows = Rt * s->n_kv_heads;
   if (p->joint) {
     p->own_few = bf && R <= kvd::kRowsFew;
-    p->S_own = small ? 1 : row_slots(units * nbo, rows, keys, least, false);
+    const bool few = p->own_few || !bf;
+    p->S_own = small ? 1 : row_slots(units * nbo, rows, keys, few, false);
     S = most_slots(p->S_own);
-    cut_keys(keys, least, &p->S_own, &p->C_own);
+    cut_keys(keys, few, &p->S_own, &p->C_own);
     p->items = units * nbo * p->S_own;
   } else {
     if (T_prefix > 0) {
       p->prefix_few = bf && Rt <= kvd::kRowsFew;
+      const bool few = p->prefix_few || !bf;
       const long long u = p->prefix_few ? s->n_kv_heads : s->n_kv_heads * nbp;
-      p->S_prefix = small && T_own == 0 ? 1 : row_slots(u, rows, T_prefix, least, false, T_own > 0);
+      p->S_prefix = small && T_own == 0 ? 1 : row_slots(u, rows, T_prefix, few, false, T_own > 0);
       S = most_slots(p->S_prefix);
-      if (!p->prefix_few) cut_keys(T_prefix, least, &p->S_prefix, &p->C_prefix);
+      if (!p->prefix_few) cut_keys(T_prefix, few, &p->S_prefix, &p->C_prefix);
       p->items += u * p->S_prefix;
     }
     if (T_own > 0) {
       p->own_few = bf && R <= kvd::kRowsFew;
+      const bool few = p->own_few || !bf;
       const long long u = p->own_few ? units : units * nbo;
       if (small && T_prefix == 0) {
         p->S_own = 1;
@@ -971,10 +980,10 @@ bool rows_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T_prefix, 
         // beside a prefix, the workgroups that it leaves (more would be a second round)
         const long long wgs = kvd::kRowsTargetWgs;
         const bool beside = p->items > 0;
-        p->S_own = causal_slots(u, rows, T_own, least, N, beside, beside ? std::max(wgs - p->items, u) / u * u : wgs);
-        S += most_slots(causal_slots(u, rows, T_own, least, N, beside, wgs));
+        p->S_own = causal_slots(u, rows, T_own, few, N, beside, beside ? std::max(wgs - p->items, u) / u * u : wgs);
+        S += most_slots(causal_slots(u, rows, T_own, few, N, beside, wgs));
       }
-      if (!p->own_few) cut_keys(T_own, least, &p->S_own, &p->C_own);
+      if (!p->own_few) cut_keys(T_own, few, &p->S_own, &p->C_own);
       p->items += u * p->S_own;
     }
   }

@@ -389,24 +389,6 @@ constexpr SaLds sa_lds(int hd, int G) {
   return L;
 }
 
-// Several query rows over stored keys (kvd_rows.hip).
-constexpr int kRowsTile = 128;    // rows per workgroup of the tile kernel
-constexpr int kRowsWave = 16;     // rows per wave of the fp32 kernel
-constexpr int kRowsFew = 16;      // rows rows_few takes (one MFMA column block)
-constexpr int kRowsTargetWgs = 512;
-constexpr int kRowsLeastKeys = 128;     // keys per slot, at least (bf16)
-constexpr int kRowsLeastKeysF32 = 128;
-constexpr int kRowsSlotKeys = 512;   // a slot's fixed cost in keys
-constexpr int kRowsStateRows = 96;   // rows whose states cost what a key costs a workgroup
-constexpr int kRowsMostSlots = 64;
-constexpr int kRowsSmall = 256;  // keys that one workgroup takes at once
-// Waves that share a row's S states when they are merged: a wave keeps 8 in flight, so that
-// many states are many round trips (512 rows of 66 states: 12.0 us with one wave per row, 9.2
-// with four).
-constexpr int rows_finish_waves(int S) { return S > 8 ? 4 : 1; }
-// A launch has fewer than 2^32 threads.
-constexpr long long most_wgs(int threads) { return ((1ll << 32) - 1) / threads; }
-
 // Value-absorbed fused attention (AbsorbArgs; head_dim 256).  Score tiles: K rows
 // x tokens per workgroup.
 enum ScoreTile { kScore512x64 = 0, kScore256x128 = 1, kScore256x64 = 2, kScoreTiles = 3 };

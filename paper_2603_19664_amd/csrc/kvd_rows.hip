@@ -22,6 +22,7 @@
 
 #include "kvd_device.hpp"
 #include "kvd_launch.h"
+#include "kvd_rows_layout.h"
 
 namespace kvd {
 
