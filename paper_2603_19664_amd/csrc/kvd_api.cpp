@@ -987,6 +987,7 @@ bool rows_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T_prefix, 
       p->items += u * p->S_own;
     }
   }
+  S = std::max(S, p->S_prefix + p->S_own);
   const int per_wg = 4 / kvd::rows_finish_waves(S);
   long long merge = S > 1 ? (rows + per_wg - 1) / per_wg : 0;
   size_t at = 0;

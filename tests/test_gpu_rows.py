@@ -90,6 +90,15 @@ def test_many_slots(dtype, hd, n_q, n_kv):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hd,n_q,n_kv", HEADS)
+def test_weights_of_long_prompts(dtype, hd, n_q, n_kv):
+    # a key's rows in several parts, of other numbers for early and late keys and for each sequence
+    run(dtype, n_q, n_kv, hd, 2, 300, 0, 700, [700, 350], [300, 123], weights=True, decay=0.5, pad=2)
+    run(dtype, n_q, n_kv, hd, 1, 400, 130, 400, weights=True)
+    run(dtype, n_q, n_kv, hd, 3, 260, 0, 260, [260, 1, 200], [260, 1, 0], weights=True, decay=1.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("N", [1, 4, 80])
 def test_sharp_and_far_scores(dtype, N):
     # scores of standard deviation 30: the running maximum moves often and most weights vanish
