@@ -63,6 +63,20 @@ __device__ __forceinline__ size_t q_off(const RowsArgs& a, int j, int fr, int hd
   return ((size_t)tok * a.n_q + (size_t)j * a.g + (fr - tok * a.g)) * hd;
 }
 
+// Whether the rb rows from row r_blk on of a sequence see no key beyond the call's first slot
+// (the first rows of a causal prompt): that slot's workgroup writes out itself, the others
+// nothing, and no state is merged (a 3001-token prompt 110 us instead of 114).
+__device__ __forceinline__ bool any_sole_slot(const RowsArgs& a) {  // of a call of several slots
+  return a.S_prefix == 0 && !a.own_few && a.sc == nullptr && (a.joint ? a.T_prefix : 0) < a.C_own &&
+         (a.own_len != nullptr || a.T_own - a.N < a.C_own);
+}
+__device__ __forceinline__ bool sole_slot(const RowsArgs& a, const Seq& sq, int r_blk, int rb) {
+  if (a.S_prefix + a.S_own == 1) return true;
+  if (!any_sole_slot(a)) return false;
+  const int seen = rows_seen(sq, token_of(a, min(r_blk + rb, sq.n * a.g) - 1));
+  return (long long)(a.joint ? a.T_prefix : 0) + seen <= a.C_own;
+}
+
 // A range of keys [k0, k1) of KV head j: of the prefix, or of sequence b's own rows.
 struct KeyRange {
   size_t row;  // first key's row in the K and V arrays
@@ -202,6 +216,8 @@ __device__ __forceinline__ void rows_tile(const RowsArgs& a, int item, uint16_t*
   const int slot = own ? a.S_prefix + s : s;
   const int r_blk = blk * kRowsTile;
   if (own && r_blk >= sq.n * a.g) return;  // no row of this block is asked for
+  const bool direct = own ? sole_slot(a, sq, r_blk, kRowsTile) : a.S_prefix + a.S_own == 1;
+  if (direct && s > 0) return;
   // key range of the item
   int p0 = 0, p1 = 0, o0 = 0, o1 = 0;
   if (!own) {
@@ -392,7 +408,6 @@ again:
   }
   if (!wanted) return;
   const float m_out = m_run == -INFINITY ? 0.0f : m_run;
-  const bool direct = a.S_prefix + a.S_own == 1;
   const size_t row = slot_row(a, slot, j, fr);
   if (hl == 0) {
     a.ml[2 * row] = m_out;
@@ -819,6 +834,8 @@ __global__ __launch_bounds__(256) void rows_f32_kernel(RowsArgs a) {
   const int slot = own ? a.S_prefix + s : s;
   const int r_blk = blk * kRowsWave;
   if (own && r_blk >= sq.n * a.g) return;
+  const bool direct = own ? sole_slot(a, sq, r_blk, kRowsWave) : a.S_prefix + a.S_own == 1;
+  if (direct && s > 0) return;
   int p0 = 0, p1 = 0, o0 = 0, o1 = 0;
   if (!own) {
     p0 = s * a.C_prefix;
@@ -989,7 +1006,6 @@ __global__ __launch_bounds__(256) void rows_f32_kernel(RowsArgs a) {
         o[u][3][r] = fmaf(wt, y.w, o[u][3][r]);
       }
   }
-  const bool direct = a.S_prefix + a.S_own == 1;
   const size_t row = slot_row(a, slot, j, fr);
   if (lg == 0) {
     a.ml[2 * row] = Mu;
@@ -1051,7 +1067,12 @@ __global__ __launch_bounds__(256) void rows_finish_kernel(RowsArgs a, int merge_
     const int Rt = a.B * a.R;
     const bool in = idx < (long long)Rt * a.n_kv;
     const int j = in ? (int)(idx / Rt) : 0, fr = in ? (int)(idx - (long long)j * Rt) : 0;
-    const bool on = in && row_wanted(a, fr);
+    bool on = in && row_wanted(a, fr);
+    if (any_sole_slot(a) && on) {
+      constexpr int RB = sizeof(T) == 2 ? kRowsTile : kRowsWave;
+      const int b = fr / a.R;
+      on = !sole_slot(a, seq_of(a, b), (fr - b * a.R) / RB * RB, RB);
+    }
     if (WPR == 1 && !on) return;
     float2 s0, s1;
     load_states(a, S, j, fr, lane, s0, s1);
