@@ -197,6 +197,17 @@ def test_repeats_and_shared_workspace(dtype, N, T_prefix, T):
     assert torch.equal(outs[0][0], outs[2][0]) and torch.equal(outs[0][1], outs[2][1])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,N,T_prefix,T", [(2, 1, 0, 100), (3, 1, 60, 500), (2, 4, 0, 900), (2, 2, 1000, 90),
+                                            (2, 50, 0, 400), (2, 30, 300, 200), (1, 150, 40, 500)])
+def test_out_is_the_same_with_weights_and_without(dtype, B, N, T_prefix, T):
+    s = shape(dtype, 6, 2, 64)
+    x = make(dtype, 6, 2, 64, B, N, T_prefix, T, 13)
+    lens = [T, T // 3][:B] + [1] * (B - 2)
+    assert torch.equal(call(s, x, T_prefix, T, lens), call(s, x, T_prefix, T, lens, None, x["weight"], 1.0))
+
+
+
 def test_weighted_is_prefix_without_a_prefix():
     s = shape("bf16", 6, 2, 128)
     x = make("bf16", 6, 2, 128, 2, 3, 0, 200, 9)
