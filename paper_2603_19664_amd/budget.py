@@ -150,7 +150,8 @@ class WeightedCache:
     Rows past the budget collect in `room` further slots (the tokens of one call at most); then kvd_evict keeps the
     `budget` heaviest: the first `sink` positions and the newest `recent` ones always, the others by the weight
     that kvd_prefix_attn has added up, `decay` times the earlier weight at every call (1: over the whole past, 0: the
-    last call's alone).  Slots are reused, so row order says nothing about age; pos holds every row's position.
+    last call's alone).  Slots are reused, so row order says nothing about age; pos holds every row's token, counted
+    from 0 behind the prefix (sink and recent count these tokens).
 
     prefix: (K, V) of [n_kv, T_prefix, head_dim], shared by the batch: its tokens sit at positions pos0 ..
     pos0 + T_prefix - 1 of every sequence, the sequences' own from pos0 + T_prefix on.

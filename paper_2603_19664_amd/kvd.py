@@ -521,7 +521,7 @@ def _dev_ptr(t, name, dtype, dev):
 
 
 def _device_of(t, name):
-    if t.device.type != "cuda":
+    if not t.is_cuda:
         raise ValueError(f"{name} must be a torch tensor on the GPU")
     return t.get_device()
 
@@ -555,12 +555,13 @@ def _prefix_call(fn, shape, q, prefix, T_prefix, own, T_own, own_t_off, out, ws,
     # extents first, of everything; then devices, dtypes and layouts; then the call
     if not isinstance(q, torch.Tensor) or q.dim() not in (3, 4):
         raise ValueError("q must be a [B, N, n_q, head_dim] or [B, n_q, head_dim] tensor")
-    B, N = q.shape[0], q.shape[1] if q.dim() == 4 else 1
-    if q.shape[-2:] != (shape.n_q_heads, shape.head_dim):
-        raise ValueError(f"q has shape {tuple(q.shape)}, expected [.., {shape.n_q_heads}, {shape.head_dim}]")
+    dims = q.shape
+    B, N = dims[0], dims[1] if len(dims) == 4 else 1
+    if dims[-1] != shape.head_dim or dims[-2] != shape.n_q_heads:
+        raise ValueError(f"q has shape {tuple(dims)}, expected [.., {shape.n_q_heads}, {shape.head_dim}]")
     if out is None:
         raise ValueError("out is required")
-    _dims(out, "out", q.shape)
+    _dims(out, "out", dims)
     pk = pv = k = v = None
     t_cap = 0
     if T_prefix > 0:
