@@ -416,10 +416,9 @@ size_t kvd_block_workspace_bytes(const kvd_attn_shape* shape, int32_t d_ff, int3
  *            cleared in theirs, kvd_workspace_bytes).
  * Results repeat bit for bit (no atomics), and out does not depend on whether weight
  * is given.  The shape's d_model, rms_eps, rope_theta and w_layout are not used.
- * bf16: where a key range has at most 16 rows (N * n_q_heads / n_kv_heads of an own
- * range or a small call, B times as many of a prefix) the softmax weights enter the value
- * product as the sum of two bf16 parts, elsewhere rounded to one bf16.  Sums of p V are
- * taken before the division by sum p, so |V| near the largest float overflows.
+ * bf16: the softmax weights enter the value product as the sum of two bf16 parts (2^-17 of a
+ * weight is lost), however many rows a call has.  Sums of p V are taken before the division by
+ * sum p, so |V| near the largest float overflows.
  * B == 0 or N == 0 is a no-op.                                                  */
 kvd_status kvd_prefix_attn(const kvd_attn_shape* shape, const void* q, int32_t N,
                            const kvd_kv_view* prefix, int32_t T_prefix, const kvd_kv_view* own,

@@ -182,9 +182,11 @@ __device__ __forceinline__ float poison_of(float codes) {
 // t is computed.  S^T = K Q^T (A: 32 keys from LDS, B: the wave's rows, in registers):
 // a lane holds scores of one row, so its running maximum and sum need one exchange with
 // lane ^ 32.  The maximum moves only by steps of more than 2^8, so that O is rescaled
-// in few tiles.  O^T += V^T P^T with P^T straight from the score registers, rounded to
-// bf16 (each weight off by at most 2^-9 of itself, as much as the output's own
-// rounding; the sum is taken before the rounding).
+// in few tiles.  O^T += V^T P^T with P^T straight from the score registers, as the sum of
+// two bf16 parts (2^-17 of a weight is lost).  Rounded to one part, each weight was off by up to
+// 2^-8: the output's error grew from 1.6e-3 to 2.3e-3, and a token's precision hung on how many
+// shared its batch (8 prompts over 8192 keys 128 us so, 155 with both parts; a 3001-token
+// prompt 110 and 122).
 template <int HD>
 __device__ __forceinline__ void rows_tile(const RowsArgs& a, int item, uint16_t* buf0, uint16_t* buf1) {
   constexpr int KT = rows_kt(HD), KH = KT / 32, KS = HD / 16, DB = HD / 32, kLead = 4;
@@ -344,28 +346,36 @@ again:
         for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
     }
     const float m_use = m_run == -INFINITY ? 0.0f : m_run;
-    bf16x8_t pf[2 * KH];
+    // P as two bf16 parts, p = hi + lo: hi's rounding error is lo
+    bf16x8_t hi[2 * KH], lo[2 * KH];
     float sum = 0.0f;
 #pragma unroll
     for (int tt = 0; tt < 2 * KH; ++tt) {
-      uint32_t pw[4];
+      uint32_t hw[4], lw[4];
 #pragma unroll
       for (int e = 0; e < 8; e += 2) {
         const int r = 8 * (tt & 1) + e;
         const float pa = exp2_hw(fmaf(st[tt >> 1][r], ScoreScale<HD>::v, -m_use));
         const float pb = exp2_hw(fmaf(st[tt >> 1][r + 1], ScoreScale<HD>::v, -m_use));
         sum += pa + pb;
-        pw[e >> 1] = pack_bf16x2(pa, pb);
+        hw[e >> 1] = pack_bf16x2(pa, pb);
+        lw[e >> 1] = pack_bf16x2(pa - bf_lo(hw[e >> 1]), pb - bf_hi(hw[e >> 1]));
       }
-      pf[tt] = __builtin_bit_cast(bf16x8_t, make_uint4(pw[0], pw[1], pw[2], pw[3]));
+      hi[tt] = __builtin_bit_cast(bf16x8_t, make_uint4(hw[0], hw[1], hw[2], hw[3]));
+      lo[tt] = __builtin_bit_cast(bf16x8_t, make_uint4(lw[0], lw[1], lw[2], lw[3]));
     }
     l_run += sum;  // this lane's keys; lane ^ 32 holds the others
     const uint32_t vbase = fresh(v_base<HD>(lane));
 #pragma unroll
     for (int tt = 0; tt < 2 * KH; ++tt)
 #pragma unroll
-      for (int db = 0; db < DB; ++db)
-        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_operand<HD>(vs, vbase, 16 * tt, db), pf[tt], o[db], 0, 0, 0);
+      for (int db = 0; db < DB; db += 2) {
+        const bf16x8_t v0 = v_operand<HD>(vs, vbase, 16 * tt, db), v1 = v_operand<HD>(vs, vbase, 16 * tt, db + 1);
+        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v0, hi[tt], o[db], 0, 0, 0);
+        o[db + 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v1, hi[tt], o[db + 1], 0, 0, 0);
+        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v0, lo[tt], o[db], 0, 0, 0);
+        o[db + 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v1, lo[tt], o[db + 1], 0, 0, 0);
+      }
   };
   if (nt > 0) load(0, buf0);
   for (int t = 0; t < nt; t += 2) {
