@@ -584,9 +584,10 @@ __device__ __forceinline__ void rows_few(const RowsArgs& a, int item, uint16_t* 
 
   f32x4_t o[DB];
   float m_run, l_run;
-  // as in rows_tile: a second pass without the infinite and NaN values that met a weight
-  // of 0 (a row that does not see them)
+  // as in rows_tile: a second pass without infinite and NaN values, which the parts of a weight
+  // (lo is 0 or negative as often as not) and the weights of rows that do not see them make NaN
   int pass = 0;
+  unsigned long long bad = 0;  // bit i % 64: block i of the wave holds such a value
 again:
 #pragma unroll
   for (int db = 0; db < DB; ++db) o[db] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
@@ -651,13 +652,16 @@ again:
     const uint2 pl = make_uint2(pack_bf16x2(lo[0], lo[1]), pack_bf16x2(lo[2], lo[3]));
     const s16x4_t pfh = __builtin_bit_cast(s16x4_t, ph), pfl = __builtin_bit_cast(s16x4_t, pl);
     if constexpr (ONE) wait_copies<NEXT ? KC : 0>();  // V; the next block's K was issued after it
-    if (masked && pass == 1) {
+    if (pass == 1) {
+      uint32_t found = 0;
 #pragma unroll 1
       for (int x = lane; x < 16 * HD / 2; x += 64) {
         uint32_t* at = reinterpret_cast<uint32_t*>(vs) + x;
         const uint32_t f = nonfinite2(*at);
+        found |= f;
         if (f != 0) *at &= (f & 0x8000u ? 0u : 0xffffu) | (f & 0x80000000u ? 0u : 0xffff0000u);
       }
+      if (__any(found != 0)) bad |= 1ull << (i & 63);
     }
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
@@ -710,12 +714,12 @@ again:
     goto again;
   }
   if (pass == 1) {
-    // the values that pass 1 took as 0 in masked blocks, for the rows that see them
+    // the values that pass 1 took as 0, for the rows that see them
 #pragma unroll 1
     for (int i = 0; i < nb; ++i) {
+      if ((bad >> (i & 63) & 1) == 0) continue;
       const bool is_own = w + NW * i >= pblk;
       const int kb = kSaBlock * (w + NW * i - (is_own ? pblk : 0));
-      if (kb + kSaBlock <= (is_own ? all : kp.n)) continue;
 #pragma unroll 1
       for (int t = kb; t < min(kb + kSaBlock, is_own ? lim : kp.n); ++t) {
         const uint16_t* vr = (is_own ? Vo : Vp) + (size_t)t * HD + 4 * lg;
