@@ -176,6 +176,10 @@ __device__ __forceinline__ float poison_of(float codes) {
   const bool pos = (c & 127) != 0, neg = ((c >> 7) & 127) != 0;
   return c >= 16384 || (pos && neg) ? __uint_as_float(0x7fc00000u) : pos ? INFINITY : -INFINITY;
 }
+// x + w y of partial sums, where a weight that 32 bits took as 0 does not make an infinity NaN.
+__device__ __forceinline__ float add_state(float x, float w, float y) {
+  return fabsf(y) < INFINITY ? fmaf(w, y, x) : x + y;
+}
 // One workgroup of 4 waves per (128-row block, key range), 32 rows per wave, through
 // the range's key tiles: first its prefix keys, then its own ones (one of them empty
 // unless the call is joint).  Tile t + 1 is copied into the other LDS buffer while tile
@@ -814,14 +818,15 @@ __global__ __launch_bounds__(256, 2) void rows_bf16_kernel(RowsArgs a, int tile_
 // lane's 16 bytes of V row 4 lg + t (dims 64 u + 4 (lane % 16) ..) are the A operands of
 // four MFMAs, MFMA e giving dims 64 u + 4 i + e.  Both operands come straight from memory;
 // LDS only merges the waves.  With a.sc (at most 16 rows) the scores of own keys are kept
-// for the weights.  Masked keys: score -inf; a non-finite value that some row does
-// not see is taken out of the product, and its code (code_of), summed over the keys a row
-// does see, puts it back.
+// for the weights.  Masked keys: score -inf.  Where O comes out non-finite, a second pass takes
+// V's non-finite values out of the products, and their codes (code_of), summed over the
+// keys of a block that a row sees, put them back after the last rescaling.
 template <int HD>
 __global__ __launch_bounds__(256) void rows_f32_kernel(RowsArgs a) {
   constexpr int KC = HD / 16, VU = HD / 64;
   __shared__ __align__(16) float part[3][16][HD + 4];
   __shared__ float ml[4][16][2];
+  __shared__ int passes[4];
   const int lane = threadIdx.x & 63, w = wave_id(), rq = lane & 15, lg = lane >> 4;
   const int nbo = (a.R + kRowsWave - 1) / kRowsWave;
   const int own_items = a.B * a.n_kv * nbo * a.S_own;
@@ -877,12 +882,16 @@ __global__ __launch_bounds__(256) void rows_f32_kernel(RowsArgs a) {
     for (int c = 0; c < KC; ++c) q[c] = *reinterpret_cast<const f32x4_t*>(qs + 16 * c);
   }
   f32x4_t o[VU][4];
+  float m_run, l_run;
+  const bool wanted = rl < nr && row_wanted(a, fr);
+  int pass = 0;
+again:
 #pragma unroll
   for (int u = 0; u < VU; ++u)
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[u][e] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-  float m_run = -INFINITY, l_run = 0.0f;
-
+  m_run = -INFINITY;
+  l_run = 0.0f;
   for (int t = w; t < nt; t += 4) {
     const bool is_own = t >= np;
     const KeyRange& kr = is_own ? ko : kp;
@@ -910,15 +919,12 @@ __global__ __launch_bounds__(256) void rows_f32_kernel(RowsArgs a) {
       }
     // key k0 + 4 lg + r, row rq
     float sv[4], mx = -INFINITY;
-    bool unseen = false;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const bool in = k0 + 4 * lg + r < row_lim;
-      unseen |= !in;
-      sv[r] = in ? (s0[r] + s1[r]) * ScoreScale<HD>::v : -INFINITY;
+      sv[r] = k0 + 4 * lg + r < row_lim ? (s0[r] + s1[r]) * ScoreScale<HD>::v : -INFINITY;
       mx = fmaxf(mx, sv[r]);
     }
-    if (a.sc != nullptr && is_own && rl < nr) {
+    if (a.sc != nullptr && is_own && rl < nr && pass == 0) {
       float* sc = a.sc + (((size_t)b * a.n_kv + j) * a.R + rl) * a.sc_ld + o0 + k0 + 4 * lg;
 #pragma unroll
       for (int r = 0; r < 4; ++r)
@@ -938,41 +944,64 @@ __global__ __launch_bounds__(256) void rows_f32_kernel(RowsArgs a) {
     for (int u = 0; u < VU; ++u)
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[u][e] *= alpha;
-    bool odd = false;
-    if (__any(unseen)) {
+    if (pass == 1) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int u = 0; u < VU; ++u)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) odd |= !(fabsf(vf[i][u][e]) < INFINITY);
-      odd = __any(odd);
+          for (int e = 0; e < 4; ++e) vf[i][u][e] = fabsf(vf[i][u][e]) < INFINITY ? vf[i][u][e] : 0.0f;
     }
-    if (!odd) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int u = 0; u < VU; ++u)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            o[u][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[i][u][e], p[i], o[u][e], 0, 0, 0);
-    } else {
+    for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int u = 0; u < VU; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          o[u][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[i][u][e], p[i], o[u][e], 0, 0, 0);
+  }
+  if (pass == 0) {
+    float x = 0.0f;
+#pragma unroll
+    for (int u = 0; u < VU; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x = fmaf(o[u][e][r], 0.0f, x);
+    if (__any(wanted && x != 0.0f)) {
+      pass = 1;
+      goto again;
+    }
+  } else {
+    // the values that pass 1 took as 0, for the rows that see them
+#pragma unroll 1
+    for (int t = w; t < nt; t += 4) {
+      const bool is_own = t >= np;
+      const KeyRange& kr = is_own ? ko : kp;
+      const float* V = static_cast<const float*>(is_own ? a.v : a.pv) + kr.row * HD;
+      const int k0 = 16 * (is_own ? t - np : t), row_lim = is_own ? lim : kp.n;
+#pragma unroll
+      for (int u = 0; u < VU; ++u) {
+        f32x4_t vf[4];
+        float x = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          vf[i] = *reinterpret_cast<const f32x4_t*>(V + (size_t)min(k0 + 4 * lg + i, kr.n - 1) * HD + 4 * rq + 64 * u);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x = fmaf(vf[i][e], 0.0f, x);
+        }
+        if (!__any(x != 0.0f)) continue;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           f32x4_t codes = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float v = vf[i][u][e];
-            const bool fin = fabsf(v) < INFINITY;
-            o[u][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(fin ? v : 0.0f, p[i], o[u][e], 0, 0, 0);
-            codes = __builtin_amdgcn_mfma_f32_16x16x4f32(fin ? 0.0f : code_of(v), k0 + 4 * lg + i < row_lim ? 1.0f : 0.0f,
-                                                         codes, 0, 0, 0);
-          }
+          for (int i = 0; i < 4; ++i)
+            codes = __builtin_amdgcn_mfma_f32_16x16x4f32(fabsf(vf[i][e]) < INFINITY ? 0.0f : code_of(vf[i][e]),
+                                                         k0 + 4 * lg + i < row_lim ? 1.0f : 0.0f, codes, 0, 0, 0);
 #pragma unroll
           for (int r = 0; r < 4; ++r) o[u][e][r] += poison_of(codes[r]);
         }
+      }
     }
   }
   l_run += __shfl_xor(l_run, 16, 64);
@@ -983,6 +1012,7 @@ __global__ __launch_bounds__(256) void rows_f32_kernel(RowsArgs a) {
     ml[w][rq][0] = m_run;
     ml[w][rq][1] = l_run;
   }
+  if (lane == 0) passes[w] = pass;
   if (w > 0) {
 #pragma unroll
     for (int u = 0; u < VU; ++u)
@@ -992,34 +1022,41 @@ __global__ __launch_bounds__(256) void rows_f32_kernel(RowsArgs a) {
             make_float4(o[u][0][r], o[u][1][r], o[u][2][r], o[u][3][r]);
   }
   __syncthreads();
-  if (w > 0 || rl >= nr || !row_wanted(a, fr)) return;
+  if (w > 0 || !wanted) return;
   float M = m_run;
 #pragma unroll
   for (int v = 1; v < 4; ++v) M = fmaxf(M, ml[v][rq][0]);
   const float Mu = M == -INFINITY ? 0.0f : M;
-  {
-    const float wt = exp2_hw(m_run - Mu);
-    l_run *= wt;
+  // SPOILT: a wave took its second pass, so that states may hold infinities
+  auto merge = [&](auto spoilt) {
+    constexpr bool SPOILT = decltype(spoilt)::value != 0;
+    const float w0 = exp2_hw(m_run - Mu);
+    l_run *= w0;
 #pragma unroll
     for (int u = 0; u < VU; ++u)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[u][e] *= wt;
-  }
+      for (int e = 0; e < 4; ++e)
 #pragma unroll
-  for (int v = 1; v < 4; ++v) {
-    const float wt = exp2_hw(ml[v][rq][0] - Mu);
-    l_run = fmaf(wt, ml[v][rq][1], l_run);
+        for (int r = 0; r < 4; ++r) o[u][e][r] = SPOILT ? add_state(0.0f, w0, o[u][e][r]) : w0 * o[u][e][r];
 #pragma unroll
-    for (int u = 0; u < VU; ++u)
+    for (int v = 1; v < 4; ++v) {
+      const float wt = exp2_hw(ml[v][rq][0] - Mu);
+      l_run = fmaf(wt, ml[v][rq][1], l_run);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float4 y = *reinterpret_cast<const float4*>(&part[v - 1][rq][64 * u + 16 * lg + 4 * r]);
-        o[u][0][r] = fmaf(wt, y.x, o[u][0][r]);
-        o[u][1][r] = fmaf(wt, y.y, o[u][1][r]);
-        o[u][2][r] = fmaf(wt, y.z, o[u][2][r]);
-        o[u][3][r] = fmaf(wt, y.w, o[u][3][r]);
-      }
-  }
+      for (int u = 0; u < VU; ++u)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const f32x4_t y = *reinterpret_cast<const f32x4_t*>(&part[v - 1][rq][64 * u + 16 * lg + 4 * r]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            o[u][e][r] = SPOILT ? add_state(o[u][e][r], wt, y[e]) : fmaf(wt, y[e], o[u][e][r]);
+        }
+    }
+  };
+  if (passes[0] + passes[1] + passes[2] + passes[3] > 0)
+    merge(IC<1>{});
+  else
+    merge(IC<0>{});
   const size_t row = slot_row(a, slot, j, fr);
   if (lg == 0) {
     a.ml[2 * row] = Mu;

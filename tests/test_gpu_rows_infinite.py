@@ -1,5 +1,6 @@
-"""Infinite and NaN values of rows that a token sees, wherever they lie: the column is infinite, NaN with both signs or
-a NaN, and every other column and every token that does not see the row keep their bits."""
+"""Infinite and NaN values of rows that a token sees, wherever they lie and however small their weight (no softmax weight
+of a finite score is zero): the column is infinite, NaN with both signs or a NaN, and every other column and every token
+that does not see the row keep their bits."""
 import pytest
 import torch
 
@@ -84,6 +85,29 @@ def test_both_signs(dtype, n_q, n_kv, N):
         spoil(x, a, INF, 5)
         spoil(x, b, -INF, 5)
         check(call(s, x, T_prefix, T), clean, range(N), 5, NAN, "both")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hd", [64, 256])
+@pytest.mark.parametrize("n_q,n_kv,N", ROWS)
+@pytest.mark.parametrize("T_prefix,T", LENGTHS)
+def test_weights_below_the_smallest_number(dtype, hd, n_q, n_kv, N, T_prefix, T):
+    # the row's weight is e^(-40 sqrt(hd)) of the others': 0 in 32 bits, yet not zero
+    if T and T < N:
+        T = N
+    s = shape(dtype, n_q, n_kv, hd)
+    x = make(dtype, n_q, n_kv, hd, 2, N, T_prefix, T, 45)
+    x["q"].fill_(1.0)
+    for n, at in enumerate(places(T_prefix, T, N)):
+        if at == ("", 0) and not T_prefix and T == N:
+            continue  # token 0 sees that row alone: its weight is one
+        y = {m: t.clone() for m, t in x.items()}
+        y[at[0] + "k"][..., at[1], :] = -40.0
+        clean = call(s, y, T_prefix, T)
+        assert torch.isfinite(clean).all()
+        bad, column = (INF, -INF, NAN)[n % 3], (5 * n + 1) % hd
+        spoil(y, at, bad, column)
+        check(call(s, y, T_prefix, T), clean, seen_by(at, T, N), column, bad, f"{at} {bad}")
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
