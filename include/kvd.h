@@ -396,6 +396,8 @@ size_t kvd_block_workspace_bytes(const kvd_attn_shape* shape, int32_t d_ff, int3
  * A token that sees no row gives out = 0.  Tokens i >= n[b] are not computed and
  * their out rows are left as they were.  Own rows from len on are never read, and
  * what a token does not see has no part in its result, whatever it holds.
+ * An infinite value that it sees makes its column infinite (NaN with both signs), however
+ * small the row's weight.
  *   q, out   [B][N][n_q_heads][head_dim].
  *   prefix   K/V [n_kv_heads][t_cap][head_dim], rows t_off .. t_off+T_prefix-1;
  *            may be NULL iff T_prefix == 0.

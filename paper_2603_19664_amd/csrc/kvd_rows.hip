@@ -774,6 +774,16 @@ again:
       x += wt * *reinterpret_cast<const f32x4_t*>(f + (v * 16 + h) * HH + 4 * ((c4 & CM) ^ (h & CM)));
       L = fmaf(wt, ml[v][h][1], L);
     }
+    if (fmaf(x[0], 0.0f, fmaf(x[1], 0.0f, fmaf(x[2], 0.0f, x[3] * 0.0f))) != 0.0f) {  // 0 x infinity, perhaps
+      x = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+      for (int v = 0; v < NW; ++v) {
+        const float wt = exp2_hw(ml[v][h][0] - Mu);
+        const f32x4_t y = *reinterpret_cast<const f32x4_t*>(f + (v * 16 + h) * HH + 4 * ((c4 & CM) ^ (h & CM)));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = add_state(x[e], wt, y[e]);
+      }
+    }
     const size_t row = slot_row(a, slot, j, fr0 + h);
     if (direct) {
       if (row_wanted(a, fr0 + h)) {
@@ -1131,31 +1141,41 @@ __global__ __launch_bounds__(256) void rows_finish_kernel(RowsArgs a, int merge_
     if (a.lse != nullptr && on && lane == 0 && w % WPR == 0)
       a.lse[(size_t)j * Rt + fr] = m.L != 0.0f ? m.M + __builtin_amdgcn_logf(m.L) : INFINITY;
     float x[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = 0.0f;
     // the states that hold keys (every WPR-th of them), 8 at a time in flight; an empty
     // state has no acc
     const float* src = a.acc + slot_row(a, 0, j, fr) * HD + E * lane;
     const size_t step = (size_t)a.n_kv * Rt * HD;
+    auto gather = [&](auto spoilt) {
+      constexpr bool SPOILT = decltype(spoilt)::value != 0;
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const float wv = half == 0 ? m.w0 : m.w1;
-      unsigned long long left = __ballot(wv != 0.0f && lane % WPR == w % WPR);
-      while (left != 0) {
-        float y[8][E], wt[8];
+      for (int e = 0; e < E; ++e) x[e] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int s = left != 0 ? __builtin_ctzll(left) : 0;
-          wt[i] = left != 0 ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wv), s)) : 0.0f;
-          if (left != 0) load_e<E>(src + (size_t)(s + 64 * half) * step, y[i]);
-          left &= left - 1;
+      for (int half = 0; half < 2; ++half) {
+        const float wv = half == 0 ? m.w0 : m.w1, sum = half == 0 ? s0.y : s1.y;
+        unsigned long long left = __ballot(sum != 0.0f && lane % WPR == w % WPR);
+        while (left != 0) {
+          float y[8][E], wt[8];
+          const int n = __popcll(left);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int s = left != 0 ? __builtin_ctzll(left) : 0;
+            wt[i] = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wv), s));
+            if (left != 0) load_e<E>(src + (size_t)(s + 64 * half) * step, y[i]);
+            left &= left - 1;
+          }
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+              x[e] = i >= n ? x[e] : SPOILT ? add_state(x[e], wt[i], y[i][e]) : fmaf(y[i][e], wt[i], x[e]);
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-          for (int e = 0; e < E; ++e) x[e] = wt[i] != 0.0f ? fmaf(y[i][e], wt[i], x[e]) : x[e];
       }
-    }
+    };
+    gather(IC<0>{});
+    float z = 0.0f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) z = fmaf(x[e], 0.0f, z);
+    if (__any(z != 0.0f)) gather(IC<1>{});  // 0 x infinity, perhaps
     if constexpr (WPR > 1) {  // one row per workgroup: its waves' sums in wave order
       __shared__ float part[WPR][HD];
 #pragma unroll

@@ -111,6 +111,30 @@ def test_weights_below_the_smallest_number(dtype, hd, n_q, n_kv, N, T_prefix, T)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hd", [64, 128, 256])
+@pytest.mark.parametrize("n_q,n_kv,N", ROWS)
+@pytest.mark.parametrize("T_prefix,T", LENGTHS)
+def test_ranges_below_the_smallest_number(dtype, hd, n_q, n_kv, N, T_prefix, T):
+    # so are the weights of every other row up to it: whole waves' and whole slots' states merge with a factor of 0
+    T = max(T, N) if T else 0
+    s = shape(dtype, n_q, n_kv, hd)
+    x = make(dtype, n_q, n_kv, hd, 2, N, T_prefix, T, 49)
+    x["q"].fill_(1.0)
+    low = T_prefix if T_prefix and T else (T_prefix or T - N + 1) // 2
+    if low == 0:
+        return  # token 0 sees one row
+    at = "p" if T_prefix else ""
+    x[at + "k"][..., :low, :] = -40.0
+    clean = call(s, x, T_prefix, T)
+    assert torch.isfinite(clean).all()
+    for n, row in enumerate(sorted({0, low // 2, low - 1})):
+        bad, column = (INF, -INF, NAN)[n], (5 * n + 1) % hd
+        y = dict(x, v=x["v"].clone(), pv=x["pv"].clone())
+        spoil(y, (at, row), bad, column)
+        check(call(s, y, T_prefix, T), clean, range(N), column, bad, f"{row} of {low} {bad}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("n_q,n_kv,N", ROWS)
 def test_weights_of_such_calls(dtype, n_q, n_kv, N):
     # the weights that rows receive come from q and K alone
