@@ -271,6 +271,7 @@ __device__ __forceinline__ void rows_tile(const RowsArgs& a, int item, uint16_t*
   // A second pass where an infinite or NaN value met a weight of 0 (a row that does not
   // see it): such values count as 0 there and are added afterwards where they are seen.
   int pass = 0;
+  unsigned long long bad = 0;  // bit t % 64: tile t holds such a value
 again:
 #pragma unroll
   for (int db = 0; db < DB; ++db)
@@ -285,12 +286,14 @@ again:
     __syncthreads();                     // every wave's share, and tile t - 1 is no longer read
     if (t + 1 < nt) load(t + 1, next);
     if (pass == 1) {
+      uint32_t found = 0;
       for (int i = threadIdx.x; i < KT * HD / 2; i += 256) {
         uint32_t* x = reinterpret_cast<uint32_t*>(vs) + i;
         const uint32_t nf = nonfinite2(*x);
+        found |= nf;
         if (nf != 0) *x &= (nf & 0x8000u ? 0u : 0xffffu) | (nf & 0x80000000u ? 0u : 0xffff0000u);
       }
-      __syncthreads();
+      if (__syncthreads_or(found != 0)) bad |= 1ull << (t & 63);
     }
     if (!wave_on) return;
     const bool is_own = t >= np;
@@ -405,19 +408,23 @@ again:
   if (pass == 1) {
     // the infinite and NaN values that pass 1 took as 0, for the rows that see them
 #pragma unroll 1
-    for (int t = 0; t < kp.n + ko.n; ++t) {
-      const bool is_own = t >= kp.n;
-      if (!wave_on || (is_own && t - kp.n >= lim)) continue;
-      const uint16_t* vr = (is_own ? Vo + (size_t)(t - kp.n) * HD : Vp + (size_t)t * HD) + 4 * hl;
+    for (int t = 0; t < nt; ++t) {
+      if ((bad >> (t & 63) & 1) == 0 || !wave_on) continue;
+      const bool is_own = t >= np;
+      const int k0 = (is_own ? t - np : t) * KT;
+#pragma unroll 1
+      for (int k = k0; k < min(k0 + KT, is_own ? lim : kp.n); ++k) {
+        const uint16_t* vr = (is_own ? Vo : Vp) + (size_t)k * HD + 4 * hl;
 #pragma unroll
-      for (int db = 0; db < DB; ++db)
+        for (int db = 0; db < DB; ++db)
 #pragma unroll
-        for (int q4 = 0; q4 < 4; ++q4) {
-          const uint2 y = *reinterpret_cast<const uint2*>(vr + 32 * db + 8 * q4);
-          const float v[4] = {bf_lo(y.x), bf_hi(y.x), bf_lo(y.y), bf_hi(y.y)};
+          for (int q4 = 0; q4 < 4; ++q4) {
+            const uint2 y = *reinterpret_cast<const uint2*>(vr + 32 * db + 8 * q4);
+            const float v[4] = {bf_lo(y.x), bf_hi(y.x), bf_lo(y.y), bf_hi(y.y)};
 #pragma unroll
-          for (int e = 0; e < 4; ++e) o[db][4 * q4 + e] += fabsf(v[e]) < INFINITY ? 0.0f : v[e];
-        }
+            for (int e = 0; e < 4; ++e) o[db][4 * q4 + e] += fabsf(v[e]) < INFINITY ? 0.0f : v[e];
+          }
+      }
     }
   }
   if (!wanted) return;
