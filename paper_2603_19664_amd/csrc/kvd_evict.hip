@@ -56,6 +56,19 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* buf, uint32
 
 constexpr int kEvictBins = 2 * kNtEvict;
 
+// f(i) for the slots i < N of a thread (rows t, t + 1024, ..) that `rows` rows reach into; the code
+// of the others is jumped over (fetching it costs more than running it), and i is a constant, so
+// that arrays indexed by it stay in registers.
+template <int I, int N, typename F>
+__device__ __forceinline__ void slots_with_rows(int rows, const F& f) {
+  if constexpr (I < N) {
+    if (I * kNtEvict < rows) {
+      f(I);
+      slots_with_rows<I + 1, N>(rows, f);
+    }
+  }
+}
+
 // The rank of the last row kept: each pass spreads the ranks that can still be it, [lo,
 // hi], over 2048 equal bins (a first pass over the ranks that occur, so that weights of
 // like size do not share a bin, whose counter they would take turns at; protected and
@@ -63,9 +76,9 @@ constexpr int kEvictBins = 2 * kNtEvict;
 // a bin of up to 64 rows (the first one as a rule) is settled by one wave that compares
 // them.  Then rows are taken thread by thread in slot order: c consecutive slots each, c
 // odd (LDS banks), one prefix sum for freed slots and movers, and before it one for the rows
-// that tie with the last rank unless all of those stay.  Latency-bound: a thread keeps the ranks of its PER rows (t, t +
-// 1024, ..) in registers, all its loads in flight at once, and LDS turns them into slot
-// order.  PER = 0: any length, ranks in the workspace.  16 caches of 8192 .. 16385 rows to
+// that tie with the last rank unless all of those stay.  Latency-bound: a thread keeps the
+// ranks of its rows (t, t + 1024, .., at most PER) in registers, all its loads in flight at once,
+// and LDS turns them into slot order.  PER = 0: any length, ranks in the workspace.  16 caches of 8192 .. 16385 rows to
 // 2048: 88 us with 8-bit digits of the whole rank and serial bin walks, 28 us with ranks
 // read from LDS in every pass and four loads in flight, 26 us with three passes always,
 // 21 us so.
@@ -85,13 +98,14 @@ __global__ __launch_bounds__(kNtEvict) void evict_select_kernel(EvictArgs a) {
   constexpr int N = PER > 0 ? PER : 1;
   float x[N];
   int p[N];
+  auto each = [&](auto f) {
+    int rows = a.T;
+    asm volatile("" : "+s"(rows));  // compared again in each loop: the results of all slots took 148 scalar registers
+    slots_with_rows<0, N>(rows, f);
+  };
   if constexpr (PER > 0) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = wt[min(tid + i * kNtEvict, a.T - 1)];
-    if (ps != nullptr) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) p[i] = ps[min(tid + i * kNtEvict, a.T - 1)];
-    }
+    each([&](int i) { x[i] = wt[(uint32_t)min(tid + i * kNtEvict, a.T - 1)]; });
+    if (ps != nullptr) each([&](int i) { p[i] = ps[(uint32_t)min(tid + i * kNtEvict, a.T - 1)]; });
   }
   const int n = a.len != nullptr ? min(max(a.len[b], 0), a.T) : a.T;
   const int newest = a.last_pos != nullptr ? a.last_pos[b] : 0;
@@ -118,13 +132,12 @@ __global__ __launch_bounds__(kNtEvict) void evict_select_kernel(EvictArgs a) {
     }
   };
   if constexpr (PER > 0) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
+    each([&](int i) {
       const int t = tid + i * kNtEvict;
       k[i] = t < n ? rank_of(a, x[i], ps != nullptr ? p[i] : 0, newest) : 0u;  // past the rows: as NaN, never counted
       lkeys[t] = k[i];
       take(k[i]);
-    }
+    });
   } else {
     for (int t = tid; t < n; t += kNtEvict) {
       const uint32_t r = rank_of(a, wt[t], ps != nullptr ? ps[t] : 0, newest);
@@ -167,9 +180,9 @@ __global__ __launch_bounds__(kNtEvict) void evict_select_kernel(EvictArgs a) {
       s_fill = 0u;
     }
     if constexpr (PER > 0) {
-#pragma unroll
-      for (int i = 0; i < N; ++i)
+      each([&](int i) {
         if (k[i] >= lo && k[i] <= hi) atomicAdd(&hist[(k[i] - lo) >> shift], 1u);
+      });
     } else {
       for (int t = tid; t < n; t += kNtEvict) {
         const uint32_t r = keys[t];
@@ -207,8 +220,7 @@ __global__ __launch_bounds__(kNtEvict) void evict_select_kernel(EvictArgs a) {
           if (r >= lo && r <= hi) list[atomicAdd(&s_fill, 1u)] = r;
         };
         if constexpr (PER > 0) {
-#pragma unroll
-          for (int i = 0; i < N; ++i) gather(k[i]);
+          each([&](int i) { gather(k[i]); });
         } else {
           for (int t = tid; t < n; t += kNtEvict) gather(keys[t]);
         }
@@ -270,11 +282,10 @@ __global__ __launch_bounds__(kNtEvict) void evict_select_kernel(EvictArgs a) {
   // weights of the freed slots from `left` on: ranks below the last one here, ties that do
   // not stay above, a mover's when it has moved
   if constexpr (PER > 0) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
+    each([&](int i) {
       const int t = tid + i * kNtEvict;
       if (t >= left && t < n && k[i] < last) wt[t] = 0.0f;
-    }
+    });
   } else {
     for (int t = left + tid; t < n; t += kNtEvict)
       if (keys[t] < last) wt[t] = 0.0f;
@@ -393,10 +404,14 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t st) {
     return hipGetLastError();
   }
   const auto select = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(bjs), dim3(kNtEvict), 0, st, a); };
-  if (a.T <= 4 * kNtEvict)
-    select(evict_select_kernel<4>);
-  else if (a.T <= 17 * kNtEvict)
-    select(evict_select_kernel<17>);
+  // Rows per thread in registers: 8, 16 or 32, all without spills (32: 101 VGPRs, 140 KB of LDS for the
+  // ranks), each for twice the length of the one before, because a slot that holds no row costs 0.1 us (8192
+  // rows: 13.5 us with 8, 14.2 with 16, 15.7 with 32; both launches of a call, 16 caches).  Beyond, ranks in
+  // the workspace (32768 rows: 33 us with 32, 59 so; 60000: 101).
+  if (a.T <= 8 * kNtEvict)
+    select(evict_select_kernel<8>);
+  else if (a.T <= 16 * kNtEvict)
+    select(evict_select_kernel<16>);
   else if (a.T <= 32 * kNtEvict)
     select(evict_select_kernel<32>);
   else
