@@ -198,11 +198,12 @@ class WeightedCache:
                 self.ws = self.torch.empty(need, dtype=self.torch.uint8, device=self.k.device)
             self._ws_tokens.add(N)
         self.pos[:, :, self.n:self.n + N] = self.torch.arange(self.T, self.T + N, device=self.k.device)
+        kvd.kvd_prefix_attn(self.shape, q, self.prefix_k, self.prefix_v, self.T_prefix, self.k, self.v, self.n + N,
+                            out, self.ws, weight=self.weight, decay=self.decay)
+        # the tokens are in once the call is: a refused one leaves the cache as it was
         self.last_pos.fill_(self.T + N - 1)
         self.n += N
         self.T += N
-        kvd.kvd_prefix_attn(self.shape, q, self.prefix_k, self.prefix_v, self.T_prefix, self.k, self.v, self.n, out,
-                            self.ws, weight=self.weight, decay=self.decay)
 
     def evict(self):
         """Back to the budget, if there is more."""
@@ -228,7 +229,11 @@ class WeightedCache:
         """Take in the tokens of h [batch, T, d], at most `room` at a time, each chunk attended (causally) to what
         the cache holds and evicted down to the budget; out [batch, T, n_q, hd].  Returns q."""
         s, torch, kvd = self.shape, self.torch, self.kvd
-        B, T = h.shape[0], h.shape[1]
+        B, T = self.B, h.shape[1]
+        if tuple(h.shape) != (B, T, s.d_model):
+            raise ValueError(f"h has shape {tuple(h.shape)}, expected {(B, T, s.d_model)}")
+        if tuple(out.shape) != (B, T, s.n_q_heads, s.head_dim):
+            raise ValueError(f"out has shape {tuple(out.shape)}, expected {(B, T, s.n_q_heads, s.head_dim)}")
         q = torch.empty((B, T, s.n_q_heads, s.head_dim), dtype=s.torch_dtype, device=self.k.device)
         for t in range(0, T, self.room):
             self.evict()
