@@ -39,6 +39,7 @@ batch may share a prefix, whose keys and values are stored once and never evicte
 """
 from __future__ import annotations
 
+import contextlib
 import dataclasses
 
 from . import accounting
@@ -185,6 +186,13 @@ class WeightedCache:
         self.ws = torch.empty(max(sizes, default=256), dtype=torch.uint8, device=dev)
         self._ws_tokens = {1, room}
 
+    def _here(self):
+        """A context in which the cache's device is the current one: the projections launch there."""
+        dev = self.k.device
+        if dev.type != "cuda" or self.torch.cuda.current_device() == dev.index:
+            return contextlib.nullcontext()
+        return self.torch.cuda.device(dev)
+
     def _positions(self, N):
         """Positions of the N tokens being added, [B, N] int32."""
         t = self.torch.arange(self.T, self.T + N, dtype=self.torch.int32, device=self.k.device)
@@ -215,14 +223,15 @@ class WeightedCache:
     def step(self, h_new, gamma, w_q, w_k, w_v, out):
         """Decode one token per sequence: h_new [batch, d] is its residual h^(l); out [batch, n_q, hd].  Returns q."""
         s = self.shape
-        if self.n + 1 > self.budget + self.room:
-            self.evict()
-        q = self.torch.empty((self.B, s.n_q_heads, s.head_dim), dtype=s.torch_dtype, device=self.k.device)
-        self.kvd.kvd_project_qkv(s, h_new, gamma, w_q, w_k, w_v, self._positions(1).view(self.B), q, self.k, self.v,
-                                 self.n)
-        self._attend(q, 1, out)
-        if self.n == self.budget + self.room:
-            self.evict()
+        with self._here():
+            if self.n + 1 > self.budget + self.room:
+                self.evict()
+            q = self.torch.empty((self.B, s.n_q_heads, s.head_dim), dtype=s.torch_dtype, device=self.k.device)
+            self.kvd.kvd_project_qkv(s, h_new, gamma, w_q, w_k, w_v, self._positions(1).view(self.B), q, self.k, self.v,
+                                     self.n)
+            self._attend(q, 1, out)
+            if self.n == self.budget + self.room:
+                self.evict()
         return q
 
     def prompt(self, h, gamma, w_q, w_k, w_v, out):
@@ -235,16 +244,17 @@ class WeightedCache:
         if tuple(out.shape) != (B, T, s.n_q_heads, s.head_dim):
             raise ValueError(f"out has shape {tuple(out.shape)}, expected {(B, T, s.n_q_heads, s.head_dim)}")
         q = torch.empty((B, T, s.n_q_heads, s.head_dim), dtype=s.torch_dtype, device=self.k.device)
-        for t in range(0, T, self.room):
+        with self._here():
+            for t in range(0, T, self.room):
+                self.evict()
+                N = min(self.room, T - t)
+                x, pos = h[:, t:t + N].contiguous(), self._positions(N)
+                qc = torch.empty((B, N, s.n_q_heads, s.head_dim), dtype=s.torch_dtype, device=self.k.device)
+                kvd.kvd_project_q(s, x.view(B * N, s.d_model), gamma, w_q, pos.view(B * N),
+                                  qc.view(B * N, s.n_q_heads, s.head_dim))
+                kvd.kvd_recompute_kv(s, x, gamma, w_k, w_v, pos[:, 0].contiguous(), N, self.k, self.v, self.n)
+                oc = torch.empty_like(qc)
+                self._attend(qc, N, oc)
+                q[:, t:t + N], out[:, t:t + N] = qc, oc
             self.evict()
-            N = min(self.room, T - t)
-            x, pos = h[:, t:t + N].contiguous(), self._positions(N)
-            qc = torch.empty((B, N, s.n_q_heads, s.head_dim), dtype=s.torch_dtype, device=self.k.device)
-            kvd.kvd_project_q(s, x.view(B * N, s.d_model), gamma, w_q, pos.view(B * N),
-                              qc.view(B * N, s.n_q_heads, s.head_dim))
-            kvd.kvd_recompute_kv(s, x, gamma, w_k, w_v, pos[:, 0].contiguous(), N, self.k, self.v, self.n)
-            oc = torch.empty_like(qc)
-            self._attend(qc, N, oc)
-            q[:, t:t + N], out[:, t:t + N] = qc, oc
-        self.evict()
         return q

@@ -92,3 +92,35 @@ def test_prompts_of_other_sizes_are_refused_before_any_call(h, out):
     with pytest.raises(ValueError, match="has shape"):
         c.prompt(x(*h), None, None, None, None, x(*out))
     assert held(c) == (0, 0, [0, 0]) and c.kvd.names == []
+
+
+def test_calls_are_made_on_the_cache_s_device():
+    # the current device is 0, the cache's 1: every call is made while its own is current
+    c = cache()
+    current = []
+
+    @contextlib.contextmanager
+    def device(dev):
+        current.append(dev.index)
+        yield
+        current.pop()
+
+    there = torch.device("cuda", 1)
+    cuda = types.SimpleNamespace(current_device=lambda: 0, device=device)
+    here = WeightedCache._here
+    c._here = lambda: here(types.SimpleNamespace(k=types.SimpleNamespace(device=there),
+                                                 torch=types.SimpleNamespace(cuda=cuda)))
+    calls = []
+    make = c.kvd.__getattr__
+    c.kvd = types.SimpleNamespace(**{n: (lambda n: lambda *a, **kw: (calls.append((n, list(current))), make(n)(*a, **kw)))(n)
+                                     for n in ("kvd_project_qkv", "kvd_project_q", "kvd_recompute_kv", "kvd_prefix_attn",
+                                               "kvd_evict")},
+                                  kvd_prefix_workspace_bytes=kvd.kvd_prefix_workspace_bytes)
+    c.prompt(x(2, 7, 512), None, None, None, None, x(2, 7, 8, 64))
+    for _ in range(4):
+        step(c)
+    assert {n for n, _ in calls} == {"kvd_project_qkv", "kvd_project_q", "kvd_recompute_kv", "kvd_prefix_attn", "kvd_evict"}
+    assert all(at == [1] for _, at in calls) and current == []
+    cuda.current_device = lambda: 1
+    with c._here():
+        assert current == []
