@@ -388,8 +388,10 @@ size_t kvd_block_workspace_bytes(const kvd_attn_shape* shape, int32_t d_ff, int3
 
 /* Attention of N >= 1 new tokens per sequence over a prefix that the whole batch
  * shares, then over each sequence's own rows (Eqs. attn_weights, head_output over
- * CONCAT(prefix, own)).  The prefix's keys and values are read once for all
- * sequences.  For sequence b, len = own_len[b], n = n_new[b] and token i < n,
+ * CONCAT(prefix, own)).  The prefix is stored once for all sequences; a workgroup reads a
+ * range of it for a block of rows, of many sequences where those are few each (128 rows to a
+ * block in bf16, 16 in fp32), of one sequence where its own rows fill such blocks or the
+ * whole call is small.  For sequence b, len = own_len[b], n = n_new[b] and token i < n,
  *   out[b][i][h] = softmax(q . K / sqrt(head_dim)) V
  * over prefix rows 0 .. T_prefix-1 and own rows t <= len - n + i: the new tokens
  * are the last n of the sequence's own rows, and each sees the rows up to itself.
@@ -397,7 +399,7 @@ size_t kvd_block_workspace_bytes(const kvd_attn_shape* shape, int32_t d_ff, int3
  * their out rows are left as they were.  Own rows from len on are never read, and
  * what a token does not see has no part in its result, whatever it holds.
  * An infinite value that it sees makes its column infinite (NaN with both signs), however
- * small the row's weight.
+ * small the row's weight (of a finite score).
  *   q, out   [B][N][n_q_heads][head_dim].
  *   prefix   K/V [n_kv_heads][t_cap][head_dim], rows t_off .. t_off+T_prefix-1;
  *            may be NULL iff T_prefix == 0.

@@ -882,7 +882,10 @@ namespace {
 // 128-row tiles; fp32 to waves of 16 rows.  A sequence whose own rows fill their blocks to
 // 9 / 10, or two and more of them, takes prefix and own keys in one pass (joint): neither half
 // leaves a partial state of its own.  Others leave the prefix to blocks of all sequences' rows,
-// none of them empty (8 x 144 rows, prefix 3000: 28 us joint, 23 so; 6 x 120: 33.5 and 35).
+// none of them empty.  In us, joint and apart, 12 heads of 128: 8 x 144 rows, prefix 3000, own 24:
+// 28.9, 25.2; 8 x 252, 8192, 42: 47.0, 50.0; 6 x 120, 3000, 300: 24.4, 22.9; 12 x 120, 8192, 20:
+// 41.4, 44.6; 8 x 384, 8192, 500: 70.7, 70.9; 16 x 258, 8192, 500: 99, 82; 8 heads of 256, 8 x 256,
+// 8192, 500: 122, 134.  (Two blocks and a little more are better apart; the rule takes them joint.)
 // Calls of few rows and at most kRowsSmall keys are joint too, and a range of that many keys is
 // one slot: one launch (8 tokens over 240 keys 8.7 us, 10.7 in two).
 struct RowsPlan {
@@ -897,10 +900,10 @@ struct RowsPlan {
 // flight at once (1000 keys 11.9 -> 11.1 us; 5000 keys in 64 slots 16.0 us, in 40 13.7).
 // Enough for `wgs` workgroups, but fewer than sqrt(keys kRowsStateRows / rows): a slot
 // leaves every row a state that is written and read, as dear as 1 / kRowsStateRows of a key in
-// a workgroup's range of keys / S.  (64 tokens, 8 heads of 256 over a prefix of 16384: 85
-// us with 64 slots, 74 with 43; 12 heads of 128: 41 and 34; prompts of 400 tokens over 1500
-// keys: 52 us with 6, 49 with 3.)  Beside own rows, whose reads fill the idle workgroups'
-// time, the states count half as much again.
+// a workgroup's range of keys / S.  (64 tokens, 8 heads of 256 over a prefix of 16384 and 1024
+// own rows: 81 us with 64 slots, 74 with 43; 12 heads of 128 and 64 own rows: 32 and 30 with 32;
+// 2 prompts of 400 tokens over 1500 keys: 47 us with 6, 46 with 3, 58 with 1.)  Beside own rows, whose
+// reads fill the idle workgroups' time, the states count half as much again.
 // Beyond `wgs`, the count S that balances what the last workgroups of a launch leave
 // idle, about half a slot (keys / S / 2), against a slot's fixed cost of kRowsSlotKeys keys
 // (first loads, state written and merged) for every workgroup's units S / kRowsTargetWgs of
@@ -1004,8 +1007,8 @@ bool rows_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T_prefix, 
       p->sc = take(4 * (size_t)units * R * p->sc_ld);
       merge += units * ((T_own + 255) / 256);
     } else {
-      // tiles of keys, the rows that see one in parts of P_w (at least 256), so that all parts
-      // together are just one round of workgroups.  Of N new tokens among T keys, 1 - N / 2 T
+      // tiles of keys, the rows that see one in parts of P_w (192 and more where there are several), so
+      // that all parts together are just one round of workgroups.  Of N new tokens among T keys, 1 - N / 2 T
       // of the rows see a key on average, and a tile's last part is half full.
       const long long keys_w = bf ? 128 : 16, tiles = units * ((T_own + keys_w - 1) / keys_w);
       const long long most = std::min(64ll, (R + 255) / 256), want = kvd::kRowsTargetWgs;

@@ -78,10 +78,10 @@ __device__ __forceinline__ void slots_with_rows(int rows, const F& f) {
 // odd (LDS banks), one prefix sum for freed slots and movers, and before it one for the rows
 // that tie with the last rank unless all of those stay.  Latency-bound: a thread keeps the
 // ranks of its rows (t, t + 1024, .., at most PER) in registers, all its loads in flight at once,
-// and LDS turns them into slot order.  PER = 0: any length, ranks in the workspace.  16 caches of 8192 .. 16385 rows to
-// 2048: 88 us with 8-bit digits of the whole rank and serial bin walks, 28 us with ranks
-// read from LDS in every pass and four loads in flight, 26 us with three passes always,
-// 21 us so.
+// and LDS turns them into slot order.  PER = 0: any length, ranks in the workspace.  16 caches of
+// 8192 .. 16385 rows to 2048: 88 us with 8-bit digits of the whole rank and serial bin walks, 28
+// us with ranks read from LDS in every pass and four loads in flight, 26 us with three passes
+// always, 22 us so.
 template <int PER>
 __global__ __launch_bounds__(kNtEvict) void evict_select_kernel(EvictArgs a) {
   __shared__ uint32_t lkeys[PER > 0 ? PER * kNtEvict : 1];
@@ -404,10 +404,10 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t st) {
     return hipGetLastError();
   }
   const auto select = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(bjs), dim3(kNtEvict), 0, st, a); };
-  // Rows per thread in registers: 8, 16 or 32, all without spills (32: 101 VGPRs, 140 KB of LDS for the
-  // ranks), each for twice the length of the one before, because a slot that holds no row costs 0.1 us (8192
-  // rows: 13.5 us with 8, 14.2 with 16, 15.7 with 32; both launches of a call, 16 caches).  Beyond, ranks in
-  // the workspace (32768 rows: 33 us with 32, 59 so; 60000: 101).
+  // Rows per thread in registers: 8, 16 or 32, all without spills (32: 101 VGPRs, 140 KB of LDS
+  // for the ranks), each for twice the length of the one before, because a slot that holds no row
+  // costs 0.1 us (8192 rows: 13.5 us with 8, 14.2 with 16, 15.7 with 32; both launches of a call,
+  // 16 caches).  Beyond, ranks in the workspace (32768 rows: 33 us with 32, 59 so; 60000: 101).
   if (a.T <= 8 * kNtEvict)
     select(evict_select_kernel<8>);
   else if (a.T <= 16 * kNtEvict)

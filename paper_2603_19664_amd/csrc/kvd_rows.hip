@@ -65,7 +65,7 @@ __device__ __forceinline__ size_t q_off(const RowsArgs& a, int j, int fr, int hd
 
 // Whether the rb rows from row r_blk on of a sequence see no key beyond the call's first slot
 // (the first rows of a causal prompt): that slot's workgroup writes out itself, the others
-// nothing, and no state is merged (a 3001-token prompt 110 us instead of 114).
+// nothing, and no state is merged (a 3001-token prompt 120.3 us instead of 122.7).
 __device__ __forceinline__ bool any_sole_slot(const RowsArgs& a) {  // of a call of several slots
   return a.S_prefix == 0 && !a.own_few && a.sc == nullptr && (a.joint ? a.T_prefix : 0) < a.C_own &&
          (a.own_len != nullptr || a.T_own - a.N < a.C_own);
@@ -188,9 +188,9 @@ __device__ __forceinline__ float add_state(float x, float w, float y) {
 // lane ^ 32.  The maximum moves only by steps of more than 2^8, so that O is rescaled
 // in few tiles.  O^T += V^T P^T with P^T straight from the score registers, as the sum of
 // two bf16 parts (2^-17 of a weight is lost).  Rounded to one part, each weight was off by up to
-// 2^-8: the output's error grew from 1.6e-3 to 2.3e-3, and a token's precision hung on how many
-// shared its batch (8 prompts over 8192 keys 128 us so, 155 with both parts; a 3001-token
-// prompt 110 and 122).
+// 2^-8: the output's error grew from 1.7e-3 to 2.3e-3, and a token's precision hung on how many
+// shared its batch (8 prompts over 8192 keys 128 us so, 154 with both parts; a 3001-token
+// prompt 110 and 120).
 template <int HD>
 __device__ __forceinline__ void rows_tile(const RowsArgs& a, int item, uint16_t* buf0, uint16_t* buf1) {
   constexpr int KT = rows_kt(HD), KH = KT / 32, KS = HD / 16, DB = HD / 32, kLead = 4;
@@ -813,7 +813,7 @@ again:
 // ones runs beside the memory traffic of the others.  The two buffers are two objects,
 // every access naming one: a copy in flight into one is then known not to touch the other
 // (of one array, every LDS read waited for all copies: 8 prompts over 8192 keys 160 us
-// instead of 147).
+// instead of 147, both with weights of one part).
 template <int HD>
 __global__ __launch_bounds__(256, 2) void rows_bf16_kernel(RowsArgs a, int tile_items) {
   constexpr int KT = rows_kt(HD);
@@ -1285,7 +1285,7 @@ __device__ __forceinline__ void copy_chunk(const uint16_t* src, uint32_t off, ui
 template <int HD>
 __global__ __launch_bounds__(256, 2) void weight_tile_kernel(RowsArgs a) {
   constexpr int KS = HD / 16, CPR = HD / 8, CH = kWtRows * CPR / 256, kLead = 4;
-  __shared__ __align__(1024) uint16_t q_a[kWtRows * HD], q_b[kWtRows * HD];  // two objects: see rows_tile_kernel
+  __shared__ __align__(1024) uint16_t q_a[kWtRows * HD], q_b[kWtRows * HD];  // two objects: see rows_bf16_kernel
   const int tid = threadIdx.x, lane = tid & 63, w = wave_id(), hl = lane >> 5;
   const int units = a.B * a.n_kv, x = (int)blockIdx.x / units, u = (int)blockIdx.x - x * units;
   const int j = u % a.n_kv, b = u / a.n_kv;

@@ -5,14 +5,15 @@ namespace kvd {
 
 // Several query rows over stored keys (kvd_rows.hip).
 constexpr int kRowsTile = 128;    // rows per workgroup of the tile kernel
-constexpr int kRowsWave = 16;     // rows per wave of the fp32 kernel
+constexpr int kRowsWave = 16;     // rows per workgroup of the fp32 kernel, all of them in each of its waves
 constexpr int kRowsFew = 16;      // rows rows_few takes (one MFMA column block)
 constexpr int kRowsTargetWgs = 512;
-constexpr int kRowsLeastKeys = 128;  // keys per slot, at least (64: within 2 %, 256: 4 - 9 % slower)
+constexpr int kRowsLeastKeys = 128;  // keys per slot, at least (64: 1 % faster to 3 % slower, 256: 9 % faster to 7 % slower)
 constexpr int kRowsSlotKeys = 512;   // a slot's fixed cost in keys
-constexpr int kRowsStateRows = 96;   // rows whose states cost what a key costs a workgroup
+// rows whose states cost what a key costs a workgroup (48: up to 6 % slower, 192: up to 14 %)
+constexpr int kRowsStateRows = 96;
 constexpr int kRowsMostSlots = 64;
-constexpr int kRowsSmall = 256;  // keys that one workgroup takes at once (512: up to 8 us slower)
+constexpr int kRowsSmall = 256;  // keys that one workgroup takes at once (512: up to 3 us slower)
 // Waves that share a row's S states when they are merged: a wave keeps 8 in flight, so that
 // many states are many round trips (512 rows of 66 states: 12.0 us with one wave per row, 9.2
 // with four).
