@@ -473,6 +473,83 @@ kvd_status kvd_evict(const kvd_attn_shape* shape, const kvd_kv_view* kv, int32_t
 /* Workspace bytes of kvd_evict (0 on invalid arguments).                         */
 size_t kvd_evict_workspace_bytes(const kvd_attn_shape* shape, int32_t B, int32_t T);
 
+/* Attention of N >= 1 new tokens per sequence over its first `sink` tokens and a sliding
+ * window (Eqs. attn_weights, head_output under the local mask of Sec. 3.2, whose first tokens
+ * stay visible).  Of sequence b, len = kv_len[b] tokens so far, the last n = n_new[b] are the
+ * new ones; new token i < n is token p = len - n + i, and with K and V as stored
+ *   out[b][i][h] = softmax(q . K / sqrt(head_dim)) V   over the tokens
+ *                  t <= p with t < sink or t > p - window.
+ * A token that sees no key (p < 0) gives out = 0.  Tokens i >= n[b] are not computed and
+ * their out rows are left as they were.  What a token does not see has no part in its result,
+ * whatever it holds; rows that hold no token that is seen are never read.  An infinite value that it
+ * sees makes its column infinite (NaN with both signs), however small the row's weight (of a finite
+ * score).
+ * Rows.  The view's slots = t_cap - t_off rows from t_off on hold a sequence's tokens.  With
+ * T <= slots token t is in row t_off + t.  With T > slots, which needs slots - sink >=
+ * window + N - 1, it is there below sink, and behind that in a ring, in row
+ *   t_off + sink + (t - sink) mod (slots - sink)
+ * (kvd_mx_store writes such rows): an endless stream in sink + window rows.
+ *   q, out   [B][N][n_q_heads][head_dim].
+ *   kv       K/V [B][n_kv_heads][t_cap][head_dim], 0 <= t_off < t_cap.
+ *   kv_len, n_new   [B] int32 or NULL (T and N for every sequence); values are taken as
+ *            clamped to 0 .. T and 0 .. N.   T >= 1, window >= 1, sink >= 0.
+ *   ws       kvd_sink_workspace_bytes(shape, B, N, T, window, sink) bytes, 256-byte
+ *            aligned, overwritten; it need not be cleared, and calls ordered on one stream may
+ *            share it (not with calls that find their counters cleared in theirs,
+ *            kvd_workspace_bytes).
+ * Results repeat bit for bit (no atomics).  Softmax weights enter the value product as in
+ * kvd_prefix_attn; the shape's d_model, rms_eps, rope_theta and w_layout are not used.
+ * B == 0 or N == 0 is a no-op.                                                  */
+kvd_status kvd_sink_attn(const kvd_attn_shape* shape, const void* q, int32_t N, const kvd_kv_view* kv,
+                         const int32_t* kv_len, const int32_t* n_new, int32_t B, int32_t T, int32_t window,
+                         int32_t sink, void* out, void* ws, size_t ws_bytes, void* stream);
+
+/* Workspace bytes of kvd_sink_attn and kvd_mx_attn (0 on invalid arguments).  They do not
+ * fall as T grows, so that a decode loop can size one workspace for its longest call.  */
+size_t kvd_sink_workspace_bytes(const kvd_attn_shape* shape, int32_t B, int32_t N, int32_t T, int32_t window,
+                                int32_t sink);
+
+/* A cache of K/V rows in 4 bits (4.25 with scales).  Groups of 32 neighbouring elements of
+ * a row share a power of two 2^E; an element is a sign and one of 0, 1/2, 1, 3/2, 2, 3, 4, 6, times
+ * 2^E (codes 0 .. 7; 8 .. 15 with the sign), two to a byte, the even element in the low half.
+ *   k, v              [B][n_kv_heads][t_cap][head_dim / 2] bytes
+ *   k_scale, v_scale  [B][n_kv_heads][t_cap][head_dim / 32] bytes, E + 127; 255: the group
+ *                     is NaN.
+ * kvd_mx_store chooses the smallest E in -100 .. 125 with |x| <= 7 2^E for all 32, and rounds
+ * x / 2^E to the nearest number (ties to the even code, above 6 to 6); a group that holds an infinity
+ * or NaN is NaN.  Every value is exact in bf16.  Others may fill a cache too, with scale bytes of
+ * 27 .. 252 and 255.                                                           */
+typedef struct {
+  void* k;
+  void* v;
+  void* k_scale;
+  void* v_scale;
+  int32_t t_cap;
+  int32_t t_off;
+} kvd_mx_view;
+
+/* The new tokens' rows into a 4-bit cache: token t = len - n + i, i < n, of sequence b from rows
+ * t_off + i of `rows` (K/V [B][n_kv_heads][t_cap][head_dim] in the shape dtype) into its row of
+ * the cache, by kvd_sink_attn's rule (with T > slots it needs slots - sink >= N); tokens
+ * with t < 0 are not there.  Other rows are left as they were.  kv_len counts the new tokens; it and
+ * n_new as in kvd_sink_attn.   T >= 1, sink >= 0.   B == 0 or N == 0 is a no-op.   */
+kvd_status kvd_mx_store(const kvd_attn_shape* shape, const kvd_kv_view* rows, int32_t N, const kvd_mx_view* cache,
+                        const int32_t* kv_len, const int32_t* n_new, int32_t B, int32_t T, int32_t sink,
+                        void* stream);
+
+/* kvd_mx_store's inverse: the last n tokens' rows read back into rows t_off + i of `rows`,
+ * exactly, in the shape dtype (a ring still holds them: slots - sink >= N).      */
+kvd_status kvd_mx_load(const kvd_attn_shape* shape, const kvd_mx_view* cache, int32_t N, const int32_t* kv_len,
+                       const int32_t* n_new, int32_t B, int32_t T, int32_t sink, const kvd_kv_view* rows,
+                       void* stream);
+
+/* kvd_sink_attn over a 4-bit cache: the same call, K and V the values that the cache's
+ * numbers stand for, exactly (no rounding but the output's; fp32 queries and softmax weights
+ * enter the products as three bf16 parts, which hold them whole).  window >= T: the whole cache.  */
+kvd_status kvd_mx_attn(const kvd_attn_shape* shape, const void* q, int32_t N, const kvd_mx_view* cache,
+                       const int32_t* kv_len, const int32_t* n_new, int32_t B, int32_t T, int32_t window,
+                       int32_t sink, void* out, void* ws, size_t ws_bytes, void* stream);
+
 /* Merge step of split-K attention: out[b][h] = sum_s w_s acc_s / sum_s w_s l_s
  * with w_s = 2^(m_s - max_s m_s), over the S partial softmax states that a
  * preceding kvd_decode_attn / kvd_cached_attn / kvd_fused_recompute_attn call

@@ -53,6 +53,7 @@ __all__ = [
     "block_forward",
     "recompute_residual",
     "rows_attention", "evict",
+    "sink_attention", "sink_rows", "mx_round", "mx_values",
 ]
 
 
@@ -354,3 +355,69 @@ def evict(k, v, weight, pos, lens, last_pos, keep, sink, recent):
             weight[b, j, left:n] = 0.0
         lens[b] = left
     return k, v, weight, pos, lens
+
+
+def sink_attention(q, k, v, lens, n_new, window, sink):
+    """Attention of new tokens over the first `sink` tokens and the newest `window` of each (Sec. 3.2's local mask
+    whose first tokens stay visible).
+
+    q [B, N, n_q, hd]; k, v [B, n_kv, T, hd], row t token t; lens, n_new [B].  Token i < n_new[b] is token p = lens[b]
+    - n_new[b] + i and sees t <= p with t < sink or t > p - window.  Returns (out, size) as rows_attention does.
+    """
+    q = np.asarray(q, dtype=np.float64)
+    B, N, n_q, hd = q.shape
+    g = n_q // k.shape[1]
+    out, size = np.zeros_like(q), np.zeros_like(q)
+    for b in range(B):
+        for i in range(int(n_new[b])):
+            p = int(lens[b]) - int(n_new[b]) + i
+            if p < 0:
+                continue
+            first = max(p - window + 1, 0)
+            for j in range(k.shape[1]):
+                kk, vv = (np.concatenate([a[b, j, :min(sink, first)], a[b, j, first:p + 1]]).astype(np.float64)
+                          for a in (k, v))
+                s = q[b, i, j * g:j * g + g] @ kk.T / np.sqrt(hd)
+                w = np.exp(s - s.max(-1, keepdims=True))
+                w /= w.sum(-1, keepdims=True)
+                out[b, i, j * g:j * g + g] = w @ vv
+                size[b, i, j * g:j * g + g] = w @ np.abs(vv)
+    return out, size
+
+
+def sink_rows(T, slots, sink):
+    """The row of every token 0 .. T-1 in a cache of `slots` rows: the first `sink`, then a ring (T <= slots: in order)."""
+    t = np.arange(T)
+    return t if T <= slots else np.where(t < sink, t, sink + (t - sink) % max(slots - sink, 1))
+
+
+_MX = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+
+
+def mx_round(x):
+    """Rows x [.., hd] as 4-bit numbers: (codes [.., hd / 2], scales [.., hd / 32]), bytes.
+
+    32 neighbours share 2^E, the smallest E in -100 .. 125 with |x| <= 7 2^E; codes 0 .. 7 are 2^E times _MX, the
+    nearest, ties to the even code; + 8 with the sign; two codes to a byte, the even element low.  A group with an
+    infinity or NaN has scale 255 and codes 0."""
+    x = np.asarray(x, dtype=np.float64)
+    g = x.reshape(*x.shape[:-1], -1, 32)
+    top = np.abs(g).max(-1)
+    bad = ~np.isfinite(top)
+    E = np.full(top.shape, -100)
+    for e in range(-100, 125):
+        E += np.where(bad, 0.0, top) > 7.0 * 2.0 ** e
+    y = np.abs(np.where(bad[..., None], 0.0, g)) / 2.0 ** E[..., None].astype(np.float64)
+    order = np.array([0, 2, 4, 6, 1, 3, 5, 7])    # the first of two equally near ones is even
+    code = order[np.abs(np.minimum(y, 6.0)[..., None] - _MX[order]).argmin(-1)]
+    code = code + 8 * np.signbit(np.where(bad[..., None], 0.0, g))
+    code = code.reshape(x.shape).astype(np.uint8)
+    return code[..., 0::2] | code[..., 1::2] << 4, np.where(bad, 255, E + 127).astype(np.uint8)
+
+
+def mx_values(codes, scales):
+    """What 4-bit rows stand for, in fp64."""
+    c = np.stack([codes & 15, codes >> 4], -1).reshape(*codes.shape[:-1], -1)
+    v = np.where(c >= 8, -1.0, 1.0) * _MX[c & 7]
+    s = np.where(scales == 255, np.nan, 2.0 ** (scales.astype(np.float64) - 127))
+    return (v.reshape(*v.shape[:-1], -1, 32) * s[..., None]).reshape(v.shape)

@@ -36,6 +36,9 @@ WeightedCache bounds the cache by attention weight instead of age: it keeps the 
 that received the most (the paper's comparison systems that score cached tokens by
 accumulated attention, Sec. 4), drops the others for good and recomputes nothing.  The
 batch may share a prefix, whose keys and values are stored once and never evicted.
+
+SinkCache bounds it by age as a sliding-window layer does, but keeps a few first tokens visible: sink + window rows
+serve an endless stream, in the shape's dtype or in 4 bits.
 """
 from __future__ import annotations
 
@@ -257,4 +260,104 @@ class WeightedCache:
                 self._attend(qc, N, oc)
                 q[:, t:t + N], out[:, t:t + N] = qc, oc
             self.evict()
+        return q
+
+
+class SinkCache:
+    """One layer's stored K/V for `batch` sequences decoded in lockstep: the first `sink` tokens and a ring of the
+    newest `window` ones (and `room` - 1 more, so that up to `room` tokens come in one call), in the shape's dtype or,
+    with mx, in 4 bits.  Every new token sees the first `sink` tokens and the newest `window`, itself among them.
+
+    Tokens sit at positions pos0, pos0 + 1, ..; a token's K keeps the rotation of its position.
+    """
+
+    def __init__(self, shape, batch: int, window: int, sink: int = 0, room: int = 1, mx: bool = False, pos0: int = 0,
+                 device="cuda"):
+        import torch
+
+        from . import kvd
+        if window < 1 or room < 1:
+            raise ValueError("window and room must be >= 1")
+        if sink < 0:
+            raise ValueError("sink must be >= 0")
+        self.kvd, self.torch = kvd, torch
+        self.shape, self.B, self.window, self.sink, self.room, self.pos0 = shape, batch, window, sink, room, pos0
+        self.ring = window + room - 1
+        dt, cap = shape.torch_dtype, sink + self.ring
+        rows = (batch, shape.n_kv_heads, room if mx else cap, shape.head_dim)
+        self.mx = kvd.mx_cache(shape, batch, cap, device) if mx else None
+        # in 4 bits: the rows of one call on their way into the cache
+        self.k = torch.zeros(rows, dtype=dt, device=device)
+        self.v = torch.zeros_like(self.k)
+        self.T = 0  # tokens seen
+        sizes = [kvd.kvd_sink_workspace_bytes(shape, batch, n, 2 ** 31 - 1, window, sink)
+                 for n in range(1, room + 1) if batch]
+        self.ws = torch.empty(max(sizes, default=256), dtype=torch.uint8, device=device)
+
+    def _here(self):
+        """A context in which the cache's device is the current one: the projections launch there."""
+        dev = self.k.device
+        if dev.type != "cuda" or self.torch.cuda.current_device() == dev.index:
+            return contextlib.nullcontext()
+        return self.torch.cuda.device(dev)
+
+    def row(self, t: int) -> int:
+        """The cache row of token t."""
+        return t if t < self.sink else self.sink + (t - self.sink) % self.ring
+
+    def _pieces(self, N):
+        """(first of the N tokens being added, how many) of the parts that lie in neighbouring rows."""
+        t, end = self.T, self.T + N
+        while t < end:
+            n = end - t if t < self.sink else min(end - t, self.ring - (t - self.sink) % self.ring)
+            if t < self.sink:
+                n = min(n, self.sink + self.ring - t)
+            yield t, n
+            t += n
+
+    def _attend(self, q, N, out):
+        kvd, s, T = self.kvd, self.shape, self.T + N
+        if self.mx is not None:
+            kvd.kvd_mx_store(s, self.k, self.v, N, self.mx, T, sink=self.sink)
+            kvd.kvd_mx_attn(s, q, self.mx, T, out, self.ws, window=self.window, sink=self.sink)
+        else:
+            kvd.kvd_sink_attn(s, q, self.k, self.v, T, self.window, out, self.ws, sink=self.sink)
+        self.T = T
+
+    def step(self, h_new, gamma, w_q, w_k, w_v, out):
+        """Decode one token per sequence: h_new [batch, d] is its residual h^(l); out [batch, n_q, hd].  Returns q."""
+        s, torch, dev = self.shape, self.torch, self.k.device
+        with self._here():
+            q = torch.empty((self.B, s.n_q_heads, s.head_dim), dtype=s.torch_dtype, device=dev)
+            pos = torch.full((self.B,), self.pos0 + self.T, dtype=torch.int32, device=dev)
+            self.kvd.kvd_project_qkv(s, h_new, gamma, w_q, w_k, w_v, pos, q, self.k, self.v,
+                                     0 if self.mx is not None else self.row(self.T))
+            self._attend(q, 1, out)
+        return q
+
+    def prompt(self, h, gamma, w_q, w_k, w_v, out):
+        """Take in the tokens of h [batch, T, d], at most `room` at a time; out [batch, T, n_q, hd].  Returns q."""
+        s, torch, kvd, dev = self.shape, self.torch, self.kvd, self.k.device
+        B, T = self.B, h.shape[1]
+        if tuple(h.shape) != (B, T, s.d_model):
+            raise ValueError(f"h has shape {tuple(h.shape)}, expected {(B, T, s.d_model)}")
+        if tuple(out.shape) != (B, T, s.n_q_heads, s.head_dim):
+            raise ValueError(f"out has shape {tuple(out.shape)}, expected {(B, T, s.n_q_heads, s.head_dim)}")
+        q = torch.empty((B, T, s.n_q_heads, s.head_dim), dtype=s.torch_dtype, device=dev)
+        with self._here():
+            for t in range(0, T, self.room):
+                N = min(self.room, T - t)
+                x = h[:, t:t + N].contiguous()
+                pos = torch.arange(self.pos0 + self.T, self.pos0 + self.T + N, dtype=torch.int32, device=dev)
+                qc = torch.empty((B, N, s.n_q_heads, s.head_dim), dtype=s.torch_dtype, device=dev)
+                kvd.kvd_project_q(s, x.view(B * N, s.d_model), gamma, w_q, pos.repeat(B),
+                                  qc.view(B * N, s.n_q_heads, s.head_dim))
+                for t0, n in [(self.T, N)] if self.mx is not None else list(self._pieces(N)):
+                    i = t0 - self.T
+                    first = torch.full((B,), self.pos0 + t0, dtype=torch.int32, device=dev)
+                    kvd.kvd_recompute_kv(s, x if n == N else x[:, i:i + n].contiguous(), gamma, w_k, w_v, first, n,
+                                         self.k, self.v, 0 if self.mx is not None else self.row(t0))
+                oc = torch.empty_like(qc)
+                self._attend(qc, N, oc)
+                q[:, t:t + N], out[:, t:t + N] = qc, oc
         return q

@@ -14,7 +14,7 @@ LIB = os.path.join(PKG, "libkvd.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 SOURCES = ["kvd_api.cpp", "kvd_kernels.hip", "kvd_absorb.hip", "kvd_block.hip", "kvd_rows.hip",
-           "kvd_evict.hip"]
+           "kvd_evict.hip", "kvd_sink.hip", "kvd_mx.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++20", "-fPIC", "-shared",
     # no packed-fp32 instructions in generated code

@@ -1204,6 +1204,199 @@ size_t kvd_evict_workspace_bytes(const kvd_attn_shape* shape, int32_t B, int32_t
   return 0;
 }
 
+// ------------------------------------------------------------------ windows with sinks, 4-bit caches
+
+namespace {
+
+// Rows of a cache behind t_off that hold T tokens, of which `need` newest ones (and the
+// first `sink`) are wanted: every token has its row, or the rows behind the sinks are a ring.
+kvd_status ring_of(int32_t t_cap, int32_t t_off, int32_t T, int32_t sink, int64_t need, const char* what, int32_t* cap,
+                   int32_t* ring) {
+  if (t_cap < 1 || t_off < 0 || t_off >= t_cap)
+    return fail(KVD_ERR_SHAPE, "kv rows from t_off=%d on exceed t_cap=%d", t_off, t_cap);
+  *cap = t_cap - t_off;
+  *ring = 0;
+  if (T <= *cap) return KVD_OK;
+  if (*cap - (int64_t)sink < need)
+    return fail(KVD_ERR_SHAPE, "%d rows behind t_off=%d hold neither T=%d tokens nor sink=%d and a ring of %s = %lld",
+                *cap, t_off, T, sink, what, (long long)need);
+  *ring = *cap - sink;
+  return KVD_OK;
+}
+
+kvd_status check_mx_view(const kvd_mx_view* c) {
+  if (c == nullptr) return fail(KVD_ERR_NULL, "cache is NULL");
+  KVD_TRY(check_ptr(c->k, "cache->k"));
+  KVD_TRY(check_ptr(c->v, "cache->v"));
+  KVD_TRY(check_ptr(c->k_scale, "cache->k_scale"));
+  return check_ptr(c->v_scale, "cache->v_scale");
+}
+
+// Launch geometry and workspace of a kvd_sink_attn / kvd_mx_attn call.
+struct SinkPlan {
+  int32_t R, S, C;
+  size_t ml, acc, end;  // byte offsets in the workspace
+};
+
+// False when a size passes the kernels' 32-bit indexes or a launch's number of threads.
+bool sink_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T, int32_t window, int32_t sink, SinkPlan* p) {
+  *p = SinkPlan{};
+  const int32_t g = s->n_q_heads / s->n_kv_heads;
+  const long long R = (long long)N * g, Rt = R * B;
+  if (Rt * s->n_kv_heads > INT32_MAX || Rt >= 1ll << 28) return false;
+  p->R = (int32_t)R;
+  p->S = 1;
+  p->end = 256;
+  return Rt * s->n_kv_heads <= kvd::most_wgs(256);
+}
+
+kvd_status sink_sizes(int32_t B, int32_t N, int32_t T, int32_t window, int32_t sink) {
+  KVD_TRY(check_batch(B));
+  if (N < 0) return fail(KVD_ERR_SHAPE, "N=%d must be >= 0", N);
+  if (T < 1) return fail(KVD_ERR_SHAPE, "T=%d must be >= 1", T);
+  if (window < 1) return fail(KVD_ERR_SHAPE, "window=%d must be >= 1", window);
+  if (sink < 0) return fail(KVD_ERR_SHAPE, "sink=%d must be >= 0", sink);
+  return KVD_OK;
+}
+
+kvd_status sink_call(const kvd_attn_shape* shape, const void* q, int32_t N, const kvd_kv_view* kv,
+                     const kvd_mx_view* mx, const int32_t* kv_len, const int32_t* n_new, int32_t B, int32_t T,
+                     int32_t window, int32_t sink, void* out, void* ws, size_t ws_bytes, void* stream,
+                     const char* name) {
+  KVD_TRY(check_shape(shape));
+  KVD_TRY(sink_sizes(B, N, T, window, sink));
+  if (B == 0 || N == 0) return KVD_OK;
+  KVD_TRY(check_ptr(q, "q"));
+  KVD_TRY(check_ptr(out, "out"));
+  kvd::SinkArgs a{};
+  const int64_t need = (int64_t)window + N - 1;
+  if (mx != nullptr) {
+    KVD_TRY(check_mx_view(mx));
+    KVD_TRY(ring_of(mx->t_cap, mx->t_off, T, sink, need, "window + N - 1", &a.cap, &a.ring));
+    a.k = mx->k;
+    a.v = mx->v;
+    a.ks = static_cast<const uint8_t*>(mx->k_scale);
+    a.vs = static_cast<const uint8_t*>(mx->v_scale);
+    a.t_cap = mx->t_cap;
+    a.t_off = mx->t_off;
+  } else {
+    if (kv == nullptr) return fail(KVD_ERR_NULL, "kv is NULL");
+    KVD_TRY(check_ptr(kv->k, "kv->k"));
+    KVD_TRY(check_ptr(kv->v, "kv->v"));
+    KVD_TRY(ring_of(kv->t_cap, kv->t_off, T, sink, need, "window + N - 1", &a.cap, &a.ring));
+    a.k = kv->k;
+    a.v = kv->v;
+    a.t_cap = kv->t_cap;
+    a.t_off = kv->t_off;
+  }
+  if (kv_len != nullptr) KVD_TRY(check_ptr4(kv_len, "kv_len"));
+  if (n_new != nullptr) KVD_TRY(check_ptr4(n_new, "n_new"));
+  SinkPlan p;
+  if (!sink_plan(shape, B, N, T, window, sink, &p))
+    return fail(KVD_ERR_SHAPE, "%s: B=%d N=%d T=%d is too large for one call", name, B, N, T);
+  if (ws == nullptr) return fail(KVD_ERR_WORKSPACE, "workspace is NULL (%zu bytes needed)", p.end);
+  if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return fail(KVD_ERR_ALIGN, "workspace is not 256-byte aligned");
+  if (ws_bytes < p.end) return fail(KVD_ERR_WORKSPACE, "workspace holds %zu bytes, %zu needed", ws_bytes, p.end);
+  char* base = static_cast<char*>(ws);
+  a.q = q;
+  a.kv_len = kv_len;
+  a.n_new = n_new;
+  a.out = out;
+  a.ml = reinterpret_cast<float*>(base + p.ml);
+  a.acc = reinterpret_cast<float*>(base + p.acc);
+  a.T = T;
+  a.B = B;
+  a.N = N;
+  a.n_q = shape->n_q_heads;
+  a.n_kv = shape->n_kv_heads;
+  a.g = shape->n_q_heads / shape->n_kv_heads;
+  a.g_inv = a.g > 1 ? (uint32_t)(((1ull << 32) + a.g - 1) / a.g) : 0;
+  a.R = p.R;
+  a.window = window;
+  a.sink = sink;
+  a.S = p.S;
+  a.C = p.C;
+  return device_status(kvd::launch_sink(a, shape->dtype == KVD_BF16, shape->head_dim, (hipStream_t)stream), name);
+}
+
+kvd_status mx_rows_call(const kvd_attn_shape* shape, const kvd_kv_view* rows, const char* rows_name, int32_t N,
+                        const kvd_mx_view* cache, const int32_t* kv_len, const int32_t* n_new, int32_t B, int32_t T,
+                        int32_t sink, int store, void* stream, const char* name) {
+  KVD_TRY(check_shape(shape));
+  KVD_TRY(sink_sizes(B, N, T, 1, sink));
+  if (B == 0 || N == 0) return KVD_OK;
+  KVD_TRY(check_view(rows, N, rows_name));
+  KVD_TRY(check_mx_view(cache));
+  kvd::MxArgs a{};
+  int32_t cap;
+  KVD_TRY(ring_of(cache->t_cap, cache->t_off, T, sink, N, "N", &cap, &a.ring));
+  if (kv_len != nullptr) KVD_TRY(check_ptr4(kv_len, "kv_len"));
+  if (n_new != nullptr) KVD_TRY(check_ptr4(n_new, "n_new"));
+  if ((long long)B * shape->n_kv_heads * N > kvd::most_wgs(256) / 2 * 256 / (shape->head_dim / 8))
+    return fail(KVD_ERR_SHAPE, "%s: B=%d N=%d is too large for one call", name, B, N);
+  a.k = static_cast<uint8_t*>(cache->k);
+  a.v = static_cast<uint8_t*>(cache->v);
+  a.ks = static_cast<uint8_t*>(cache->k_scale);
+  a.vs = static_cast<uint8_t*>(cache->v_scale);
+  a.t_cap = cache->t_cap;
+  a.t_off = cache->t_off;
+  a.pk = rows->k;
+  a.pv = rows->v;
+  a.p_cap = rows->t_cap;
+  a.p_off = rows->t_off;
+  a.kv_len = kv_len;
+  a.n_new = n_new;
+  a.T = T;
+  a.B = B;
+  a.N = N;
+  a.n_kv = shape->n_kv_heads;
+  a.sink = sink;
+  return device_status(kvd::launch_mx(a, shape->dtype == KVD_BF16, shape->head_dim, store, (hipStream_t)stream), name);
+}
+
+}  // namespace
+
+kvd_status kvd_sink_attn(const kvd_attn_shape* shape, const void* q, int32_t N, const kvd_kv_view* kv,
+                         const int32_t* kv_len, const int32_t* n_new, int32_t B, int32_t T, int32_t window,
+                         int32_t sink, void* out, void* ws, size_t ws_bytes, void* stream) {
+  return sink_call(shape, q, N, kv, nullptr, kv_len, n_new, B, T, window, sink, out, ws, ws_bytes, stream,
+                   "kvd_sink_attn");
+}
+
+kvd_status kvd_mx_attn(const kvd_attn_shape* shape, const void* q, int32_t N, const kvd_mx_view* cache,
+                       const int32_t* kv_len, const int32_t* n_new, int32_t B, int32_t T, int32_t window,
+                       int32_t sink, void* out, void* ws, size_t ws_bytes, void* stream) {
+  KVD_TRY(check_shape(shape));
+  if (B != 0 && N != 0 && cache == nullptr) return fail(KVD_ERR_NULL, "cache is NULL");
+  return sink_call(shape, q, N, nullptr, cache, kv_len, n_new, B, T, window, sink, out, ws, ws_bytes, stream,
+                   "kvd_mx_attn");
+}
+
+size_t kvd_sink_workspace_bytes(const kvd_attn_shape* shape, int32_t B, int32_t N, int32_t T, int32_t window,
+                                int32_t sink) {
+  if (check_shape(shape) != KVD_OK || sink_sizes(B, N, T, window, sink) != KVD_OK) return 0;
+  if (B < 1 || N < 1) {
+    fail(KVD_ERR_SHAPE, "B=%d N=%d must be >= 1", B, N);
+    return 0;
+  }
+  SinkPlan p;
+  if (sink_plan(shape, B, N, T, window, sink, &p)) return p.end;
+  fail(KVD_ERR_SHAPE, "B=%d N=%d T=%d is too large for one call", B, N, T);
+  return 0;
+}
+
+kvd_status kvd_mx_store(const kvd_attn_shape* shape, const kvd_kv_view* rows, int32_t N, const kvd_mx_view* cache,
+                        const int32_t* kv_len, const int32_t* n_new, int32_t B, int32_t T, int32_t sink,
+                        void* stream) {
+  return mx_rows_call(shape, rows, "rows", N, cache, kv_len, n_new, B, T, sink, 1, stream, "kvd_mx_store");
+}
+
+kvd_status kvd_mx_load(const kvd_attn_shape* shape, const kvd_mx_view* cache, int32_t N, const int32_t* kv_len,
+                       const int32_t* n_new, int32_t B, int32_t T, int32_t sink, const kvd_kv_view* rows,
+                       void* stream) {
+  return mx_rows_call(shape, rows, "rows", N, cache, kv_len, n_new, B, T, sink, 0, stream, "kvd_mx_load");
+}
+
 namespace {
 
 // Block-forward workspace: q [B][T][n_q][hd], K and V [B][n_kv][T][hd], attention

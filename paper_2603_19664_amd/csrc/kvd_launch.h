@@ -229,6 +229,44 @@ struct RowsArgs {
 };
 hipError_t launch_rows(const RowsArgs& a, int dtype_bf16, int hd, hipStream_t st);
 
+// Attention of N new tokens of each of B sequences over the first `sink` tokens and the newest
+// `window` of a cache of `cap` rows behind t_off (kvd_sink.hip): K/V of the call's type, or 4-bit
+// numbers with scales.  ring: rows of the ring behind the sinks, 0 where every token has its row.
+struct SinkArgs {
+  const void* q;
+  const void* k;
+  const void* v;
+  const uint8_t* ks;       // nullptr: k and v hold the call's type
+  const uint8_t* vs;
+  const int32_t* kv_len;   // nullptr: T
+  const int32_t* n_new;    // nullptr: N
+  void* out;
+  float* acc;
+  float* ml;
+  int t_cap, t_off, cap, ring;
+  int T, B, N, n_q, n_kv, g, R, window, sink;
+  int S, C;
+  uint32_t g_inv;
+};
+hipError_t launch_sink(const SinkArgs& a, int dtype_bf16, int hd, hipStream_t st);
+
+// Rows of a 4-bit cache, from or to plain K/V rows [B][n_kv][p_cap][hd] from p_off on (kvd_mx.hip).
+constexpr int kMxGroup = 32;                 // elements that share a scale
+constexpr int kMxLeast = 27, kMxMost = 252;  // scale bytes of numbers: 2^-100 .. 2^125
+struct MxArgs {
+  uint8_t* k;
+  uint8_t* v;
+  uint8_t* ks;
+  uint8_t* vs;
+  void* pk;
+  void* pv;
+  const int32_t* kv_len;
+  const int32_t* n_new;
+  int t_cap, t_off, ring, p_cap, p_off;
+  int T, B, N, n_kv, sink;
+};
+hipError_t launch_mx(const MxArgs& a, int dtype_bf16, int hd, int store, hipStream_t st);
+
 // Eviction by weight (kvd_evict.hip) of the T rows of B n_kv caches down to keep.
 struct EvictArgs {
   void* k;

@@ -13,6 +13,7 @@ import dataclasses
 import os
 import re
 from dataclasses import dataclass
+from typing import NamedTuple
 
 import torch
 
@@ -54,6 +55,11 @@ class KvView(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("t_cap", ctypes.c_int32), ("t_off", ctypes.c_int32)]
 
 
+class MxView(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scale", "v_scale")] + [("t_cap", ctypes.c_int32),
+                                                                                   ("t_off", ctypes.c_int32)]
+
+
 class BlockWeights(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("gamma_attn", "w_q", "w_k", "w_v", "w_o", "gamma_mlp", "w_gate",
                                                "w_up", "w_down")] + [("d_ff", ctypes.c_int32)]
@@ -65,7 +71,7 @@ def _load() -> ctypes.CDLL:
                           "(or __graft_entry__.build()) first")
     lib = ctypes.CDLL(LIB_PATH)
     P, I32, SZ, VP = ctypes.POINTER, ctypes.c_int32, ctypes.c_size_t, ctypes.c_void_p
-    S, V = P(AttnShape), P(KvView)
+    S, V, M = P(AttnShape), P(KvView), P(MxView)
     sig = {
         "kvd_recompute_kv": [S, VP, I32, VP, VP, VP, VP, I32, I32, V, VP],
         "kvd_project_qkv": [S, VP, VP, VP, VP, VP, VP, I32, VP, V, VP],
@@ -79,6 +85,10 @@ def _load() -> ctypes.CDLL:
     sig["kvd_prefix_attn"] = [S, VP, I32, V, I32, V, VP, VP, I32, I32, VP, VP, ctypes.c_float, VP, SZ, VP]
     sig["kvd_weighted_attn"] = [S, VP, I32, V, VP, VP, I32, I32, VP, VP, ctypes.c_float, VP, SZ, VP]
     sig["kvd_evict"] = [S, V, VP, I32, I32, I32, VP, VP, VP, I32, I32, VP, SZ, VP]
+    sig["kvd_sink_attn"] = [S, VP, I32, V, VP, VP, I32, I32, I32, I32, VP, VP, SZ, VP]
+    sig["kvd_mx_attn"] = [S, VP, I32, M, VP, VP, I32, I32, I32, I32, VP, VP, SZ, VP]
+    sig["kvd_mx_store"] = [S, V, I32, M, VP, VP, I32, I32, I32, VP]
+    sig["kvd_mx_load"] = [S, M, I32, VP, VP, I32, I32, I32, V, VP]
     for name, args in sig.items():
         f = getattr(lib, name)
         f.argtypes = args
@@ -99,6 +109,8 @@ def _load() -> ctypes.CDLL:
     lib.kvd_prefix_workspace_bytes.restype = SZ
     lib.kvd_evict_workspace_bytes.argtypes = [S, I32, I32]
     lib.kvd_evict_workspace_bytes.restype = SZ
+    lib.kvd_sink_workspace_bytes.argtypes = [S, I32, I32, I32, I32, I32]
+    lib.kvd_sink_workspace_bytes.restype = SZ
     lib.kvd_combine.argtypes = [S, I32, I32, VP, SZ, VP, VP]
     lib.kvd_combine.restype = ctypes.c_int
     lib.kvd_workspace_bytes.argtypes = [S, I32, I32, I32, I32]
@@ -653,6 +665,124 @@ def kvd_evict(shape: Shape, k, v, T: int, keep: int, weight, ws, pos=None, last_
     _run_on(dev, lib.kvd_evict, ctypes.byref(shape.c()), ctypes.byref(view), _dev_ptr(kv_len, "kv_len", i32, dev), B, T,
             keep, _dev_ptr(weight, "weight", torch.float32, dev), _dev_ptr(pos, "pos", i32, dev),
             _dev_ptr(last_pos, "last_pos", i32, dev), sink, recent, _dev_ptr(ws, "ws", ws.dtype, dev), ws.nbytes)
+
+
+class MxCache(NamedTuple):
+    """A 4-bit cache (kvd_mx_view): codes [B, n_kv, t_cap, hd / 2] and scales [B, n_kv, t_cap, hd / 32] of K and V,
+    uint8, used from row t_off on."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+    t_off: int = 0
+
+
+def mx_cache(shape: Shape, B: int, t_cap: int, device="cuda") -> MxCache:
+    """A 4-bit cache of t_cap rows per sequence and KV head, all of them 0."""
+    def zeros(n):
+        return torch.zeros((B, shape.n_kv_heads, t_cap, n), dtype=torch.uint8, device=device)
+    hd = shape.head_dim
+    return MxCache(zeros(hd // 2), zeros(hd // 2), zeros(hd // 32), zeros(hd // 32))
+
+
+def kvd_sink_workspace_bytes(shape: Shape, B: int, N: int, T: int, window: int, sink: int = 0) -> int:
+    return lib.kvd_sink_workspace_bytes(ctypes.byref(shape.c()), B, N, T, window, sink)
+
+
+def _mx_view(cache, shape, B, dev):
+    if not isinstance(cache, MxCache):
+        raise ValueError("cache must be an MxCache")
+    k, v, ks, vs, t_off = cache
+    if not isinstance(k, torch.Tensor) or k.dim() != 4:
+        raise ValueError("cache.k must be a [B, n_kv, t_cap, head_dim / 2] tensor")
+    n_kv, hd, t_cap, u8 = shape.n_kv_heads, shape.head_dim, k.shape[2], torch.uint8
+    codes, scales = (B, n_kv, t_cap, hd // 2), (B, n_kv, t_cap, hd // 32)
+    _dims(k, "cache.k", codes)
+    _dims(v, "cache.v", codes)
+    _dims(ks, "cache.k_scale", scales)
+    _dims(vs, "cache.v_scale", scales)
+    return MxView(_dev_ptr(k, "cache.k", u8, dev), _dev_ptr(v, "cache.v", u8, dev),
+                  _dev_ptr(ks, "cache.k_scale", u8, dev), _dev_ptr(vs, "cache.v_scale", u8, dev), t_cap, t_off)
+
+
+def _sink_call(fn, shape, q, view, T, window, sink, out, ws, kv_len, n_new):
+    # q's extents first; view(B, dev) checks the keys
+    if not isinstance(q, torch.Tensor) or q.dim() not in (3, 4):
+        raise ValueError("q must be a [B, N, n_q, head_dim] or [B, n_q, head_dim] tensor")
+    dims = q.shape
+    B, N = dims[0], dims[1] if len(dims) == 4 else 1
+    if dims[-1] != shape.head_dim or dims[-2] != shape.n_q_heads:
+        raise ValueError(f"q has shape {tuple(dims)}, expected [.., {shape.n_q_heads}, {shape.head_dim}]")
+    if out is None:
+        raise ValueError("out is required")
+    _dims(out, "out", dims)
+    if kv_len is not None:
+        _dims(kv_len, "kv_len", (B,))
+    if n_new is not None:
+        _dims(n_new, "n_new", (B,))
+    if not isinstance(ws, torch.Tensor):
+        raise ValueError("ws must be a torch tensor")
+    dt, dev, i32 = shape.torch_dtype, _device_of(q, "q"), torch.int32
+    _run_on(dev, fn, ctypes.byref(shape.c()), _dev_ptr(q, "q", dt, dev), N, ctypes.byref(view(B, dev)),
+            _dev_ptr(kv_len, "kv_len", i32, dev), _dev_ptr(n_new, "n_new", i32, dev), B, T, window, sink,
+            _dev_ptr(out, "out", dt, dev), _dev_ptr(ws, "ws", ws.dtype, dev), ws.nbytes)
+
+
+def kvd_sink_attn(shape: Shape, q, k, v, T: int, window: int, out, ws, sink: int = 0, kv_len=None, n_new=None,
+                  t_off: int = 0):
+    """Attention of q [B, N, n_q, hd] (or [B, n_q, hd]), the last n_new [B] int32 (N if None) of kv_len [B] int32
+    (T if None) tokens, over the first `sink` tokens and the newest `window` of each new one.  Rows t_off.. of k / v
+    [B, n_kv, t_cap, hd] hold the tokens in order if T fit, else the first `sink` and behind them a ring of the
+    others (t_cap - t_off - sink >= window + N - 1 rows).  Runs on the tensors' device and its current stream."""
+    def view(B, dev):
+        if k is None or v is None:
+            raise ValueError("kv: k and v are required")
+        if not isinstance(k, torch.Tensor) or k.dim() != 4:
+            raise ValueError("kv: k and v must both be [B, n_kv, t_cap, head_dim] tensors")
+        want = (B, shape.n_kv_heads, k.shape[2], shape.head_dim)
+        _dims(k, "kv_k", want)
+        _dims(v, "kv_v", want)
+        dt = shape.torch_dtype
+        return KvView(_dev_ptr(k, "kv_k", dt, dev), _dev_ptr(v, "kv_v", dt, dev), want[2], t_off)
+    _sink_call(lib.kvd_sink_attn, shape, q, view, T, window, sink, out, ws, kv_len, n_new)
+
+
+def kvd_mx_attn(shape: Shape, q, cache: MxCache, T: int, out, ws, window: int = None, sink: int = 0, kv_len=None,
+                n_new=None):
+    """kvd_sink_attn over a 4-bit cache (window None: every token)."""
+    _sink_call(lib.kvd_mx_attn, shape, q, lambda B, dev: _mx_view(cache, shape, B, dev), T,
+               max(T, 1) if window is None else window, sink, out, ws, kv_len, n_new)
+
+
+def _mx_rows(shape, k, v, N, cache, T, t_off, kv_len, n_new):
+    if not isinstance(k, torch.Tensor) or k.dim() != 4:
+        raise ValueError("rows: k and v must both be [B, n_kv, t_cap, head_dim] tensors")
+    B = k.shape[0]
+    t_cap = _own_dims(k, v, "rows", B, shape, N, t_off)
+    if kv_len is not None:
+        _dims(kv_len, "kv_len", (B,))
+    if n_new is not None:
+        _dims(n_new, "n_new", (B,))
+    dt, dev, i32 = shape.torch_dtype, _device_of(k, "rows_k"), torch.int32
+    rows = KvView(_dev_ptr(k, "rows_k", dt, dev), _dev_ptr(v, "rows_v", dt, dev), t_cap, t_off)
+    return (dev, ctypes.byref(shape.c()), ctypes.byref(rows), ctypes.byref(_mx_view(cache, shape, B, dev)),
+            _dev_ptr(kv_len, "kv_len", i32, dev), _dev_ptr(n_new, "n_new", i32, dev), B)
+
+
+def kvd_mx_store(shape: Shape, k, v, N: int, cache: MxCache, T: int, sink: int = 0, kv_len=None, n_new=None,
+                 t_off: int = 0):
+    """Put the last n_new [B] int32 (N if None) of kv_len [B] int32 (T if None) tokens, rows t_off.. of k / v
+    [B, n_kv, t_cap, hd], into a 4-bit cache: in order if its rows hold T tokens, else the first `sink` and behind
+    them a ring of the others."""
+    dev, s, rows, view, lens, new, B = _mx_rows(shape, k, v, N, cache, T, t_off, kv_len, n_new)
+    _run_on(dev, lib.kvd_mx_store, s, rows, N, view, lens, new, B, T, sink)
+
+
+def kvd_mx_load(shape: Shape, cache: MxCache, T: int, N: int, k, v, sink: int = 0, kv_len=None, n_new=None,
+                t_off: int = 0):
+    """Read the last n_new tokens of a 4-bit cache back into rows t_off.. of k / v (kvd_mx_store's inverse)."""
+    dev, s, rows, view, lens, new, B = _mx_rows(shape, k, v, N, cache, T, t_off, kv_len, n_new)
+    _run_on(dev, lib.kvd_mx_load, s, view, N, lens, new, B, T, sink, rows)
 
 
 def kvd_pack_matrix(w):
