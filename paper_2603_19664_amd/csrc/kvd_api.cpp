@@ -1242,12 +1242,38 @@ struct SinkPlan {
 bool sink_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T, int32_t window, int32_t sink, SinkPlan* p) {
   *p = SinkPlan{};
   const int32_t g = s->n_q_heads / s->n_kv_heads;
-  const long long R = (long long)N * g, Rt = R * B;
-  if (Rt * s->n_kv_heads > INT32_MAX || Rt >= 1ll << 28) return false;
+  const long long R = (long long)N * g, Rt = R * B, units = (long long)B * s->n_kv_heads, rows = R * units;
+  if (rows > INT32_MAX || Rt >= 1ll << 28) return false;
   p->R = (int32_t)R;
+  const bool few = s->dtype != KVD_BF16 || R <= kvd::kRowsFew;
+  const long long RB = few ? kvd::kRowsWave : kvd::kRowsTile, nb = (R + RB - 1) / RB;
+  // keys of a block: its tokens' windows together, and the sinks before them
+  const long long tokens = std::min<long long>(N, (RB + g - 2) / g + 1), span = (long long)window + tokens - 1;
+  const long long keys = std::min<long long>(T, span + sink);
+  if (keys > INT32_MAX - 8192) return false;
+  // Slots for which the workspace has room: as of a causal call, which has most, and falling with no length.
+  // Blocks that windows limit are of one size.
+  int32_t S = 1;
   p->S = 1;
-  p->end = 256;
-  return Rt * s->n_kv_heads <= kvd::most_wgs(256);
+  p->C = kvd::kRowsSmall;
+  if (keys > kvd::kRowsSmall) {
+    p->S = causal_slots(units * nb, rows, (int32_t)keys, few, N, false, kvd::kRowsTargetWgs);
+    S = most_slots(p->S);
+    if (keys < T) p->S = row_slots(units * nb, rows, keys, few, false);
+    cut_keys(keys, few, &p->S, &p->C);
+  }
+  S = std::max(S, p->S);
+  size_t at = 0;
+  const auto take = [&at](size_t bytes) {
+    const size_t o = at;
+    at += kvd::align_up(bytes, 256);
+    return o;
+  };
+  p->ml = take(S > 1 ? 8 * (size_t)S * rows : 0);
+  p->acc = take(S > 1 ? 4 * (size_t)S * rows * s->head_dim : 0);
+  p->end = std::max<size_t>(at, 256);
+  const int per_wg = 4 / kvd::rows_finish_waves(S);
+  return std::max(units * nb * p->S, (rows + per_wg - 1) / per_wg) <= kvd::most_wgs(256);
 }
 
 kvd_status sink_sizes(int32_t B, int32_t N, int32_t T, int32_t window, int32_t sink) {
@@ -1312,7 +1338,7 @@ kvd_status sink_call(const kvd_attn_shape* shape, const void* q, int32_t N, cons
   a.g = shape->n_q_heads / shape->n_kv_heads;
   a.g_inv = a.g > 1 ? (uint32_t)(((1ull << 32) + a.g - 1) / a.g) : 0;
   a.R = p.R;
-  a.window = window;
+  a.window = std::min(window, T);
   a.sink = sink;
   a.S = p.S;
   a.C = p.C;

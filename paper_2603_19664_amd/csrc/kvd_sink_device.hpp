@@ -37,7 +37,7 @@ struct SinkKeys {
 };
 __device__ __forceinline__ SinkKeys sink_keys(const SinkArgs& a, int p0, int p1) {
   SinkKeys k;
-  const int w0 = max(p0 - a.window + 1, 0);
+  const int w0 = max(max(p0, -1) - a.window + 1, 0);  // window <= T
   k.ns = min(a.sink, w0);
   k.skip = w0 - k.ns;
   k.n = p1 < 0 ? 0 : p1 + 1 - k.skip;
@@ -51,6 +51,7 @@ struct SinkRow {
   int lo, hi;
 };
 __device__ __forceinline__ SinkRow sink_row_of(const SinkArgs& a, const SinkKeys& k, int p) {
+  p = max(p, -1);
   return SinkRow{p - a.window + 1 - k.skip, p + 1 - k.skip};
 }
 

@@ -147,12 +147,15 @@ def test_empty_calls():
 def test_workspace_does_not_fall_as_tokens_grow(dtype, heads):
     s = shape(dtype=dtype, n_q_heads=heads[0], n_kv_heads=heads[1], head_dim=heads[2])
     grid = sorted({1, 2, 16, 17, 100, 127, 128, 129, 255, 256, 257, 400, 511, 513, 1000, 2048, 2049, 5000, 16384, 40000,
-                   1 << 20, INT_MAX, *range(1, 6000, 13)})
+                   1 << 20, INT_MAX - 8192, *range(1, 6000, 13)})
     for B, N in ((1, 1), (3, 1), (64, 1), (1, 33), (2, 300), (7, 9), (1, 3000)):
         for window, sink in ((INT_MAX, 0), (1024, 4), (64, 0), (1, 100), (4096, INT_MAX)):
             sizes = [lib.kvd_sink_workspace_bytes(ref(s), B, N, t, window, sink) for t in grid]
             assert sizes[0] >= 256 and sizes == sorted(sizes)
-    n = lib.kvd_sink_workspace_bytes(ref(s), 2, 1, 16, 8, 4)
+    f = lib.kvd_sink_workspace_bytes
+    assert f(ref(s), 2, 1, INT_MAX, 1024, 4) == f(ref(s), 2, 1, 5000, 1024, 4)  # a stream without end
+    assert f(ref(s), 2, 1, INT_MAX, INT_MAX, 0) == 0
+    n = f(ref(s), 2, 1, 16, 8, 4)
     assert sink_attn(s, n=n - 1) == mx_attn(s, n=n - 1) == kvd.KVD_ERR_WORKSPACE
 
 
