@@ -1239,7 +1239,8 @@ struct SinkPlan {
 };
 
 // False when a size passes the kernels' 32-bit indexes or a launch's number of threads.
-bool sink_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T, int32_t window, int32_t sink, SinkPlan* p) {
+bool sink_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T, int32_t window, int32_t sink, bool mx,
+               SinkPlan* p) {
   *p = SinkPlan{};
   const int32_t g = s->n_q_heads / s->n_kv_heads;
   const long long R = (long long)N * g, Rt = R * B, units = (long long)B * s->n_kv_heads, rows = R * units;
@@ -1250,16 +1251,25 @@ bool sink_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T, int32_t
   // keys of a block: its tokens' windows together, and the sinks before them
   const long long tokens = std::min<long long>(N, (RB + g - 2) / g + 1), span = (long long)window + tokens - 1;
   const long long keys = std::min<long long>(T, span + sink);
-  if (keys > INT32_MAX - 8192) return false;
-  // Slots for which the workspace has room: as of a causal call, which has most, and falling with no length.
-  // Blocks that windows limit are of one size.
+  if (keys > INT32_MAX - 8192 || nb > 65535 || units > INT32_MAX) return false;
+  // Few rows fill the chip once (64 streams of 1028 rows at head_dim 256: 43 us in one slot each, 48 in two), 4 bits
+  // up to three times while a slot keeps 512 keys (8 x 32768 keys 59 -> 57 us, 64 x 4096 .. 8192 keys 32.2 -> 30.2; 16
+  // drafts over 2056 keys in 8 slots instead of 4 14.8 -> 18.6).  Blocks that windows limit are of one size.  The
+  // workspace has room for the slots of a causal call, which has most, and falls with no length.
   int32_t S = 1;
   p->S = 1;
   p->C = kvd::kRowsSmall;
   if (keys > kvd::kRowsSmall) {
-    p->S = causal_slots(units * nb, rows, (int32_t)keys, few, N, false, kvd::kRowsTargetWgs);
+    const long long u = units * nb, wgs = few ? 256 : kvd::kRowsTargetWgs;
+    const auto slots = [&](bool causal) {
+      int32_t n = causal ? causal_slots(u, rows, (int32_t)keys, few, N, false, wgs)
+                         : row_slots(u, rows, keys, few, false, false, wgs);
+      if (few && mx) n = std::max(n, (int32_t)std::min({(768 + u - 1) / u, keys / 512, (long long)kvd::kRowsMostSlots}));
+      return n;
+    };
+    p->S = slots(true);
     S = most_slots(p->S);
-    if (keys < T) p->S = row_slots(units * nb, rows, keys, few, false);
+    if (keys < T) p->S = slots(false);
     cut_keys(keys, few, &p->S, &p->C);
   }
   S = std::max(S, p->S);
@@ -1318,7 +1328,7 @@ kvd_status sink_call(const kvd_attn_shape* shape, const void* q, int32_t N, cons
   if (kv_len != nullptr) KVD_TRY(check_ptr4(kv_len, "kv_len"));
   if (n_new != nullptr) KVD_TRY(check_ptr4(n_new, "n_new"));
   SinkPlan p;
-  if (!sink_plan(shape, B, N, T, window, sink, &p))
+  if (!sink_plan(shape, B, N, T, window, sink, mx != nullptr, &p))
     return fail(KVD_ERR_SHAPE, "%s: B=%d N=%d T=%d is too large for one call", name, B, N, T);
   if (ws == nullptr) return fail(KVD_ERR_WORKSPACE, "workspace is NULL (%zu bytes needed)", p.end);
   if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return fail(KVD_ERR_ALIGN, "workspace is not 256-byte aligned");
@@ -1405,8 +1415,9 @@ size_t kvd_sink_workspace_bytes(const kvd_attn_shape* shape, int32_t B, int32_t 
     fail(KVD_ERR_SHAPE, "B=%d N=%d must be >= 1", B, N);
     return 0;
   }
-  SinkPlan p;
-  if (sink_plan(shape, B, N, T, window, sink, &p)) return p.end;
+  SinkPlan p, q;
+  if (sink_plan(shape, B, N, T, window, sink, false, &p) && sink_plan(shape, B, N, T, window, sink, true, &q))
+    return std::max(p.end, q.end);
   fail(KVD_ERR_SHAPE, "B=%d N=%d T=%d is too large for one call", B, N, T);
   return 0;
 }

@@ -30,15 +30,14 @@ struct SinkItem {
 __device__ __forceinline__ int sink_slots(const SinkArgs& a, const SinkKeys& k) {
   return max((int)(((uint32_t)k.n + (uint32_t)a.C - 1u) / (uint32_t)a.C), 1);
 }
-// False where the workgroup has nothing to do.  Heavy blocks (the last tokens) first.
+// Grid: B n_kv (sequence, KV head), slots, blocks.  False where the workgroup has nothing to do.
 template <int RB>
-__device__ __forceinline__ bool sink_item(const SinkArgs& a, int item, SinkItem& it) {
-  const int nb = (a.R + RB - 1) / RB, units = a.B * a.n_kv, x = item / units, u = item - x * units;
-  it.j = u % a.n_kv;
-  it.b = u / a.n_kv;
-  const int y = x / a.S;
-  it.s = (x + y) % a.S;  // from another slot in every block: XCDs (item % 8) share early and late keys
-  it.r0 = (nb - 1 - y) * RB;
+__device__ __forceinline__ bool sink_item(const SinkArgs& a, SinkItem& it) {
+  it.b = (int)(blockIdx.x / (uint32_t)a.n_kv);
+  it.j = (int)blockIdx.x - it.b * a.n_kv;
+  // from another slot in every block: XCDs (workgroups in turn) share early and late keys
+  it.s = a.S == 1 ? 0 : (int)((blockIdx.y + blockIdx.z) % (uint32_t)a.S);
+  it.r0 = (int)(gridDim.z - 1 - blockIdx.z) * RB;  // heavy blocks, the last tokens, first
   const SinkSeq sq = sink_seq(a.kv_len, a.n_new, a.T, a.N, it.b);
   it.nr = min(RB, sq.n * a.g - it.r0);
   if (it.nr <= 0) return false;
@@ -52,6 +51,53 @@ __device__ __forceinline__ bool sink_item(const SinkArgs& a, int item, SinkItem&
 }
 __device__ __forceinline__ size_t sink_state(const SinkArgs& a, int s, int b, int j, int r) {
   return ((size_t)s * a.n_kv + j) * ((size_t)a.B * a.R) + (size_t)b * a.R + r;
+}
+// The item's keys in blocks of KB that lie in neighbouring rows each: those of the sinks, of the
+// window up to the ring's end, and behind it.  All of it is uniform.
+template <int KB>
+struct SinkBlocks {
+  int e0, e1, n, n0, n1, blocks;  // ends of the first two parts, keys; blocks of the first part, of the first two, in all
+  int row0, d, ring;
+  __device__ __forceinline__ SinkBlocks(const SinkItem& it) {
+    n = it.n;
+    e0 = min(max(it.keys.ns - it.x0, 0), n);
+    e1 = min(max(it.keys.cap - it.keys.d - it.x0, e0), n);
+    n0 = (e0 + KB - 1) / KB;
+    n1 = n0 + (e1 - e0 + KB - 1) / KB;
+    blocks = n1 + (n - e1 + KB - 1) / KB;
+    row0 = it.x0;
+    d = it.keys.d;
+    ring = it.keys.ring;
+  }
+  // block i: keys x .. end - 1 (at most KB of them), from cache row `row` on
+  struct Block {
+    int x, end, row;
+  };
+  __device__ __forceinline__ Block at(int i) const {
+    Block b;
+    if (i < n0) {
+      b.x = KB * i;
+      b.end = e0;
+      b.row = row0 + b.x;
+    } else if (i < n1) {
+      b.x = e0 + KB * (i - n0);
+      b.end = e1;
+      b.row = row0 + b.x + d;
+    } else {
+      b.x = e1 + KB * (i - n1);
+      b.end = n;
+      b.row = row0 + b.x + d - ring;
+    }
+    b.x = __builtin_amdgcn_readfirstlane(b.x);
+    b.end = __builtin_amdgcn_readfirstlane(min(b.end, b.x + KB));
+    b.row = __builtin_amdgcn_readfirstlane(b.row);
+    return b;
+  }
+};
+// Rows row .. row + n - 1 of an array with `bytes` to a row: reads behind them give 0.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_resource(const void* p, size_t row, int n, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(p)) + row * bytes, (short)0,
+                                           n * bytes, 0x00027000);
 }
 // Element offset of row r of (b, j) in q and out.
 __device__ __forceinline__ size_t sink_q(const SinkArgs& a, int b, int j, int r, int hd) {
@@ -71,6 +117,18 @@ __device__ __forceinline__ void mx_put(u32x4_t code, float scale, char* row_at, 
     *reinterpret_cast<u32x4_t*>(row_at + ((4 * g + e) ^ swz ^ mx_swz(g)) * 16) =
         u32x4_t{mx_bf16x2<0>(w, scale), mx_bf16x2<1>(w, scale), mx_bf16x2<2>(w, scale), mx_bf16x2<3>(w, scale)};
   }
+}
+
+// 32 rows of V by direct copies into a wave's slice of LDS, 16-byte chunks permuted (few_v_swz).
+template <int HD>
+__device__ __forceinline__ void copy_v32(__amdgpu_buffer_rsrc_t res, char* dst) {
+  constexpr int CPR = HD / 8, RPI = 64 / CPR;
+  const int lane = (int)fresh(threadIdx.x & 63);
+#pragma unroll
+  for (int l = 0; l < 32 / RPI; ++l)
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        res, (__attribute__((address_space(3))) void*)(dst + 1024 * l), 16,
+        (lane / CPR) * HD * 2 + 16 * (lane % CPR ^ few_v_swz<HD>(lane / CPR + RPI * l)), 1024 * l, 0, 0);
 }
 
 // x as a sum of bf16 parts, rounded (P parts), returned as the packed pairs of (x, y).
@@ -110,23 +168,27 @@ __device__ __forceinline__ void split2_trunc(float x, float y, uint32_t (&w)[P])
 // (two for bf16 queries: 2^-17 of a weight is lost; three for fp32), V through LDS: plain by direct copies,
 // 4 bits as the bf16 numbers that they are (one instruction for two), read transposed.
 // K of the next block is asked for when the scores are taken, V after its product.
+// Workgroups per CU that the registers are to leave room for.
+constexpr int few_wgs(int hd, bool mx, bool bf) {
+  return hd == 256 ? (bf ? 2 : 1) : hd == 128 ? 3 : 4;
+}
 template <int HD, bool MX, typename QT>
-__global__ __launch_bounds__(256, 2) void sink_few_kernel(SinkArgs a) {
+__global__ __launch_bounds__(256, few_wgs(HD, MX, sizeof(QT) == 2)) void sink_few_kernel(SinkArgs a) {
   constexpr bool BF = sizeof(QT) == 2;
-  constexpr int NW = 4, KB = 32, KC = HD / 32, DB = HD / 16;
+  constexpr int NW = 4, KB = 32, KC = HD / 32, DB = HD / 16, kLead = 4;
   constexpr int QP = BF ? 1 : 3, PP = BF ? 2 : 3;  // parts of a query element and of a weight
   constexpr int KW = HD == 64 ? 2 : 4;             // words of 4-bit codes a lane loads at once
   constexpr int KL = HD / 32 / KW;                 // how many times (MX)
   constexpr int G = HD / kMxGroup, NV = HD / 64;   // groups of a row; groups of V a lane turns into bf16
   __shared__ __align__(1024) uint16_t vbuf[NW][KB * HD];
   __shared__ float ml[NW][16][2];
+  __shared__ unsigned long long bads[NW];
   const int tid = threadIdx.x, lane = tid & 63, w = wave_id(), hq = lane & 15, lg = lane >> 4;
   SinkItem it;
-  if (!sink_item<16>(a, (int)blockIdx.x, it)) return;
-  const int nblk = (it.n + KB - 1) / KB;
-  const int nb = nblk > w ? (nblk - 1 - w) / NW + 1 : 0;  // this wave's blocks: w, w + NW, ..
+  if (!sink_item<16>(a, it)) return;
+  const SinkBlocks<KB> blk(it);
+  const int nb = blk.blocks > w ? (blk.blocks - 1 - w) / NW + 1 : 0;  // this wave's blocks: w, w + NW, ..
   const size_t base = ((size_t)it.b * a.n_kv + it.j) * a.t_cap + a.t_off;
-  const auto row_at = [&](int x) { return base + it.keys.row(it.x0 + min(x, it.n - 1)); };
   // keys of this slot that the lane's row sees: x < hi with x < sink or x >= lo; that every row sees
   const auto seen_by = [&](int r) {
     SinkRow s = sink_row_of(a, it.keys, it.p0 + token_of(a, it.r0 + min(r, it.nr - 1)));
@@ -164,56 +226,51 @@ __global__ __launch_bounds__(256, 2) void sink_few_kernel(SinkArgs a) {
   // K of a block: two sets of 16 keys
   u32x4_t kp[2][MX ? 1 : KC];
   uint32_t kc[2][MX ? KL : 1][KW];
-  uint32_t ks[2][MX ? KL : 1];
+  uint8_t ks[2][MX ? KL : 1];  // (as 32 bits, their extension waited for the load that it follows)
   u32x4_t vc[MX ? NV : 1];
-  uint32_t vs[MX ? NV : 1];
+  uint8_t vs[MX ? NV : 1];
   char* const vl = reinterpret_cast<char*>(vbuf[w]);
-  auto load_k = [&](int i) {
-    const int kb = KB * (w + NW * i);
+  typedef typename SinkBlocks<KB>::Block Block;
+  auto load_k = [&](const Block& kb) {
+    const auto res = rows_resource(a.k, base + kb.row, kb.end - kb.x, MX ? HD / 2 : HD * 2);
+    if constexpr (MX) {
+      const auto sres = rows_resource(a.ks, base + kb.row, kb.end - kb.x, G);
+      const int at = hq * (HD / 2) + 4 * KW * lg, sat = hq * G + (HD == 64 ? lg >> 1 : lg);
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const size_t r = row_at(kb + 16 * t + hq);
-      if constexpr (MX) {
-        const uint8_t* src = static_cast<const uint8_t*>(a.k) + r * (HD / 2) + 4 * KW * lg;
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int l = 0; l < KL; ++l) {
           if constexpr (KW == 4) {
-            const u32x4_t v = *reinterpret_cast<const u32x4_t*>(src + 64 * l);
+            const auto v = __builtin_amdgcn_raw_buffer_load_b128(res, at + 16 * t * (HD / 2) + 64 * l, 0, 0);
 #pragma unroll
             for (int e = 0; e < 4; ++e) kc[t][l][e] = v[e];
           } else {
-            const uint2 v = *reinterpret_cast<const uint2*>(src);
-            kc[t][l][0] = v.x;
-            kc[t][l][1] = v.y;
+            const auto v = __builtin_amdgcn_raw_buffer_load_b64(res, at + 16 * t * (HD / 2), 0, 0);
+            kc[t][l][0] = v[0];
+            kc[t][l][1] = v[1];
           }
-          ks[t][l] = a.ks[r * G + (HD == 64 ? lg >> 1 : lg + 4 * l)];
+          ks[t][l] = __builtin_amdgcn_raw_buffer_load_b8(sres, sat + 16 * t * G + 4 * l, 0, 0);
         }
-      } else {
-        const uint16_t* src = static_cast<const uint16_t*>(a.k) + r * HD + 8 * lg;
+    } else {
+      const int at = hq * HD * 2 + 16 * lg;
 #pragma unroll
-        for (int c = 0; c < KC; ++c) kp[t][c] = *reinterpret_cast<const u32x4_t*>(src + 32 * c);
-      }
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int c = 0; c < KC; ++c)
+          kp[t][c] = __builtin_amdgcn_raw_buffer_load_b128(res, at + 64 * c, 32 * t * HD, 0);
     }
   };
-  auto load_v = [&](int i) {
-    const int kb = KB * (w + NW * i);
+  auto load_v = [&](const Block& kb) {
+    const auto res = rows_resource(a.v, base + kb.row, kb.end - kb.x, MX ? HD / 2 : HD * 2);
     if constexpr (MX) {
+      const auto sres = rows_resource(a.vs, base + kb.row, kb.end - kb.x, G);
 #pragma unroll
       for (int l = 0; l < NV; ++l) {
-        const int id = lane + 64 * l;
-        const size_t r = row_at(kb + id / G);
-        vc[l] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint8_t*>(a.v) + r * (HD / 2) + 16 * (id % G));
-        vs[l] = a.vs[r * G + id % G];
+        vc[l] = __builtin_amdgcn_raw_buffer_load_b128(res, 16 * lane + 1024 * l, 0, 0);
+        vs[l] = __builtin_amdgcn_raw_buffer_load_b8(sres, lane + 64 * l, 0, 0);
       }
     } else {
-      constexpr int CPR = HD / 8, RPI = 64 / CPR;
-#pragma unroll
-      for (int l = 0; l < KB / RPI; ++l) {
-        const int r = lane / CPR + RPI * l;
-        const uint16_t* src = static_cast<const uint16_t*>(a.v) + row_at(kb + r) * HD + 8 * (lane % CPR ^ few_v_swz<HD>(r));
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
-                                         (__attribute__((address_space(3))) void*)(vl + 1024 * l), 16, 0, 0);
-      }
+      copy_v32<HD>(res, vl);
     }
   };
   // every LDS read of the wave is done: its slice may be written again
@@ -222,12 +279,12 @@ __global__ __launch_bounds__(256, 2) void sink_few_kernel(SinkArgs a) {
     __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
     __builtin_amdgcn_sched_barrier(0);
   };
-  if (nb > 0) {
-    load_k(0);
-    load_v(0);
-  }
-  const int vrow = 4 * lg + (hq >> 2);
-  const uint32_t vbase = vrow * HD * 2 + ((((hq & 3) >> 1) ^ few_v_swz<HD>(vrow)) << 4) + 8 * (hq & 1);
+  // byte offsets in LDS: of the lane's V operands, and of the bf16 numbers that it makes (group lane % G of row lane /
+  // G; 64 lanes on, the swizzles are the same)
+  char* const lds = reinterpret_cast<char*>(&vbuf[0][0]);
+  const int vrow = 4 * lg + (hq >> 2), prow = lane / G, pg = lane % G;
+  const uint32_t vrow_at = (w * KB + vrow) * HD * 2 + ((((hq & 3) >> 1) ^ few_v_swz<HD>(vrow)) << 4) + 8 * (hq & 1);
+  const uint32_t put_at = (w * KB + prow) * HD * 2 + ((4 * pg ^ few_v_swz<HD>(prow) ^ mx_swz(pg)) << 4);
 
   f32x4_t o[DB];
   float m_run, l_run;
@@ -236,19 +293,27 @@ __global__ __launch_bounds__(256, 2) void sink_few_kernel(SinkArgs a) {
   int pass = 0;
   unsigned long long bad = 0;  // bit i % 64: block i of the wave holds such a value
 again:
+  Block kb{0, 0, 0};
+  if (nb > 0) {
+    kb = blk.at(w);
+    load_k(kb);
+    load_v(kb);
+  }
 #pragma unroll
   for (int db = 0; db < DB; ++db) o[db] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
   m_run = -INFINITY;
   l_run = 0.0f;
-  for (int i = 0; i < nb; ++i) {
-    const int kb = KB * (w + NW * i);
-    const bool masked = kb + KB > all_hi || (kb + KB > sink && all_lo > max(kb, sink));
-    f32x4_t st[2];
+  // One copy of the code, also for a wave's last block, whose successor is empty: a small call waits for its
+  // instructions (60 ns for 64 bytes), and with a condition around the loads every wait was one for all of them.
+  auto step = [&](auto second, int i) {
+    constexpr bool SECOND = decltype(second)::value != 0;
+    const Block kb1 = i + 1 < nb ? blk.at(w + NW * (i + 1)) : Block{0, 0, 0};
+    const bool masked = kb.x + KB > min(all_hi, kb.end) || (kb.end > sink && all_lo > max(kb.x, sink));
+    f32x4_t st[2] = {{0.0f, 0.0f, 0.0f, 0.0f}, {0.0f, 0.0f, 0.0f, 0.0f}};
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      st[t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int c = 0; c < KC; ++c)
 #pragma unroll
-      for (int c = 0; c < KC; ++c) {
+      for (int t = 0; t < 2; ++t) {  // two chains of products
         u32x4_t kf;
         if constexpr (MX) {
           const uint32_t code = kc[t][c / KW][c % KW];
@@ -265,36 +330,45 @@ again:
               __builtin_bit_cast(bf16x8_t, make_uint4(qw[e][c][0], qw[e][c][1], qw[e][c][2], qw[e][c][3])), st[t], 0, 0,
               0);
       }
-    }
-    if (i + 1 < nb) load_k(i + 1);
+    load_k(kb1);
     if constexpr (MX) {
+      const uint32_t to = fresh(put_at);
       uint32_t found = 0;
 #pragma unroll
       for (int l = 0; l < NV; ++l) {
-        const int id = lane + 64 * l, r = id / G, g = id % G;
         u32x4_t code = vc[l];
         uint32_t byte = vs[l];
-        if (pass == 1 && byte == 255) {
+        if (SECOND && byte == 255) {
           found = 1;
           byte = 127;
           code = u32x4_t{0u, 0u, 0u, 0u};
         }
-        mx_put(code, mx_scale(byte), vl + r * HD * 2, g, few_v_swz<HD>(r));
-      }
-      if (pass == 1 && __any(found != 0)) bad |= 1ull << (i & 63);
-      if (i + 1 < nb) load_v(i + 1);
-    }
-    // st[t][r]: key kb + 16 t + 4 lg + r, row hq
-    float sv[8], mx = -INFINITY;
+        const float scale = mx_scale(byte);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int x = kb + 16 * (e >> 2) + 4 * lg + (e & 3);
-      sv[e] = st[e >> 2][e & 3] * ScoreScale<HD>::v;
-      if (masked) sv[e] = x < mine.hi && (x < sink || x >= mine.lo) ? sv[e] : -INFINITY;
-      mx = fmaxf(mx, sv[e]);
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t cw = code[e];
+          *reinterpret_cast<u32x4_t*>(lds + (to ^ (e << 4)) + l * (64 / G) * HD * 2) =
+              u32x4_t{mx_bf16x2<0>(cw, scale), mx_bf16x2<1>(cw, scale), mx_bf16x2<2>(cw, scale), mx_bf16x2<3>(cw, scale)};
+        }
+      }
+      if (SECOND && __any(found != 0)) bad |= 1ull << (i & 63);
+      load_v(kb1);
     }
+    // st[t][r]: key kb.x + 16 t + 4 lg + r, row hq
+    if (masked) {
+      asm volatile("");  // one branch
+      const int hi = min(mine.hi, kb.end);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int x = kb.x + 16 * (e >> 2) + 4 * lg + (e & 3);
+        st[e >> 2][e & 3] = (x < hi) & ((x < sink) | (x >= mine.lo)) ? st[e >> 2][e & 3] : -INFINITY;
+      }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mx = fmaxf(mx, st[e >> 2][e & 3]);
     mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * ScoreScale<HD>::v;
     const bool grow = mx > m_run + 8.0f;
     if (__any(grow)) {
       const float m_new = grow ? mx : m_run;
@@ -308,7 +382,9 @@ again:
     uint32_t pw[PP][4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float pa = exp2_hw(sv[2 * e] - m_use), pb = exp2_hw(sv[2 * e + 1] - m_use);
+      const int r = 2 * (e & 1);
+      const float pa = exp2_hw(fmaf(st[e >> 1][r], ScoreScale<HD>::v, -m_use));
+      const float pb = exp2_hw(fmaf(st[e >> 1][r + 1], ScoreScale<HD>::v, -m_use));
       l_run += pa + pb;
       uint32_t part[PP];
       split2<PP>(pa, pb, part);
@@ -317,10 +393,7 @@ again:
     }
     if constexpr (!MX) {
       // V, in order after which the next block's K was asked for
-      if (i + 1 < nb)
-        wait_copies<2 * KC>();
-      else
-        wait_copies<0>();
+      wait_copies<2 * KC>();
       if (pass == 1) {
         uint32_t found = 0;
 #pragma unroll 1
@@ -333,9 +406,10 @@ again:
         if (__any(found != 0)) bad |= 1ull << (i & 63);
       }
     }
+    const uint32_t vbase = fresh(vrow_at);
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
-      const char* at = vl + (vbase ^ (db << 5) ^ (MX ? mx_swz(db >> 1) << 4 : 0));
+      const char* at = lds + (vbase ^ (db << 5) ^ (MX ? mx_swz(db >> 1) << 4 : 0));
       const i16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4_t*)at);
       const i16x4_t hi =
           __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4_t*)(at + 16 * HD * 2));
@@ -346,10 +420,24 @@ again:
         o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
             vf, __builtin_bit_cast(bf16x8_t, make_uint4(pw[p][0], pw[p][1], pw[p][2], pw[p][3])), o[db], 0, 0, 0);
     }
+    // V operands kLead products ahead: all at once they would take the registers that K waits in
+    __builtin_amdgcn_sched_group_barrier(0x100, 2 * kLead, 0);
+#pragma unroll
+    for (int db = 0; db < DB - kLead; ++db) {
+      __builtin_amdgcn_sched_group_barrier(0x008, PP, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, PP * kLead, 0);
     if constexpr (!MX) {
       reads_done();
-      if (i + 1 < nb) load_v(i + 1);
+      load_v(kb1);
     }
+    kb = kb1;
+  };
+  if (!MX || pass == 0) {
+    for (int i = 0; i < nb; ++i) step(IC<0>{}, i);
+  } else {
+    for (int i = 0; i < nb; ++i) step(IC<1>{}, i);
   }
   if (pass == 0) {
     float x = 0.0f;
@@ -359,33 +447,7 @@ again:
       for (int e = 0; e < 4; ++e) x = fmaf(o[db][e], 0.0f, x);
     if (__any(hq < it.nr && x != 0.0f)) {
       pass = 1;
-      load_k(0);
-      load_v(0);
       goto again;
-    }
-  } else {
-    // the values that pass 1 took as 0, for the rows that see them
-#pragma unroll 1
-    for (int i = 0; i < nb; ++i) {
-      if ((bad >> (i & 63) & 1) == 0) continue;
-      const int kb = KB * (w + NW * i);
-#pragma unroll 1
-      for (int x = kb; x < min(kb + KB, it.n); ++x) {
-        const size_t r = row_at(x);
-        const bool see = x < mine.hi && (x < sink || x >= mine.lo);
-#pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          float v[4];
-          if constexpr (MX) {
-            v[0] = v[1] = v[2] = v[3] = a.vs[r * G + (db >> 1)] == 255 ? __uint_as_float(0x7fc00000u) : 0.0f;
-          } else {
-            const uint2 y = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(a.v) + r * HD + 16 * db + 4 * lg);
-            v[0] = bf_lo(y.x), v[1] = bf_hi(y.x), v[2] = bf_lo(y.y), v[3] = bf_hi(y.y);
-          }
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[db][e] += see && !(fabsf(v[e]) < INFINITY) ? v[e] : 0.0f;
-        }
-      }
     }
   }
   l_run += __shfl_xor(l_run, 16, 64);
@@ -393,6 +455,7 @@ again:
 
   // The waves' states into LDS (16-byte chunks permuted by the row), then merged in wave order:
   // the slot's state, or with one slot the output.
+  if constexpr (!MX) wait_copies<0>();
   __syncthreads();
   constexpr int CM = HD / 4 - 1;
   float* f = reinterpret_cast<float*>(&vbuf[0][0]);
@@ -400,6 +463,7 @@ again:
     ml[w][hq][0] = m_run;
     ml[w][hq][1] = l_run;
   }
+  if (lane == 0) bads[w] = bad;
 #pragma unroll
   for (int db = 0; db < DB; ++db)
     *reinterpret_cast<f32x4_t*>(f + (w * 16 + hq) * HD + 4 * ((4 * db + lg) ^ (hq & CM))) = o[db];
@@ -419,6 +483,31 @@ again:
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[e] = add_state(x[e], wt, y[e]);
       L = fmaf(wt, ml[v][h][1], L);
+    }
+    // the values that a second pass took as 0, where the row sees them
+#pragma unroll 1
+    for (int v = 0; v < NW; ++v) {
+      if (bads[v] == 0) continue;
+      const SinkRow see = seen_by(h);
+#pragma unroll 1
+      for (int k = 0; v + NW * k < blk.blocks; ++k) {
+        if ((bads[v] >> (k & 63) & 1) == 0) continue;
+        const auto kb = blk.at(v + NW * k);
+#pragma unroll 1
+        for (int y = kb.x; y < kb.end; ++y) {
+          if (!((y < see.hi) & ((y < sink) | (y >= see.lo)))) continue;
+          const size_t r = base + kb.row + (y - kb.x);
+          float z[4];
+          if constexpr (MX) {
+            z[0] = z[1] = z[2] = z[3] = a.vs[r * G + (c4 >> 3)] == 255 ? __uint_as_float(0x7fc00000u) : 0.0f;
+          } else {
+            const uint2 u = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(a.v) + r * HD + 4 * c4);
+            z[0] = bf_lo(u.x), z[1] = bf_hi(u.x), z[2] = bf_lo(u.y), z[3] = bf_hi(u.y);
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] += fabsf(z[e]) < INFINITY ? 0.0f : z[e];
+        }
+      }
     }
     if (it.slots == 1) {
       QT* dst = static_cast<QT*>(a.out) + sink_q(a, it.b, it.j, it.r0 + h, HD) + 4 * c4;
@@ -457,7 +546,7 @@ __global__ __launch_bounds__(256, 2) void sink_tile_kernel(SinkArgs a) {
   __shared__ __align__(1024) uint16_t buf0[2 * KT * HD], buf1[2 * KT * HD];
   const int lane = threadIdx.x & 63, w = wave_id(), hl = lane >> 5;
   SinkItem it;
-  if (!sink_item<kRowsTile>(a, (int)blockIdx.x, it)) return;
+  if (!sink_item<kRowsTile>(a, it)) return;
   const int nt = (it.n + KT - 1) / KT;
   const size_t base = ((size_t)it.b * a.n_kv + it.j) * a.t_cap + a.t_off;
 
@@ -598,7 +687,7 @@ again:
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int key = k0 + 32 * kh + 8 * (r >> 2) + 4 * hl + (r & 3);
-          st[kh][r] = key < mine.hi && (key < sink || key >= mine.lo) ? st[kh][r] : -INFINITY;
+          st[kh][r] = (key < mine.hi) & ((key < sink) | (key >= mine.lo)) ? st[kh][r] : -INFINITY;
         }
     }
     float mx = -INFINITY;
@@ -748,14 +837,14 @@ __global__ __launch_bounds__(256) void sink_f32_kernel(SinkArgs a) {
   __shared__ float ml[4][16][2];
   const int lane = threadIdx.x & 63, w = wave_id(), rq = lane & 15, lg = lane >> 4;
   SinkItem it;
-  if (!sink_item<kRowsWave>(a, (int)blockIdx.x, it)) return;
+  if (!sink_item<kRowsWave>(a, it)) return;
   const int nt = (it.n + 15) / 16;
   const size_t base = ((size_t)it.b * a.n_kv + it.j) * a.t_cap + a.t_off;
   const auto row_at = [&](int x) { return (base + it.keys.row(it.x0 + min(x, it.n - 1))) * HD; };
   const int sink = max(a.sink - it.x0, 0);
   SinkRow mine = sink_row_of(a, it.keys, it.p0 + token_of(a, it.r0 + min(rq, it.nr - 1)));
   mine = SinkRow{max(mine.lo, 0) - it.x0, min(mine.hi - it.x0, it.n)};
-  const auto sees = [&](int x) { return x < mine.hi && (x < sink || x >= mine.lo); };
+  const auto sees = [&](int x) { return (x < mine.hi) & ((x < sink) | (x >= mine.lo)); };
   const float* K = static_cast<const float*>(a.k);
   const float* V = static_cast<const float*>(a.v);
   f32x4_t q[KC];
@@ -1025,7 +1114,7 @@ static hipError_t launch_sink_t(const SinkArgs& a, hipStream_t st) {
   constexpr bool BF = sizeof(T) == 2;
   const bool mx = a.ks != nullptr, tile = BF && a.R > kRowsFew;
   const int RB = tile ? kRowsTile : kRowsWave;
-  const dim3 grid((unsigned)((long long)a.B * a.n_kv * ((a.R + RB - 1) / RB) * a.S));
+  const dim3 grid((unsigned)(a.B * a.n_kv), (unsigned)a.S, (unsigned)((a.R + RB - 1) / RB));
   if (tile) {
     if constexpr (BF) {
       if (mx)

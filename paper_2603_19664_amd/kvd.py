@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import dataclasses
+import functools
 import os
 import re
 from dataclasses import dataclass
@@ -174,6 +175,10 @@ class Shape:
     def c(self) -> AttnShape:
         return AttnShape(self.d_model, self.n_q_heads, self.n_kv_heads, self.head_dim, self.rms_eps,
                          self.rope_theta, self.dtype, self.w_layout)
+
+    @functools.cached_property
+    def _ref(self):
+        return ctypes.byref(self.c())
 
     def packed(self) -> "Shape":
         """The same shape with weights in the packed MFMA layout (kvd_pack_weights)."""
@@ -532,6 +537,17 @@ def _dev_ptr(t, name, dtype, dev):
     raise ValueError(f"{name} must be contiguous")
 
 
+def _arg(t, name, want, dtype, dev):
+    """t's pointer, once its extents, dtype, device (an index) and layout are checked."""
+    try:
+        if t.shape == want and t.dtype is dtype and t.get_device() == dev and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _dims(t, name, want)
+    return _dev_ptr(t, name, dtype, dev)
+
+
 def _device_of(t, name):
     if not t.is_cuda:
         raise ValueError(f"{name} must be a torch tensor on the GPU")
@@ -697,16 +713,20 @@ def _mx_view(cache, shape, B, dev):
         raise ValueError("cache.k must be a [B, n_kv, t_cap, head_dim / 2] tensor")
     n_kv, hd, t_cap, u8 = shape.n_kv_heads, shape.head_dim, k.shape[2], torch.uint8
     codes, scales = (B, n_kv, t_cap, hd // 2), (B, n_kv, t_cap, hd // 32)
-    _dims(k, "cache.k", codes)
-    _dims(v, "cache.v", codes)
-    _dims(ks, "cache.k_scale", scales)
-    _dims(vs, "cache.v_scale", scales)
-    return MxView(_dev_ptr(k, "cache.k", u8, dev), _dev_ptr(v, "cache.v", u8, dev),
-                  _dev_ptr(ks, "cache.k_scale", u8, dev), _dev_ptr(vs, "cache.v_scale", u8, dev), t_cap, t_off)
+    return MxView(_arg(k, "cache.k", codes, u8, dev), _arg(v, "cache.v", codes, u8, dev),
+                  _arg(ks, "cache.k_scale", scales, u8, dev), _arg(vs, "cache.v_scale", scales, u8, dev), t_cap, t_off)
 
 
-def _sink_call(fn, shape, q, view, T, window, sink, out, ws, kv_len, n_new):
-    # q's extents first; view(B, dev) checks the keys
+def _kv_view(k, v, t_off, shape, B, dev):
+    if k is None or v is None:
+        raise ValueError("kv: k and v are required")
+    if not isinstance(k, torch.Tensor) or k.dim() != 4:
+        raise ValueError("kv: k and v must both be [B, n_kv, t_cap, head_dim] tensors")
+    want, dt = (B, shape.n_kv_heads, k.shape[2], shape.head_dim), shape.torch_dtype
+    return KvView(_arg(k, "kv_k", want, dt, dev), _arg(v, "kv_v", want, dt, dev), want[2], t_off)
+
+
+def _sink_call(fn, view, keys, shape, q, T, window, sink, out, ws, kv_len, n_new):
     if not isinstance(q, torch.Tensor) or q.dim() not in (3, 4):
         raise ValueError("q must be a [B, N, n_q, head_dim] or [B, n_q, head_dim] tensor")
     dims = q.shape
@@ -715,17 +735,18 @@ def _sink_call(fn, shape, q, view, T, window, sink, out, ws, kv_len, n_new):
         raise ValueError(f"q has shape {tuple(dims)}, expected [.., {shape.n_q_heads}, {shape.head_dim}]")
     if out is None:
         raise ValueError("out is required")
-    _dims(out, "out", dims)
-    if kv_len is not None:
-        _dims(kv_len, "kv_len", (B,))
-    if n_new is not None:
-        _dims(n_new, "n_new", (B,))
     if not isinstance(ws, torch.Tensor):
         raise ValueError("ws must be a torch tensor")
-    dt, dev, i32 = shape.torch_dtype, _device_of(q, "q"), torch.int32
-    _run_on(dev, fn, ctypes.byref(shape.c()), _dev_ptr(q, "q", dt, dev), N, ctypes.byref(view(B, dev)),
-            _dev_ptr(kv_len, "kv_len", i32, dev), _dev_ptr(n_new, "n_new", i32, dev), B, T, window, sink,
-            _dev_ptr(out, "out", dt, dev), _dev_ptr(ws, "ws", ws.dtype, dev), ws.nbytes)
+    dt, dev, i32 = shape.torch_dtype, q.get_device(), torch.int32
+    if dev < 0:
+        for t, name, want in ((out, "out", dims), (kv_len, "kv_len", (B,)), (n_new, "n_new", (B,))):
+            if t is not None:
+                _dims(t, name, want)
+        _device_of(q, "q")
+    _run_on(dev, fn, shape._ref, _arg(q, "q", dims, dt, dev), N, ctypes.byref(view(*keys, shape, B, dev)),
+            None if kv_len is None else _arg(kv_len, "kv_len", (B,), i32, dev),
+            None if n_new is None else _arg(n_new, "n_new", (B,), i32, dev), B, T, window, sink,
+            _arg(out, "out", dims, dt, dev), _dev_ptr(ws, "ws", ws.dtype, dev), ws.nbytes)
 
 
 def kvd_sink_attn(shape: Shape, q, k, v, T: int, window: int, out, ws, sink: int = 0, kv_len=None, n_new=None,
@@ -734,39 +755,32 @@ def kvd_sink_attn(shape: Shape, q, k, v, T: int, window: int, out, ws, sink: int
     (T if None) tokens, over the first `sink` tokens and the newest `window` of each new one.  Rows t_off.. of k / v
     [B, n_kv, t_cap, hd] hold the tokens in order if T fit, else the first `sink` and behind them a ring of the
     others (t_cap - t_off - sink >= window + N - 1 rows).  Runs on the tensors' device and its current stream."""
-    def view(B, dev):
-        if k is None or v is None:
-            raise ValueError("kv: k and v are required")
-        if not isinstance(k, torch.Tensor) or k.dim() != 4:
-            raise ValueError("kv: k and v must both be [B, n_kv, t_cap, head_dim] tensors")
-        want = (B, shape.n_kv_heads, k.shape[2], shape.head_dim)
-        _dims(k, "kv_k", want)
-        _dims(v, "kv_v", want)
-        dt = shape.torch_dtype
-        return KvView(_dev_ptr(k, "kv_k", dt, dev), _dev_ptr(v, "kv_v", dt, dev), want[2], t_off)
-    _sink_call(lib.kvd_sink_attn, shape, q, view, T, window, sink, out, ws, kv_len, n_new)
+    _sink_call(lib.kvd_sink_attn, _kv_view, (k, v, t_off), shape, q, T, window, sink, out, ws, kv_len, n_new)
 
 
 def kvd_mx_attn(shape: Shape, q, cache: MxCache, T: int, out, ws, window: int = None, sink: int = 0, kv_len=None,
                 n_new=None):
     """kvd_sink_attn over a 4-bit cache (window None: every token)."""
-    _sink_call(lib.kvd_mx_attn, shape, q, lambda B, dev: _mx_view(cache, shape, B, dev), T,
-               max(T, 1) if window is None else window, sink, out, ws, kv_len, n_new)
+    _sink_call(lib.kvd_mx_attn, _mx_view, (cache,), shape, q, T, max(T, 1) if window is None else window, sink, out, ws,
+               kv_len, n_new)
 
 
 def _mx_rows(shape, k, v, N, cache, T, t_off, kv_len, n_new):
     if not isinstance(k, torch.Tensor) or k.dim() != 4:
         raise ValueError("rows: k and v must both be [B, n_kv, t_cap, head_dim] tensors")
-    B = k.shape[0]
-    t_cap = _own_dims(k, v, "rows", B, shape, N, t_off)
-    if kv_len is not None:
-        _dims(kv_len, "kv_len", (B,))
-    if n_new is not None:
-        _dims(n_new, "n_new", (B,))
-    dt, dev, i32 = shape.torch_dtype, _device_of(k, "rows_k"), torch.int32
-    rows = KvView(_dev_ptr(k, "rows_k", dt, dev), _dev_ptr(v, "rows_v", dt, dev), t_cap, t_off)
-    return (dev, ctypes.byref(shape.c()), ctypes.byref(rows), ctypes.byref(_mx_view(cache, shape, B, dev)),
-            _dev_ptr(kv_len, "kv_len", i32, dev), _dev_ptr(n_new, "n_new", i32, dev), B)
+    dims = k.shape
+    B, t_cap, dt, dev, i32 = dims[0], dims[2], shape.torch_dtype, k.get_device(), torch.int32
+    want = (B, shape.n_kv_heads, t_cap, shape.head_dim)
+    if dev < 0 or v is None or t_off < 0 or t_off + N > t_cap:
+        _own_dims(k, v, "rows", B, shape, N, t_off)
+        for t, name in ((kv_len, "kv_len"), (n_new, "n_new")):
+            if t is not None:
+                _dims(t, name, (B,))
+        _device_of(k, "rows_k")
+    rows = KvView(_arg(k, "rows_k", want, dt, dev), _arg(v, "rows_v", want, dt, dev), t_cap, t_off)
+    return (dev, shape._ref, ctypes.byref(rows), ctypes.byref(_mx_view(cache, shape, B, dev)),
+            None if kv_len is None else _arg(kv_len, "kv_len", (B,), i32, dev),
+            None if n_new is None else _arg(n_new, "n_new", (B,), i32, dev), B)
 
 
 def kvd_mx_store(shape: Shape, k, v, N: int, cache: MxCache, T: int, sink: int = 0, kv_len=None, n_new=None,
