@@ -1256,10 +1256,14 @@ bool sink_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T, int32_t
   // up to three times while a slot keeps 512 keys (8 x 32768 keys 59 -> 57 us, 64 x 4096 .. 8192 keys 32.2 -> 30.2; 16
   // drafts over 2056 keys in 8 slots instead of 4 14.8 -> 18.6).  Blocks that windows limit are of one size.  The
   // workspace has room for the slots of a causal call, which has most, and falls with no length.
+  // Up to 256 keys, 512 of few rows whose K is short, are one slot: one launch (384 keys in 4 bits: 6.7 to 9.1 us over
+  // the head dims, 8.8 to 10.1 in two; bf16 at head_dim 256: 11.8, 10.9).
+  const bool brief = few && (mx || s->head_dim * (int)elem_size(s) <= 256);
+  const long long small = brief ? 2 * kvd::kRowsSmall : kvd::kRowsSmall;
   int32_t S = 1;
   p->S = 1;
-  p->C = kvd::kRowsSmall;
-  if (keys > kvd::kRowsSmall) {
+  p->C = (int32_t)small;
+  if (keys > small) {
     const long long u = units * nb, wgs = few ? 256 : kvd::kRowsTargetWgs;
     const auto slots = [&](bool causal) {
       int32_t n = causal ? causal_slots(u, rows, (int32_t)keys, few, N, false, wgs)
@@ -1282,8 +1286,7 @@ bool sink_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T, int32_t
   p->ml = take(S > 1 ? 8 * (size_t)S * rows : 0);
   p->acc = take(S > 1 ? 4 * (size_t)S * rows * s->head_dim : 0);
   p->end = std::max<size_t>(at, 256);
-  const int per_wg = 4 / kvd::rows_finish_waves(S);
-  return std::max(units * nb * p->S, (rows + per_wg - 1) / per_wg) <= kvd::most_wgs(256);
+  return std::max(units * nb * p->S, rows) <= kvd::most_wgs(512);
 }
 
 kvd_status sink_sizes(int32_t B, int32_t N, int32_t T, int32_t window, int32_t sink) {

@@ -30,6 +30,7 @@ struct SinkItem {
 __device__ __forceinline__ int sink_slots(const SinkArgs& a, const SinkKeys& k) {
   return max((int)(((uint32_t)k.n + (uint32_t)a.C - 1u) / (uint32_t)a.C), 1);
 }
+
 // Grid: B n_kv (sequence, KV head), slots, blocks.  False where the workgroup has nothing to do.
 template <int RB>
 __device__ __forceinline__ bool sink_item(const SinkArgs& a, SinkItem& it) {
@@ -537,13 +538,17 @@ again:
 // tiles; the products, the running maximum and the two parts of a weight as in rows_tile
 // (kvd_rows.hip).  Plain K and V are copied straight into the other LDS buffer while a tile is
 // computed; the rows of a tile that the sinks' or the ring's end cuts are copied one by one.  4 bits: the
-// next tile's numbers wait in registers and become bf16 in LDS once for the 128 rows.  A
+// next tile's numbers wait as they are and become bf16 in LDS once for the 128 rows.  A
 // wave skips the tiles that none of its rows sees.
 template <int HD, bool MX>
 __global__ __launch_bounds__(256, 2) void sink_tile_kernel(SinkArgs a) {
   constexpr int KT = rows_kt(HD), KH = KT / 32, KS = HD / 16, DB = HD / 32, kLead = 4;
   constexpr int G = HD / kMxGroup, NC = KT * G >= 256 ? KT * G / 256 : 1;  // groups of a row; groups a thread brings
   __shared__ __align__(1024) uint16_t buf0[2 * KT * HD], buf1[2 * KT * HD];
+  // Where a thread's own groups of the next tile wait: head_dim 256 has no registers for them (63 us so, 52 through LDS:
+  // 2 x 256 tokens over 4000 keys), the others no time to spare (8 x 256 tokens over 8448 keys: 160, 176).
+  constexpr bool RAW = MX && HD == 256;
+  __shared__ __align__(1024) u32x4_t raw[RAW ? 2 * 256 * NC : 1];
   const int lane = threadIdx.x & 63, w = wave_id(), hl = lane >> 5;
   SinkItem it;
   if (!sink_item<kRowsTile>(a, it)) return;
@@ -592,29 +597,42 @@ __global__ __launch_bounds__(256, 2) void sink_tile_kernel(SinkArgs a) {
           (__attribute__((address_space(3))) void*)(buf + KT * HD + 512 * w + 2048 * i), 16, 0, 0);
     }
   };
-  // 4 bits: tile t into registers, and from there into buf
-  u32x4_t kc[NC], vc[NC];
-  uint32_t kb[NC], vb[NC];
+  // 4 bits: tile t's numbers on their way, and from there into buf
+  u32x4_t kc[RAW ? 1 : NC], vc[RAW ? 1 : NC];
+  uint8_t kb[NC], vb[NC];
   auto fetch = [&](int t) {
     const int k0 = it.x0 + KT * t, n = it.n - KT * t;
+    const int tid = (int)fresh(threadIdx.x);
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
-      const int id = (int)threadIdx.x + 256 * i, r = id / G, g = id % G;
+      const int id = tid + 256 * i, r = id / G, g = id % G;
       if (KT * G < 256 && r >= KT) break;
       const size_t row = base + it.keys.row(k0 + min(r, n - 1));
-      kc[i] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint8_t*>(a.k) + row * (HD / 2) + 16 * g);
-      vc[i] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint8_t*>(a.v) + row * (HD / 2) + 16 * g);
+      const uint8_t* ksrc = static_cast<const uint8_t*>(a.k) + row * (HD / 2) + 16 * g;
+      const uint8_t* vsrc = static_cast<const uint8_t*>(a.v) + row * (HD / 2) + 16 * g;
+      if constexpr (RAW) {
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)ksrc,
+                                         (__attribute__((address_space(3))) void*)(raw + 256 * i + 64 * w), 16, 0, 0);
+        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)vsrc,
+                                         (__attribute__((address_space(3))) void*)(raw + 256 * (NC + i) + 64 * w), 16, 0, 0);
+      } else {
+        kc[i] = *reinterpret_cast<const u32x4_t*>(ksrc);
+        vc[i] = *reinterpret_cast<const u32x4_t*>(vsrc);
+      }
       kb[i] = a.ks[row * G + g];
       vb[i] = a.vs[row * G + g];
     }
   };
   auto put = [&](uint16_t* buf) {
+    if constexpr (RAW) wait_copies<0>();
+    const int tid = (int)fresh(threadIdx.x);
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
-      const int id = (int)threadIdx.x + 256 * i, r = id / G, g = id % G;
+      const int id = tid + 256 * i, r = id / G, g = id % G;
       if (KT * G < 256 && r >= KT) break;
-      mx_put(kc[i], mx_scale(kb[i]), reinterpret_cast<char*>(buf) + r * HD * 2, g, score_swz<HD>(r));
-      mx_put(vc[i], mx_scale(vb[i]), reinterpret_cast<char*>(buf + KT * HD) + r * HD * 2, g, v_swz<HD>(r));
+      mx_put(RAW ? raw[id] : kc[RAW ? 0 : i], mx_scale(kb[i]), reinterpret_cast<char*>(buf) + r * HD * 2, g, score_swz<HD>(r));
+      mx_put(RAW ? raw[256 * NC + id] : vc[RAW ? 0 : i], mx_scale(vb[i]), reinterpret_cast<char*>(buf + KT * HD) + r * HD * 2, g,
+             v_swz<HD>(r));
     }
   };
 
@@ -828,13 +846,14 @@ again:
 
 // ------------------------------------------------------------------ fp32 K/V
 
-// One workgroup of 4 waves per (16-row block, slot), 16-key blocks to the waves in turn; the
+// One workgroup per (16-row block, slot), 16-key blocks to the waves in turn; the
 // products, lanes and infinities as in rows_f32_kernel (kvd_rows.hip).
+constexpr int sink_f32_waves(int hd) { return hd == 64 ? 8 : 4; }  // (8 do not leave the registers for longer rows)
 template <int HD>
-__global__ __launch_bounds__(256) void sink_f32_kernel(SinkArgs a) {
-  constexpr int KC = HD / 16, VU = HD / 64;
-  __shared__ __align__(16) float part[3][16][HD + 4];
-  __shared__ float ml[4][16][2];
+__global__ __launch_bounds__(64 * sink_f32_waves(HD)) void sink_f32_kernel(SinkArgs a) {
+  constexpr int NW = sink_f32_waves(HD), KC = HD / 16, VU = HD / 64;
+  __shared__ __align__(16) float part[NW - 1][16][HD + 4];
+  __shared__ float ml[NW][16][2];
   const int lane = threadIdx.x & 63, w = wave_id(), rq = lane & 15, lg = lane >> 4;
   SinkItem it;
   if (!sink_item<kRowsWave>(a, it)) return;
@@ -863,7 +882,7 @@ again:
     for (int e = 0; e < 4; ++e) o[u][e] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
   m_run = -INFINITY;
   l_run = 0.0f;
-  for (int t = w; t < nt; t += 4) {
+  for (int t = w; t < nt; t += NW) {
     const int k0 = 16 * t;
     f32x4_t kf[KC], vf[4][VU];
     const float* ks = K + row_at(k0 + rq) + 4 * lg;
@@ -935,7 +954,7 @@ again:
   } else {
     // the values that pass 1 took as 0, for the rows that see them
 #pragma unroll 1
-    for (int t = w; t < nt; t += 4) {
+    for (int t = w; t < nt; t += NW) {
       const int k0 = 16 * t;
 #pragma unroll
       for (int u = 0; u < VU; ++u) {
@@ -980,7 +999,7 @@ again:
   if (w > 0 || rq >= it.nr) return;
   float M = m_run;
 #pragma unroll
-  for (int v = 1; v < 4; ++v) M = fmaxf(M, ml[v][rq][0]);
+  for (int v = 1; v < NW; ++v) M = fmaxf(M, ml[v][rq][0]);
   const float Mu = M == -INFINITY ? 0.0f : M;
   const float w0 = exp2_hw(m_run - Mu);
   l_run *= w0;
@@ -991,7 +1010,7 @@ again:
 #pragma unroll
       for (int r = 0; r < 4; ++r) o[u][e][r] = add_state(0.0f, w0, o[u][e][r]);
 #pragma unroll
-  for (int v = 1; v < 4; ++v) {
+  for (int v = 1; v < NW; ++v) {
     const float wt = exp2_hw(ml[v][rq][0] - Mu);
     l_run = fmaf(wt, ml[v][rq][1], l_run);
 #pragma unroll
@@ -1026,17 +1045,74 @@ again:
 
 // ------------------------------------------------------------------ merge
 
-// A row's states, by WPR waves (each every WPR-th state, 8 in flight): lane s takes the (max, sum) of
-// state s.  RB: rows of the attention's blocks, which know how many slots they have.
-template <typename T, int HD, int RB, int WPR>
+// Rows of up to 8 states, or many rows: a thread takes 4 elements of a row, its states 8 at a time in flight.
+// Bound by the states' traffic.  RB: rows of the attention's blocks, which know how many slots they have.
+template <typename T, int HD, int RB>
+__global__ __launch_bounds__(256) void sink_merge_kernel(SinkArgs a) {
+  constexpr int TPR = HD / 4;
+  const long long idx = (long long)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+  const int c = 4 * (threadIdx.x % TPR);
+  const int u = (int)(idx / a.R), r = (int)(idx - (long long)u * a.R);  // neighbours' states lie side by side
+  if (u >= a.B * a.n_kv) return;
+  const int j = u / a.B, b = u - j * a.B;
+  const SinkSeq sq = sink_seq(a.kv_len, a.n_new, a.T, a.N, b);
+  const int rows = sq.n * a.g;
+  if (r >= rows) return;
+  const int r0 = r / RB * RB, p0 = sq.len - sq.n;
+  const int S = sink_slots(a, sink_keys(a, p0 + token_of(a, r0), p0 + token_of(a, min(r0 + RB, rows) - 1)));
+  if (S == 1) return;
+  const size_t step = (size_t)a.n_kv * a.B * a.R, first = sink_state(a, 0, b, j, r);
+  const float2* st = reinterpret_cast<const float2*>(a.ml) + first;
+  const float* acc = a.acc + first * HD + c;
+  float M = -INFINITY, L = 0.0f;
+  f32x4_t x = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int s0 = 0; s0 < S; s0 += 8) {
+    float2 ml[8];
+    f32x4_t y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      ml[i] = make_float2(-INFINITY, 0.0f);
+      if (s0 + i < S) ml[i] = st[(s0 + i) * step];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (s0 + i < S) y[i] = *reinterpret_cast<const f32x4_t*>(acc + (s0 + i) * step * HD);
+    float m = M;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (ml[i].y != 0.0f) m = fmaxf(m, ml[i].x);
+    const float mu = m == -INFINITY ? 0.0f : m, old = exp2_hw(M - mu);
+    M = m;
+    L *= old;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = add_state(0.0f, old, x[e]);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (ml[i].y == 0.0f) continue;  // an empty state has no acc
+      const float wt = exp2_hw(ml[i].x - mu);
+      L = fmaf(wt, ml[i].y, L);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = add_state(x[e], wt, y[i][e]);
+    }
+  }
+  T* dst = static_cast<T*>(a.out) + sink_q(a, b, j, r, HD) + c;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] = L != 0.0f ? x[e] / L : 0.0f;
+  if constexpr (sizeof(T) == 2)
+    *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+  else
+    *reinterpret_cast<f32x4_t*>(dst) = x;
+}
+
+// Few rows of many states: a row by 4 waves (each every 4th state, 8 in flight), lane s taking the
+// (max, sum) of state s.
+template <typename T, int HD, int RB>
 __global__ __launch_bounds__(256) void sink_finish_kernel(SinkArgs a) {
-  constexpr int E = HD / 64;
-  __shared__ float part[WPR > 1 ? WPR : 1][HD];
+  constexpr int E = HD / 64, WPR = 4;
+  __shared__ float part[WPR][HD];
   const int lane = threadIdx.x & 63, w = wave_id();
-  const long long idx = (long long)blockIdx.x * (4 / WPR) + w / WPR;
-  const int units = a.B * a.n_kv;
-  const int r = (int)(idx / units), u = (int)(idx - (long long)r * units), j = u % a.n_kv, b = u / a.n_kv;
-  if (r >= a.R) return;  // (4 waves to a row: of one row)
+  const int units = a.B * a.n_kv, r = (int)(blockIdx.x / (uint32_t)units), u = (int)blockIdx.x - r * units;
+  const int j = u % a.n_kv, b = u / a.n_kv;
   const SinkSeq sq = sink_seq(a.kv_len, a.n_new, a.T, a.N, b);
   const int rows = sq.n * a.g;
   if (r >= rows) return;
@@ -1081,17 +1157,15 @@ __global__ __launch_bounds__(256) void sink_finish_kernel(SinkArgs a) {
 #pragma unroll
       for (int e = 0; e < E; ++e) x[e] = i >= n ? x[e] : add_state(x[e], ws[i], y[i][e]);
   }
-  if constexpr (WPR > 1) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) part[w][E * lane + e] = x[e];
-    __syncthreads();
-    if (w > 0) return;
+  for (int e = 0; e < E; ++e) part[w][E * lane + e] = x[e];
+  __syncthreads();
+  if (w > 0) return;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      x[e] = part[0][E * lane + e];
+  for (int e = 0; e < E; ++e) {
+    x[e] = part[0][E * lane + e];
 #pragma unroll
-      for (int v = 1; v < WPR; ++v) x[e] += part[v][E * lane + e];
-    }
+    for (int v = 1; v < WPR; ++v) x[e] += part[v][E * lane + e];
   }
   T* dst = static_cast<T*>(a.out) + sink_q(a, b, j, r, HD) + E * lane;
 #pragma unroll
@@ -1108,6 +1182,8 @@ __global__ __launch_bounds__(256) void sink_finish_kernel(SinkArgs a) {
 }
 
 // ------------------------------------------------------------------ launchers
+
+constexpr long long kSinkManyRows = 2048;
 
 template <typename T, int HD>
 static hipError_t launch_sink_t(const SinkArgs& a, hipStream_t st) {
@@ -1128,18 +1204,17 @@ static hipError_t launch_sink_t(const SinkArgs& a, hipStream_t st) {
     if constexpr (BF)
       hipLaunchKernelGGL((sink_few_kernel<HD, false, T>), grid, dim3(256), 0, st, a);
     else
-      hipLaunchKernelGGL(sink_f32_kernel<HD>, grid, dim3(256), 0, st, a);
+      hipLaunchKernelGGL(sink_f32_kernel<HD>, grid, dim3(64 * sink_f32_waves(HD)), 0, st, a);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.S == 1) return e;
-  const int per = 4 / rows_finish_waves(a.S);  // merged rows per workgroup
-  const dim3 merge((unsigned)(((long long)a.B * a.n_kv * a.R + per - 1) / per));
+  const long long rows = (long long)a.B * a.n_kv * a.R;
   const auto finish = [&](auto rb) {
-    constexpr int B_ = decltype(rb)::value;
-    if (per == 1)
-      hipLaunchKernelGGL((sink_finish_kernel<T, HD, B_, 4>), merge, dim3(256), 0, st, a);
+    constexpr int RB_ = decltype(rb)::value, per = 256 / (HD / 4);
+    if (a.S > 8 && rows < kSinkManyRows)
+      hipLaunchKernelGGL((sink_finish_kernel<T, HD, RB_>), dim3((unsigned)rows), dim3(256), 0, st, a);
     else
-      hipLaunchKernelGGL((sink_finish_kernel<T, HD, B_, 1>), merge, dim3(256), 0, st, a);
+      hipLaunchKernelGGL((sink_merge_kernel<T, HD, RB_>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, st, a);
   };
   if (tile)
     finish(IC<kRowsTile>{});
