@@ -602,7 +602,7 @@ __global__ __launch_bounds__(256, 2) void sink_tile_kernel(SinkArgs a) {
   uint8_t kb[NC], vb[NC];
   auto fetch = [&](int t) {
     const int k0 = it.x0 + KT * t, n = it.n - KT * t;
-    const int tid = (int)fresh(threadIdx.x);
+    const int tid = RAW ? (int)fresh(threadIdx.x) : (int)threadIdx.x;
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
       const int id = tid + 256 * i, r = id / G, g = id % G;
@@ -625,7 +625,7 @@ __global__ __launch_bounds__(256, 2) void sink_tile_kernel(SinkArgs a) {
   };
   auto put = [&](uint16_t* buf) {
     if constexpr (RAW) wait_copies<0>();
-    const int tid = (int)fresh(threadIdx.x);
+    const int tid = RAW ? (int)fresh(threadIdx.x) : (int)threadIdx.x;
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
       const int id = tid + 256 * i, r = id / G, g = id % G;
