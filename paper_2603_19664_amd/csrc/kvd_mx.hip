@@ -23,16 +23,16 @@ struct MxItem {
 };
 template <int HD>
 __device__ __forceinline__ MxItem mx_item(const MxArgs& a) {
-  constexpr int CPR = HD / 8;
-  const long long id = (long long)blockIdx.x * 256 + threadIdx.x;
+  constexpr uint32_t CPR = HD / 8;
+  const uint32_t id = blockIdx.x * 256u + threadIdx.x;  // (a call has fewer than 2^31)
   MxItem it;
   it.c = (int)(id % CPR);
-  const long long row = id / CPR;  // (b n_kv + j) N + i
-  const long long bj = row / a.N;
-  const int i = (int)(row - bj * a.N);
-  it.on = bj < (long long)a.B * a.n_kv;
+  const uint32_t row = id / CPR;  // (b n_kv + j) N + i
+  const uint32_t bj = row / (uint32_t)a.N;
+  const int i = (int)(row - bj * (uint32_t)a.N);
+  it.on = bj < (uint32_t)a.B * (uint32_t)a.n_kv;
   if (!it.on) return it;
-  const SinkSeq s = sink_seq(a.kv_len, a.n_new, a.T, a.N, (int)(bj / a.n_kv));
+  const SinkSeq s = sink_seq(a.kv_len, a.n_new, a.T, a.N, (int)(bj / (uint32_t)a.n_kv));
   const int t = s.len - s.n + i;
   it.on = i < s.n && t >= 0;
   if (!it.on) return it;
