@@ -481,8 +481,7 @@ again:
     for (int v = 0; v < NW; ++v) {
       const float wt = exp2_hw(ml[v][h][0] - Mu);
       const f32x4_t y = *reinterpret_cast<const f32x4_t*>(f + (v * 16 + h) * HD + 4 * (c4 ^ (h & CM)));
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = add_state(x[e], wt, y[e]);
+      x += wt * y;  // (a second pass has left no infinity in a state)
       L = fmaf(wt, ml[v][h][1], L);
     }
     // the values that a second pass took as 0, where the row sees them

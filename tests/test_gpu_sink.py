@@ -1,6 +1,8 @@
 """kvd_sink_attn and kvd_mx_attn against the 64-bit oracle, element by element, on caches whose unused rows are NaN.
 
 Bounds come from the arithmetic (sink_cases.bound) before any run."""
+import random
+
 import pytest
 import torch
 
@@ -321,3 +323,64 @@ def test_offsets_beyond_32_bits(mx, ring):
         if not ring:
             assert torch.equal(a, call(s, x["q"], c, 400, window, sink))
         del big, kv
+
+
+@pytest.mark.parametrize("seed", range(48))
+def test_calls_of_many_shapes(seed):
+    # single tokens, drafts and prompts of both formats: whole caches, windows and rings, ragged or not
+    rng = random.Random(seed)
+    hd, n_q, n_kv = rng.choice(HEADS)
+    B, N = rng.choice([(1, 1), (3, 1), (7, 1), (2, 2), (1, 5), (2, 17), (1, 64), (1, 129)])
+    window, sink = rng.choice([1, 7, 32, 64, 100, 513]), rng.choice([0, 1, 4, 31, 33, 64])
+    T = N + rng.choice([0, 1, 31, 200, 777])
+    slots = None
+    if rng.random() < 0.4:
+        slots = sink + window + N - 1 + rng.choice([0, 1, 32])
+        T = slots + rng.randint(1, 600)
+    lens = news = None
+    if rng.random() < 0.6:
+        lens = [rng.randint(0, T) for _ in range(B)]
+        news = [rng.randint(0, N) for _ in range(B)]
+    run(rng.choice(["bf16", "f32"]), n_q, n_kv, hd, B, N, T, window, sink, rng.random() < 0.5, lens, news, slots, seed,
+        rng.choice([0, 2]))
+
+
+def test_the_binding_refuses_what_the_kernels_would_misread():
+    s = shape("bf16", 4, 2, 64)
+    x = tokens("bf16", 4, 2, 64, 2, 3, 20, 1)
+    q, k, v = x["q"], x["k"], x["v"]
+    c = kvd.mx_cache(s, 2, 20)
+    out, ws = torch.empty_like(q), torch.empty(4096, dtype=torch.uint8, device="cuda")
+    lens = i32([20, 20])
+
+    def no(match, fn, *a, **kw):
+        with pytest.raises(ValueError, match=match):
+            fn(s, *a, **kw)
+    f = kvd.kvd_sink_attn
+    no("q has dtype", f, q.float(), k, v, 20, 8, out, ws)
+    no("out must be contiguous", f, q, k, v, 20, 8, torch.empty((2, 3, 64, 4), dtype=q.dtype, device="cuda").transpose(2, 3), ws)
+    no("out is on|on the GPU", f, q, k, v, 20, 8, out.cpu(), ws)
+    no("kv_k has dtype", f, q, k.float(), v.float(), 20, 8, out, ws)
+    no("kv_v has shape", f, q, k, v[:, :, :19], 20, 8, out, ws)
+    no("kv_k must be contiguous", f, q, k.transpose(2, 3).contiguous().transpose(2, 3), v, 20, 8, out, ws)
+    no("k and v are required", f, q, k, None, 20, 8, out, ws)
+    no("kv_len has dtype", f, q, k, v, 20, 8, out, ws, kv_len=lens.long())
+    no("n_new has shape", f, q, k, v, 20, 8, out, ws, n_new=i32([1]))
+    no("ws must be|on the GPU", f, q, k, v, 20, 8, out, ws.cpu())
+    g = kvd.kvd_mx_attn
+    no("cache.k has dtype", g, q, c._replace(k=c.k.char()), 20, out, ws)
+    no("cache.v_scale has shape", g, q, c._replace(v_scale=c.k_scale[..., :1]), 20, out, ws)
+    no("cache.k_scale is on|on the GPU", g, q, c._replace(k_scale=c.k_scale.cpu()), 20, out, ws)
+    no("cache.k must be a", g, q, c._replace(k=None), 20, out, ws)
+    no("cache.v must be a", g, q, c._replace(v=None), 20, out, ws)
+    r = kvd.kvd_mx_store
+    no("rows_k has dtype", r, k.float(), v.float(), 20, c, 20)
+    no("rows: rows", r, k, v, 21, c, 20)
+    no("k and v are required", r, k, None, 20, c, 20)
+    for bad in (dict(T=21, window=18, N=3), dict(T=21, window=20, N=1)):
+        with pytest.raises(kvd.KvdError) as e:   # a ring that is too short
+            f(s, q[:, :bad["N"]].contiguous(), k, v, bad["T"], bad["window"], out[:, :bad["N"]].contiguous(), ws, sink=1)
+        assert e.value.status == kvd.KVD_ERR_SHAPE
+    with pytest.raises(kvd.KvdError) as e:
+        f(s, q, k, v, 20, 8, out, ws[:0])
+    assert e.value.status == kvd.KVD_ERR_WORKSPACE
