@@ -8,7 +8,8 @@
 // 4-bit form, whatever computes it.
 //
 // HBM-bound: a thread takes 8 elements (16 or 32 bytes) of one row, the four of a group of 32
-// find its largest between them.
+// find its largest between them.  (6503 rows of 4 heads of 256, K and V: 10 us to store, 9.6 to load, 3.4 to
+// 3.5 TB/s; 32 rows of 2 heads of 128: 2.8 and 2.6 us, launch and round trip.)
 #include <hip/hip_runtime.h>
 
 #include "kvd_sink_device.hpp"

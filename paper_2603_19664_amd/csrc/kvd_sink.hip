@@ -5,7 +5,8 @@
 //                       its own (bf16: single tokens and short drafts; 4 bits with fp32 queries: every call).
 //   sink_tile_kernel    bf16: 128 rows per workgroup that share key tiles in LDS.
 //   sink_f32_kernel     fp32 K/V: blocks of 16 rows, both products on MFMA 16x16x4 f32.
-//   sink_finish_kernel  merges the key ranges' softmax states into out.
+//   sink_merge_kernel, sink_finish_kernel
+//                       merge the slots' softmax states into out.
 //
 // Rows.  The rows of (sequence b, KV head j) are (token i, head h of the group), r = i g + h.
 // A block of them sees the keys x = 0 .. n - 1 that sink_keys names, in slots of C; slot s
@@ -169,6 +170,10 @@ __device__ __forceinline__ void split2_trunc(float x, float y, uint32_t (&w)[P])
 // (two for bf16 queries: 2^-17 of a weight is lost; three for fp32), V through LDS: plain by direct copies,
 // 4 bits as the bf16 numbers that they are (one instruction for two), read transposed.
 // K of the next block is asked for when the scores are taken, V after its product.
+// Measured (several caches in turn, so that HBM is read): 64 streams of 1028 bf16 rows, 4 KV heads of 256, 48.6 us,
+// 5.5 TB/s; in 4 bits 8 x 32768 rows of them 57 us, 5.0 TB/s; 64 x 4096 .. 8192 rows of 2 heads of 128 27 us, 3.9 TB/s:
+// half the bytes to a block's fixed work, waves waiting for memory 44% of their time.  (Two blocks of these on
+// their way, 204 registers: 37 us.)  A call of few keys takes 5 us, at head_dim 256 7 to 8, most of it instructions.
 // Workgroups per CU that the registers are to leave room for.
 constexpr int few_wgs(int hd, bool mx, bool bf) {
   return hd == 256 ? (bf ? 2 : 1) : hd == 128 ? 3 : 4;
@@ -539,6 +544,10 @@ again:
 // computed; the rows of a tile that the sinks' or the ring's end cuts are copied one by one.  4 bits: the
 // next tile's numbers wait as they are and become bf16 in LDS once for the 128 rows.  A
 // wave skips the tiles that none of its rows sees.
+// Measured: 8192 tokens, window 1024, 8 heads of 256: 117 us, 0.55 PFLOP/s of the formula's flops, 0.83 of products
+// (a large matrix product reaches 1.17); MFMA is busy in half of the cycles, at 1.6 GHz.  The next tile's scores
+// between a tile's weights and its product cost registers and time (2 x 512 tokens over 4611 keys of 128: 44 -> 51
+// us), tiles of 32 keys and three workgroups per CU too (47).
 template <int HD, bool MX>
 __global__ __launch_bounds__(256, 2) void sink_tile_kernel(SinkArgs a) {
   constexpr int KT = rows_kt(HD), KH = KT / 32, KS = HD / 16, DB = HD / 32, kLead = 4;
@@ -846,7 +855,8 @@ again:
 // ------------------------------------------------------------------ fp32 K/V
 
 // One workgroup per (16-row block, slot), 16-key blocks to the waves in turn; the
-// products, lanes and infinities as in rows_f32_kernel (kvd_rows.hip).
+// products, lanes and infinities as in rows_f32_kernel (kvd_rows.hip).  Bound by round trips: no
+// load is in flight behind the products (one token over 132 keys of 64: 7.2 us).
 constexpr int sink_f32_waves(int hd) { return hd == 64 ? 8 : 4; }  // (8 do not leave the registers for longer rows)
 template <int HD>
 __global__ __launch_bounds__(64 * sink_f32_waves(HD)) void sink_f32_kernel(SinkArgs a) {
@@ -1045,7 +1055,8 @@ again:
 // ------------------------------------------------------------------ merge
 
 // Rows of up to 8 states, or many rows: a thread takes 4 elements of a row, its states 8 at a time in flight.
-// Bound by the states' traffic.  RB: rows of the attention's blocks, which know how many slots they have.
+// Bound by the states' traffic (2 x 512 tokens of 12 heads of 128, up to 5 states a row: 9 us; with a wave to a row
+// 9.9).  RB: rows of the attention's blocks, which know how many slots they have.
 template <typename T, int HD, int RB>
 __global__ __launch_bounds__(256) void sink_merge_kernel(SinkArgs a) {
   constexpr int TPR = HD / 4;
@@ -1182,6 +1193,8 @@ __global__ __launch_bounds__(256) void sink_finish_kernel(SinkArgs a) {
 
 // ------------------------------------------------------------------ launchers
 
+// From as many rows on, those of more than 8 states too are merged by rows side by side (5000 keys of 128: 1200 rows
+// 7.2 us, by four waves each 5.1; 3600 rows 6.8 and 9.0).
 constexpr long long kSinkManyRows = 2048;
 
 template <typename T, int HD>
