@@ -54,6 +54,7 @@ __device__ __forceinline__ bool sink_item(const SinkArgs& a, SinkItem& it) {
 __device__ __forceinline__ size_t sink_state(const SinkArgs& a, int s, int b, int j, int r) {
   return ((size_t)s * a.n_kv + j) * ((size_t)a.B * a.R) + (size_t)b * a.R + r;
 }
+
 // The item's keys in blocks of KB that lie in neighbouring rows each: those of the sinks, of the
 // window up to the ring's end, and behind it.  All of it is uniform.
 template <int KB>
@@ -96,11 +97,13 @@ struct SinkBlocks {
     return b;
   }
 };
+
 // Rows row .. row + n - 1 of an array with `bytes` to a row: reads behind them give 0.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_resource(const void* p, size_t row, int n, int bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(p)) + row * bytes, (short)0,
                                            n * bytes, 0x00027000);
 }
+
 // Element offset of row r of (b, j) in q and out.
 __device__ __forceinline__ size_t sink_q(const SinkArgs& a, int b, int j, int r, int hd) {
   const int i = token_of(a, r);
@@ -158,6 +161,11 @@ __device__ __forceinline__ void split2_trunc(float x, float y, uint32_t (&w)[P])
 
 // ------------------------------------------------------------------ blocks of 16 rows
 
+// Workgroups per CU that the registers are to leave room for.
+constexpr int few_wgs(int hd, bool bf) {
+  return hd == 256 ? (bf ? 2 : 1) : hd == 128 ? 3 : 4;
+}
+
 // One workgroup of 4 waves per (16-row block, slot).  The slot's 32-key blocks go to the waves in
 // turn, each wave with its own slice of LDS and no barrier: HBM-bound, so what matters is
 // loads in flight.
@@ -174,12 +182,8 @@ __device__ __forceinline__ void split2_trunc(float x, float y, uint32_t (&w)[P])
 // 5.5 TB/s; in 4 bits 8 x 32768 rows of them 57 us, 5.0 TB/s; 64 x 4096 .. 8192 rows of 2 heads of 128 27 us, 3.9 TB/s:
 // half the bytes to a block's fixed work, waves waiting for memory 44% of their time.  (Two blocks of these on
 // their way, 204 registers: 37 us.)  A call of few keys takes 5 us, at head_dim 256 7 to 8, most of it instructions.
-// Workgroups per CU that the registers are to leave room for.
-constexpr int few_wgs(int hd, bool mx, bool bf) {
-  return hd == 256 ? (bf ? 2 : 1) : hd == 128 ? 3 : 4;
-}
 template <int HD, bool MX, typename QT>
-__global__ __launch_bounds__(256, few_wgs(HD, MX, sizeof(QT) == 2)) void sink_few_kernel(SinkArgs a) {
+__global__ __launch_bounds__(256, few_wgs(HD, sizeof(QT) == 2)) void sink_few_kernel(SinkArgs a) {
   constexpr bool BF = sizeof(QT) == 2;
   constexpr int NW = 4, KB = 32, KC = HD / 32, DB = HD / 16, kLead = 4;
   constexpr int QP = BF ? 1 : 3, PP = BF ? 2 : 3;  // parts of a query element and of a weight
@@ -453,6 +457,7 @@ again:
       for (int e = 0; e < 4; ++e) x = fmaf(o[db][e], 0.0f, x);
     if (__any(hq < it.nr && x != 0.0f)) {
       pass = 1;
+      if constexpr (!MX) wait_copies<0>();  // the last, empty block's copy is no longer on its way into the slice
       goto again;
     }
   }
@@ -563,8 +568,7 @@ __global__ __launch_bounds__(256, 2) void sink_tile_kernel(SinkArgs a) {
   const int nt = (it.n + KT - 1) / KT;
   const size_t base = ((size_t)it.b * a.n_kv + it.j) * a.t_cap + a.t_off;
 
-  // this lane's row, and what the wave's rows see: all of them x < all.hi with x < sink or x >= all.lo, any of
-  // them x < any_hi with x < sink or x >= any_lo
+  // this lane's row, and what it and the wave's first and last row see: x < hi with x < sink or x >= lo
   const int rl = 32 * w + (lane & 31);
   const bool wave_on = 32 * w < it.nr;
   const auto seen_by = [&](int r) {
