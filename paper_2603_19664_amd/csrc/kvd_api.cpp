@@ -1257,8 +1257,9 @@ bool sink_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T, int32_t
   // drafts over 2056 keys in 8 slots instead of 4 14.8 -> 18.6).  Blocks that windows limit are of one size.  The
   // workspace has room for the slots of a causal call, which has most, and falls with no length.
   // Up to 256 keys, 512 of few rows whose K is short, are one slot: one launch (384 keys in 4 bits: 6.7 to 9.1 us over
-  // the head dims, 8.8 to 10.1 in two; bf16 at head_dim 256: 11.8, 10.9).
-  const bool brief = few && (mx || s->head_dim * (int)elem_size(s) <= 256);
+  // the head dims, 8.8 to 10.1 in two; 512 of bf16 at head_dim 128 8.5, 9.2; 384 at head_dim 256 11.8, 10.9; 500 of
+  // fp32 11.7, 9.9).
+  const bool brief = few && (mx || (s->dtype == KVD_BF16 && s->head_dim <= 128));
   const long long small = brief ? 2 * kvd::kRowsSmall : kvd::kRowsSmall;
   int32_t S = 1;
   p->S = 1;
