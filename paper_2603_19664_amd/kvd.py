@@ -180,6 +180,9 @@ class Shape:
     def _ref(self):
         return ctypes.byref(self.c())
 
+    def __getstate__(self):  # copies and pickles are of the fields alone
+        return {f.name: getattr(self, f.name) for f in dataclasses.fields(self)}
+
     def packed(self) -> "Shape":
         """The same shape with weights in the packed MFMA layout (kvd_pack_weights)."""
         return dataclasses.replace(self, w_layout=KVD_W_PACKED)

@@ -1,6 +1,9 @@
 """kvd_sink_attn, kvd_mx_attn, kvd_mx_store, kvd_mx_load and budget.SinkCache on the CPU: refusals before any HIP call,
 workspace sizes, the binding's checks, the cache's bookkeeping, and the oracle's own properties."""
+import copy
 import ctypes
+import dataclasses
+import pickle
 
 import numpy as np
 import pytest
@@ -218,6 +221,14 @@ def test_binding_checks_extents_and_devices():
             kvd._mx_view(c._replace(**{name: bad}), SH, 2, 0)
     with pytest.raises(ValueError, match="on the GPU"):
         kvd._mx_view(c, SH, 2, 0)
+
+
+def test_a_shape_in_use_is_copied_and_pickled_as_its_fields():
+    s = kvd.Shape(512, 8, 4, 64, 1e-6, 1e4, kvd.KVD_BF16)
+    assert s._ref is s._ref
+    for t in (pickle.loads(pickle.dumps(s)), copy.deepcopy(s), copy.copy(s), dataclasses.replace(s)):
+        assert t == s and hash(t) == hash(s) and t._ref is not s._ref
+    assert s.packed().w_layout == kvd.KVD_W_PACKED and s.packed()._ref is not s._ref
 
 
 # ------------------------------------------------------------------ the cache's bookkeeping
