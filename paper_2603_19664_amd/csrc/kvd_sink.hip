@@ -613,6 +613,11 @@ __global__ __launch_bounds__(256, 2) void sink_tile_kernel(SinkArgs a) {
   u32x4_t kc[RAW ? 1 : NC], vc[RAW ? 1 : NC];
   uint8_t kb[NC], vb[NC];
   auto fetch = [&](int t) {
+    if constexpr (RAW) {  // the wave's reads of its places are done
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+      __builtin_amdgcn_sched_barrier(0);
+    }
     const int k0 = it.x0 + KT * t, n = it.n - KT * t;
     const int tid = RAW ? (int)fresh(threadIdx.x) : (int)threadIdx.x;
 #pragma unroll
