@@ -98,7 +98,8 @@ struct SinkBlocks {
   }
 };
 
-// Rows row .. row + n - 1 of an array with `bytes` to a row: reads behind them give 0.
+// Rows row .. row + n - 1 of an array with `bytes` to a row: reads behind them give 0.  The range check is of
+// the vector offset with the immediate: offsets of rows are in these whole, and the scalar offset is 0.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_resource(const void* p, size_t row, int n, int bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(static_cast<const char*>(p)) + row * bytes, (short)0,
                                            n * bytes, 0x00027000);
@@ -133,7 +134,7 @@ __device__ __forceinline__ void copy_v32(__amdgpu_buffer_rsrc_t res, char* dst) 
   for (int l = 0; l < 32 / RPI; ++l)
     __builtin_amdgcn_raw_ptr_buffer_load_lds(
         res, (__attribute__((address_space(3))) void*)(dst + 1024 * l), 16,
-        (lane / CPR) * HD * 2 + 16 * (lane % CPR ^ few_v_swz<HD>(lane / CPR + RPI * l)), 1024 * l, 0, 0);
+        (lane / CPR) * HD * 2 + 16 * (lane % CPR ^ few_v_swz<HD>(lane / CPR + RPI * l)) + 1024 * l, 0, 0, 0);
 }
 
 // x as a sum of bf16 parts, rounded (P parts), returned as the packed pairs of (x, y).
@@ -267,7 +268,7 @@ __global__ __launch_bounds__(256, few_wgs(HD, sizeof(QT) == 2)) void sink_few_ke
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int c = 0; c < KC; ++c)
-          kp[t][c] = __builtin_amdgcn_raw_buffer_load_b128(res, at + 64 * c, 32 * t * HD, 0);
+          kp[t][c] = __builtin_amdgcn_raw_buffer_load_b128(res, at + 64 * c + 32 * t * HD, 0, 0);
     }
   };
   auto load_v = [&](const Block& kb) {
