@@ -483,7 +483,7 @@ size_t kvd_evict_workspace_bytes(const kvd_attn_shape* shape, int32_t B, int32_t
  * their out rows are left as they were.  What a token does not see has no part in its result,
  * whatever it holds; rows that hold no token that is seen are never read.  An infinite value that it
  * sees makes its column infinite (NaN with both signs), however small the row's weight (of a finite
- * score).
+ * score).  Finite values, up to the type's largest, give finite results.
  * Rows.  The view's slots = t_cap - t_off rows from t_off on hold a sequence's tokens.  With
  * T <= slots token t is in row t_off + t.  With T > slots, which needs slots - sink >=
  * window + N - 1, it is there below sink, and behind that in a ring, in row

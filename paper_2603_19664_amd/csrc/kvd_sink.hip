@@ -160,6 +160,12 @@ __device__ __forceinline__ void split2_trunc(float x, float y, uint32_t (&w)[P])
   }
 }
 
+// Sums of finite values may pass 2^128 where their weighted mean does not.  A wave's sums of 2^117 and more send it
+// through its keys once more, with weights of at most 2^-sum_room(keys that the block sees): all of the block's states
+// together stay below 2^127 then, and those of up to 512 others below 2^126, so no merge overflows.
+__device__ __forceinline__ float too_large(float o, float x) { return fmaf(o * 0x1p11f, 0.0f, x); }  // x, NaN if it is
+__device__ __forceinline__ float sum_room(int n) { return (float)(33 - __clz(n)); }
+
 // ------------------------------------------------------------------ blocks of 16 rows
 
 // Workgroups per CU that the registers are to leave room for.
@@ -300,8 +306,9 @@ __global__ __launch_bounds__(256, few_wgs(HD, sizeof(QT) == 2)) void sink_few_ke
   f32x4_t o[DB];
   float m_run, l_run;
   // A second pass where an infinite or NaN value met a weight of 0: such values count as 0 there and
-  // are added afterwards where they are seen
+  // are added afterwards where they are seen.  A third one for sums that are too large.
   int pass = 0;
+  float lag = 8.0f, room = 0.0f;  // how far the maximum may lie behind; weights are 2^-room of what they would be
   unsigned long long bad = 0;  // bit i % 64: block i of the wave holds such a value
 again:
   Block kb{0, 0, 0};
@@ -380,7 +387,7 @@ again:
     for (int e = 0; e < 8; ++e) mx = fmaxf(mx, st[e >> 2][e & 3]);
     mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * ScoreScale<HD>::v;
-    const bool grow = mx > m_run + 8.0f;
+    const bool grow = mx > m_run + lag;
     if (__any(grow)) {
       const float m_new = grow ? mx : m_run;
       const float alpha = exp2_hw(grow ? m_run - m_new : 0.0f);
@@ -389,7 +396,7 @@ again:
 #pragma unroll
       for (int db = 0; db < DB; ++db) o[db] *= alpha;
     }
-    const float m_use = m_run == -INFINITY ? 0.0f : m_run;
+    const float m_use = (m_run == -INFINITY ? 0.0f : m_run) + room;
     uint32_t pw[PP][4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -405,7 +412,7 @@ again:
     if constexpr (!MX) {
       // V, in order after which the next block's K was asked for
       wait_copies<2 * KC>();
-      if (pass == 1) {
+      if (pass != 0) {
         uint32_t found = 0;
 #pragma unroll 1
         for (int x = lane; x < KB * HD / 2; x += 64) {
@@ -450,20 +457,26 @@ again:
   } else {
     for (int i = 0; i < nb; ++i) step(IC<1>{}, i);
   }
-  if (pass == 0) {
+  l_run += __shfl_xor(l_run, 16, 64);
+  l_run += __shfl_xor(l_run, 32, 64);
+  if (pass < 2) {
     float x = 0.0f;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x = fmaf(o[db][e], 0.0f, x);
-    if (__any(hq < it.nr && x != 0.0f)) {
-      pass = 1;
+      for (int e = 0; e < 4; ++e) x = too_large(o[db][e], x);
+    x += __shfl_xor(x, 16, 64);
+    x += __shfl_xor(x, 32, 64);
+    const bool odd = hq < it.nr && x != 0.0f && (pass == 0 || l_run < INFINITY);  // (a NaN score stays one)
+    if (__any(odd)) {
+      if (++pass == 2 && odd) {  // for such a row alone: what it does not see changes no bit of another
+        lag = 0.0f;
+        room = sum_room(it.keys.n);
+      }
       if constexpr (!MX) wait_copies<0>();  // the last, empty block's copy is no longer on its way into the slice
       goto again;
     }
   }
-  l_run += __shfl_xor(l_run, 16, 64);
-  l_run += __shfl_xor(l_run, 32, 64);
 
   // The waves' states into LDS (16-byte chunks permuted by the row), then merged in wave order:
   // the slot's state, or with one slot the output.
@@ -472,7 +485,7 @@ again:
   constexpr int CM = HD / 4 - 1;
   float* f = reinterpret_cast<float*>(&vbuf[0][0]);
   if (lg == 0) {
-    ml[w][hq][0] = m_run;
+    ml[w][hq][0] = m_run + room;
     ml[w][hq][1] = l_run;
   }
   if (lane == 0) bads[w] = bad;
@@ -492,7 +505,7 @@ again:
     for (int v = 0; v < NW; ++v) {
       const float wt = exp2_hw(ml[v][h][0] - Mu);
       const f32x4_t y = *reinterpret_cast<const f32x4_t*>(f + (v * 16 + h) * HD + 4 * (c4 ^ (h & CM)));
-      x += wt * y;  // (a second pass has left no infinity in a state)
+      x += wt * y;  // (no state holds an infinity, and no sum of them passes 2^128)
       L = fmaf(wt, ml[v][h][1], L);
     }
     // the values that a second pass took as 0, where the row sees them
@@ -656,7 +669,9 @@ __global__ __launch_bounds__(256, 2) void sink_tile_kernel(SinkArgs a) {
 
   // A second pass where an infinite or NaN value met a weight of 0 (a row that does not
   // see it): such values count as 0 there and are added afterwards where they are seen.
+  // A third one for sums that are too large.
   int pass = 0;
+  float lag = 8.0f, room = 0.0f;  // as in sink_few_kernel
   unsigned long long bad = 0;  // bit t % 64: tile t holds such a value
 again:
 #pragma unroll
@@ -678,7 +693,7 @@ again:
     } else {
       if (t + 1 < nt) load(t + 1, next);
     }
-    if (pass == 1) {
+    if (pass != 0) {
       uint32_t found = 0;
       for (int i = threadIdx.x; i < KT * HD / 2; i += 256) {
         uint32_t* x = reinterpret_cast<uint32_t*>(vs) + i;
@@ -732,7 +747,7 @@ again:
 #pragma unroll
       for (int r = 0; r < 16; ++r) mx = fmaxf(mx, st[kh][r]);
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * ScoreScale<HD>::v;
-    const bool grow = mx > m_run + 8.0f;
+    const bool grow = mx > m_run + lag;
     if (__any(grow)) {
       const float m_new = grow ? mx : m_run;
       const float alpha = exp2_hw(grow ? m_run - m_new : 0.0f);
@@ -743,7 +758,7 @@ again:
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[db][i] *= alpha;
     }
-    const float m_use = m_run == -INFINITY ? 0.0f : m_run;
+    const float m_use = (m_run == -INFINITY ? 0.0f : m_run) + room;
     // P as two bf16 parts, p = hi + lo: hi's rounding error is lo
     bf16x8_t hi[2 * KH], lo[2 * KH];
     float sum = 0.0f;
@@ -790,22 +805,26 @@ again:
     if (t + 1 < nt) step(t + 1, buf1, buf0);
   }
   const bool wanted = rl < it.nr;
-  if (pass == 0 && wanted) {
+  l_run += __shfl_xor(l_run, 32, 64);
+  if (pass < 2) {
     float x = 0.0f;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) x = fmaf(o[db][i], 0.0f, x);
-    odd = x != 0.0f;
+      for (int i = 0; i < 16; ++i) x = too_large(o[db][i], x);
+    x += __shfl_xor(x, 32, 64);
+    odd = wanted && x != 0.0f && (pass == 0 || l_run < INFINITY);
   }
-  if (pass == 0 && __syncthreads_or(odd)) {
-    pass = 1;
+  if (pass < 2 && __syncthreads_or(odd)) {
+    if (++pass == 2 && odd) {
+      lag = 0.0f;
+      room = sum_room(it.keys.n);
+    }
     goto again;
   }
-  l_run += __shfl_xor(l_run, 32, 64);
 
-  if (pass == 1) {
-    // the infinite and NaN values that pass 1 took as 0, for the rows that see them
+  if (pass != 0) {
+    // the infinite and NaN values that were taken as 0, for the rows that see them
 #pragma unroll 1
     for (int t = 0; t < nt; ++t) {
       if ((bad >> (t & 63) & 1) == 0 || !wave_on) continue;
@@ -848,7 +867,7 @@ again:
   }
   const size_t row = sink_state(a, it.s, it.b, it.j, it.r0 + rl);
   if (hl == 0) {
-    a.ml[2 * row] = m_run == -INFINITY ? 0.0f : m_run;
+    a.ml[2 * row] = m_run == -INFINITY ? 0.0f : m_run + room;
     a.ml[2 * row + 1] = l_run;
   }
   if (l_run != 0.0f) {
@@ -894,6 +913,7 @@ __global__ __launch_bounds__(64 * sink_f32_waves(HD)) void sink_f32_kernel(SinkA
   f32x4_t o[VU][4];
   float m_run, l_run;
   int pass = 0;
+  float room = 0.0f;  // as in sink_few_kernel
 again:
 #pragma unroll
   for (int u = 0; u < VU; ++u)
@@ -936,13 +956,13 @@ again:
     m_run = m_new;
     float p[4];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) p[r] = exp2_hw(sv[r] - m_use);
+    for (int r = 0; r < 4; ++r) p[r] = exp2_hw(sv[r] - (m_use + room));
     l_run = fmaf(l_run, alpha, (p[0] + p[1]) + (p[2] + p[3]));
 #pragma unroll
     for (int u = 0; u < VU; ++u)
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[u][e] *= alpha;
-    if (pass == 1) {
+    if (pass != 0) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -958,20 +978,26 @@ again:
         for (int e = 0; e < 4; ++e)
           o[u][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[i][u][e], p[i], o[u][e], 0, 0, 0);
   }
-  if (pass == 0) {
+  l_run += __shfl_xor(l_run, 16, 64);
+  l_run += __shfl_xor(l_run, 32, 64);
+  if (pass < 2) {
     float x = 0.0f;
 #pragma unroll
     for (int u = 0; u < VU; ++u)
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) x = fmaf(o[u][e][r], 0.0f, x);
-    if (__any(rq < it.nr && x != 0.0f)) {
-      pass = 1;
+        for (int r = 0; r < 4; ++r) x = too_large(o[u][e][r], x);
+    x += __shfl_xor(x, 16, 64);
+    x += __shfl_xor(x, 32, 64);
+    const bool odd = rq < it.nr && x != 0.0f && (pass == 0 || l_run < INFINITY);
+    if (__any(odd)) {
+      if (++pass == 2 && odd) room = sum_room(it.keys.n);
       goto again;
     }
-  } else {
-    // the values that pass 1 took as 0, for the rows that see them
+  }
+  if (pass != 0) {
+    // the values that were taken as 0, for the rows that see them
 #pragma unroll 1
     for (int t = w; t < nt; t += NW) {
       const int k0 = 16 * t;
@@ -999,8 +1025,7 @@ again:
       }
     }
   }
-  l_run += __shfl_xor(l_run, 16, 64);
-  l_run += __shfl_xor(l_run, 32, 64);
+  m_run += room;
   // the waves' states, merged by the first in wave order.  o[u][e][r]: dim 64 u + 16 lg + 4 r + e
   if (lg == 0) {
     ml[w][rq][0] = m_run;
