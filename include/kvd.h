@@ -515,8 +515,8 @@ size_t kvd_sink_workspace_bytes(const kvd_attn_shape* shape, int32_t B, int32_t 
  *   k, v              [B][n_kv_heads][t_cap][head_dim / 2] bytes
  *   k_scale, v_scale  [B][n_kv_heads][t_cap][head_dim / 32] bytes, E + 127; 255: the group
  *                     is NaN.
- * kvd_mx_store chooses the smallest E in -100 .. 125 with |x| <= 7 2^E for all 32, and rounds
- * x / 2^E to the nearest number (ties to the even code, above 6 to 6); a group that holds an infinity
+ * kvd_mx_store chooses the smallest E in -100 .. 125 with |x| <= 7 2^E for all 32 (125 where none
+ * is), and rounds x / 2^E to the nearest number (ties to the even code, above 6 to 6); a group that holds an infinity
  * or NaN is NaN.  Every value is exact in bf16.  Others may fill a cache too, with scale bytes of
  * 27 .. 252 and 255.                                                           */
 typedef struct {
@@ -544,8 +544,9 @@ kvd_status kvd_mx_load(const kvd_attn_shape* shape, const kvd_mx_view* cache, in
                        void* stream);
 
 /* kvd_sink_attn over a 4-bit cache: the same call, K and V the values that the cache's
- * numbers stand for, exactly (no rounding but the output's; fp32 queries and softmax weights
- * enter the products as three bf16 parts, which hold them whole).  window >= T: the whole cache.  */
+ * numbers stand for, exactly.  Scores, softmax and sums are rounded in fp32 as there; bf16 calls take
+ * a softmax weight as two bf16 parts (2^-17 of it is lost), fp32 calls queries and weights as three,
+ * which hold them whole.  window >= T: the whole cache.                        */
 kvd_status kvd_mx_attn(const kvd_attn_shape* shape, const void* q, int32_t N, const kvd_mx_view* cache,
                        const int32_t* kv_len, const int32_t* n_new, int32_t B, int32_t T, int32_t window,
                        int32_t sink, void* out, void* ws, size_t ws_bytes, void* stream);

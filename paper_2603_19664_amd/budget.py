@@ -268,6 +268,9 @@ class SinkCache:
     newest `window` ones (and `room` - 1 more, so that up to `room` tokens come in one call), in the shape's dtype or,
     with mx, in 4 bits.  Every new token sees the first `sink` tokens and the newest `window`, itself among them.
 
+    A prompt is taken in parts of `room` tokens: the default of 1 is for decoding and runs a prompt token by token, as
+    many launches each as a step; prompts run at full speed in parts of some hundreds, for as many more rows.
+
     Tokens sit at positions pos0, pos0 + 1, ..; a token's K keeps the rotation of its position.
     """
 

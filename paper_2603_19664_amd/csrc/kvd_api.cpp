@@ -1252,7 +1252,7 @@ bool sink_plan(const kvd_attn_shape* s, int32_t B, int32_t N, int32_t T, int32_t
   const long long tokens = std::min<long long>(N, (RB + g - 2) / g + 1), span = (long long)window + tokens - 1;
   const long long keys = std::min<long long>(T, span + sink);
   if (keys > INT32_MAX - 8192 || nb > 65535 || units > INT32_MAX) return false;
-  // Few rows fill the chip once (64 streams of 1028 rows at head_dim 256: 43 us in one slot each, 48 in two), 4 bits
+  // Few rows fill the chip once (64 streams of 1028 rows at head_dim 256: 49 us in one slot each, 55 in two), 4 bits
   // up to three times while a slot keeps 512 keys (8 x 32768 keys 59 -> 57 us, 64 x 4096 .. 8192 keys 32.2 -> 30.2; 16
   // drafts over 2056 keys in 8 slots instead of 4 14.8 -> 18.6).  Blocks that windows limit are of one size.  The
   // workspace has room for the slots of a causal call, which has most, and falls with no length.

@@ -185,7 +185,7 @@ constexpr int few_wgs(int hd, bool bf) {
 // (two for bf16 queries: 2^-17 of a weight is lost; three for fp32), V through LDS: plain by direct copies,
 // 4 bits as the bf16 numbers that they are (one instruction for two), read transposed.
 // K of the next block is asked for when the scores are taken, V after its product.
-// Measured (several caches in turn, so that HBM is read): 64 streams of 1028 bf16 rows, 4 KV heads of 256, 48.6 us,
+// Measured (several caches in turn, so that HBM is read): 64 streams of 1028 bf16 rows, 4 KV heads of 256, 49.2 us,
 // 5.5 TB/s; in 4 bits 8 x 32768 rows of them 57 us, 5.0 TB/s; 64 x 4096 .. 8192 rows of 2 heads of 128 27 us, 3.9 TB/s:
 // half the bytes to a block's fixed work, waves waiting for memory 44% of their time.  (Two blocks of these on
 // their way, 204 registers: 37 us.)  A call of few keys takes 5 us, at head_dim 256 7 to 8, most of it instructions.
@@ -322,7 +322,8 @@ again:
   m_run = -INFINITY;
   l_run = 0.0f;
   // One copy of the code, also for a wave's last block, whose successor is empty: a small call waits for its
-  // instructions (60 ns for 64 bytes), and with a condition around the loads every wait was one for all of them.
+  // instructions (60 ns for 64 bytes).  (The waits for K are shorter than the loads behind it would allow: to the
+  // compiler the queries' loads may still be pending, as they are past the branch of a wave without blocks.)
   auto step = [&](auto second, int i) {
     constexpr bool SECOND = decltype(second)::value != 0;
     const Block kb1 = i + 1 < nb ? blk.at(w + NW * (i + 1)) : Block{0, 0, 0};
@@ -438,7 +439,9 @@ again:
         o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
             vf, __builtin_bit_cast(bf16x8_t, make_uint4(pw[p][0], pw[p][1], pw[p][2], pw[p][3])), o[db], 0, 0, 0);
     }
-    // V operands kLead products ahead: all at once they would take the registers that K waits in
+    // V operands kLead products ahead: all at once they would take the registers that K waits in.  (A hint: in 4 bits
+    // at head_dim 64, and at 128 with fp32 queries, every operand is waited for where it is used, and in the plain
+    // kernel at 256 every wait is one for all reads.)
     __builtin_amdgcn_sched_group_barrier(0x100, 2 * kLead, 0);
 #pragma unroll
     for (int db = 0; db < DB - kLead; ++db) {
@@ -563,7 +566,7 @@ again:
 // computed; the rows of a tile that the sinks' or the ring's end cuts are copied one by one.  4 bits: the
 // next tile's numbers wait as they are and become bf16 in LDS once for the 128 rows.  A
 // wave skips the tiles that none of its rows sees.
-// Measured: 8192 tokens, window 1024, 8 heads of 256: 117 us, 0.55 PFLOP/s of the formula's flops, 0.83 of products
+// Measured: 8192 tokens, window 1024, 8 heads of 256: 113 us, 0.57 PFLOP/s of the formula's flops, 0.86 of products
 // (a large matrix product reaches 1.17); MFMA is busy in half of the cycles, at 1.6 GHz.  The next tile's scores
 // between a tile's weights and its product cost registers and time (2 x 512 tokens over 4611 keys of 128: 44 -> 51
 // us), tiles of 32 keys and three workgroups per CU too (47).
@@ -722,7 +725,8 @@ again:
         st[kh] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[kk], st[kh], 0, 0, 0);
       }
     }
-    // reads kLead operands ahead of the products
+    // reads kLead operands ahead of the products (a hint: with copies of single rows in the loop, global_load_lds, the
+    // compiler makes every wait for LDS one for all reads, so that the lead ends at every fourth operand)
     __builtin_amdgcn_sched_group_barrier(0x100, kLead, 0);
 #pragma unroll
     for (int i = 0; i < KS * KH - kLead; ++i) {
@@ -1227,6 +1231,12 @@ __global__ __launch_bounds__(256) void sink_finish_kernel(SinkArgs a) {
 }
 
 // ------------------------------------------------------------------ launchers
+
+// bf16 calls of more than kRowsFew rows go to the tiles (us per call in blocks of 16 rows, and in tiles).  Plain, 8
+// sequences over 4096 keys: 30 rows of 128 14.6, 16.1; 96 rows 27.7, 19.4; 18 rows of 256 48.5, 36.5; 96 rows 96.7,
+// 50.7; with windows of 1024 (16 sequences) 18 rows of 256 25.5, 27.3, 96 rows 49.5, 35.8.  4 bits at head_dim 128 are
+// even (18 rows 13.0, 12.8; 96 rows 20.3, 19.1; 16 windows of 1024 16.4, 19.8), at 256 blocks of 16 would be faster
+// up to 96 rows (18 rows 21.5, 27.3; 96 rows 41.6, 49.7; windows 17.9, 24.6 and 35.4, 37.6): left to do.
 
 // From as many rows on, those of more than 8 states too are merged by rows side by side (5000 keys of 128: 1200 rows
 // 7.2 us, by four waves each 5.1; 3600 rows 6.8 and 9.0).
